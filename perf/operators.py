@@ -236,8 +236,8 @@ def _plain(s):
             return 0.5 * x * (1 + t), None if dy is None else dy * (0.5 * (1 + t) + 0.5 * x * (1 - t * t) * k * (1 + 3 * c * x * x))
 
         y, _ = act(s["x"].float(), None)
-        q, e = plain_store(s["x"], fmt)
-        again, dx = act(plain_load(q, e, fmt, w), s["dy"].float())
+        q, e = plain_store(s["x"].view(-1, f), fmt)          # rows of f values: gate and up apart
+        again, dx = act(plain_load(q, e, fmt, f).reshape(-1, w), s["dy"].float())
         return {"y": y.to(T), "dx": dx.to(T), "again": again.to(T)}
     if s["kind"] == "dw":
         return s["dy"].float().T @ plain_load(s["q"], s["e"], fmt, s["N"])
@@ -312,7 +312,7 @@ def _own(s):
     if s["kind"] == "act":
         N, f, x = s["N"], s["f"], s["x"]
         y, again, dx = (torch.empty(N, w, dtype=T, device="cuda") for w in (f, f, x.shape[1]))
-        q, e = codes(*x.shape)
+        q, e = codes(x.numel() // f, f)
         zl.zl_op_act8_act(dt, s["act"], fmt, x, N, f, y, q, e, stream)
         zl.zl_op_act8_act_bwd(dt, s["act"], fmt, q, e, s["dy"], N, f, dx, again, stream)
         return {"y": y, "dx": dx, "again": again}
@@ -420,7 +420,7 @@ def exact(case, seed):
                 return torch.sigmoid(g) * g * u
             return 0.5 * x * (1 + torch.tanh(math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)))
 
-        x8 = _exact_codes(s["x"].double(), fmt).requires_grad_(True)
+        x8 = _exact_codes(s["x"].double().view(-1, s["f"]), fmt).reshape(s["x"].shape).requires_grad_(True)
         again = act(x8)
         (dx,) = torch.autograd.grad(again, x8, s["dy"].double())
         return {"y": act(s["x"].double()), "dx": dx, "again": again.detach()}
