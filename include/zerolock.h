@@ -308,6 +308,95 @@ zl_status zl_op_gemm_ex(int dtype, int mode, int M, int N, int K, const void* A,
 zl_status zl_op_qkv_rope(int dtype, int M, int N, int K, const void* A, const void* B, void* C, const float* bias,
                          const float* cs, int S, int hd, int rot_cols, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Activations kept in 8 bits between a chunk's forward and its local backward (no counterpart in the
+ * paper: its executors hold activations in the compute dtype; what a chunk holds until its backward is
+ * the memory that decoupling bounds). A tensor of N rows and d columns is held as codes q [N, D], D =
+ * ZL_ACT8_LD(d), and group bytes e [N, D / 32], both dense: 32 consecutive columns of a row share the
+ * power of two 2^(e - 127), the smallest with (largest finite magnitude) <= Q 2^(e - 127) and e >= 10 (Q = 448 for
+ * e4m3 codes, 127 for integer ones). A code is x 2^(127 - e) rounded to nearest, ties to even; what it
+ * stands for, code * 2^(e - 127), is exactly a bf16, so reading rounds nothing. NaN and infinities are
+ * kept as NaN (code 0x7f, integer code -128), magnitudes above 1.875 2^127 as 1.875 2^127, columns
+ * d .. D - 1 as 0. q must be 16-byte aligned. Sizes: 0 <= N <= 2^24, 1 <= d <= 2^20, N * D < 2^34; with
+ * N = 0 nothing is read or written (a gradient that is not accumulated becomes zero). Tensors in the
+ * compute dtype need the alignment of their elements only; rows that start on 16 bytes are read and
+ * written faster. These calls allocate nothing. Outputs must not overlap inputs except where said.
+ * Errors: ZL_ERR_ARG (a size, format or alignment, a NULL pointer, a workspace that is too small),
+ * ZL_ERR_CUDA (a launch failed); kernels report nothing.
+ * ------------------------------------------------------------------------------------- */
+enum { ZL_ACT8_E4M3 = 0, ZL_ACT8_INT8 = 1 };
+enum { ZL_ACT_SWIGLU = 0, ZL_ACT_GELU = 1 };   /* silu(gate) * up;  GELU (tanh form)        */
+#define ZL_ACT8_MAX_ROWS (1 << 24)
+#define ZL_ACT8_MAX_COLS (1 << 20)
+#define ZL_ACT8_LD(d) (((size_t)(d) + 31) / 32 * 32)
+
+/* x (N rows of d values, ldx apart, ldx >= d) -> q, e; and back: the values in dtype, which need not be
+ * the dtype they were stored from. Columns d .. ldx - 1 of x are neither read nor written. */
+zl_status zl_op_act8_store(int dtype, int fmt, const void* x, int N, int d, int ldx, uint8_t* q, uint8_t* e,
+                           void* stream);
+zl_status zl_op_act8_load(int dtype, int fmt, const uint8_t* q, const uint8_t* e, int N, int d, int ldx, void* x,
+                          void* stream);
+
+/* The activation of a feed-forward block (inside f_k, Eq. 1) that keeps its input in 8 bits. act
+ * ZL_ACT_SWIGLU: x [N, 2 f] = (gate, up), y [N, f] = silu(gate) * up; ZL_ACT_GELU: x, y [N, f]. In the
+ * same pass x is written as q, e: the rows of f values of x, N (GELU) or 2 N (SwiGLU: gate 0, up 0,
+ * gate 1, ..) of them, as zl_op_act8_store writes that many rows. The backward reads x from there: dx
+ * (like x) from dy [N, f], and, if y is not NULL, y [N, f] once more (the input of the next linear,
+ * which need not be kept either). */
+zl_status zl_op_act8_act(int dtype, int act, int fmt, const void* x, int N, int f, void* y, uint8_t* q, uint8_t* e,
+                         void* stream);
+zl_status zl_op_act8_act_bwd(int dtype, int act, int fmt, const uint8_t* q, const uint8_t* e, const void* dy, int N,
+                             int f, void* dx, void* y, void* stream);
+
+/* Weight gradient of a linear from the checkpoint of its input: C [M, N] fp32 = A^T X (accumulate 0) or
+ * C += A^T X (accumulate 1), A [K, M] (dtype) the gradient at the linear's output, X [K, N] held as q, e
+ * (K rows of N columns): mode 2 of zl_op_gemm with its B in 8 bits. ws: a device buffer of at least
+ * zl_op_act8_dw_bytes bytes (256-byte aligned) that no other call uses meanwhile. */
+zl_status zl_op_act8_dw_bytes(int dtype, int M, int N, int K, size_t* bytes);
+zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, const uint8_t* q, const uint8_t* e,
+                        float* C, int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* The step from one block of a layer to the next, fused: the block's output f through its own norm
+ * (post), gated and added to the residual stream h, and the next block's norm (pre):
+ *   p = PostNorm(f);  h' = res_scale h + branch_scale gate * p;  n = PreNorm(h')  (of h' before its rounding)
+ * A norm is ZL_NORM_NONE, ZL_NORM_RMS (x / sqrt(mean x^2 + eps) * w) or ZL_NORM_LAYER ((x - mean x) /
+ * sqrt(var x + eps) * w + b). gate: fp32 rows of d, row n uses row n / gate_rows (gate_rows 0: one row
+ * for all; gate NULL: 1). */
+enum { ZL_NORM_NONE = 0, ZL_NORM_RMS = 1, ZL_NORM_LAYER = 2 };
+typedef struct {
+  int dtype;                /* of h, f, h', n and their gradients                                      */
+  int post_norm, pre_norm;  /* ZL_NORM_*                                                               */
+  int N, d;                 /* rows, columns (sizes as above)                                          */
+  int gate_rows;            /* >= 0                                                                    */
+  float eps;                /* > 0, both norms                                                         */
+  float res_scale, branch_scale;
+  int fmt;                  /* ZL_ACT8_* of the 8-bit tensors of the call                              */
+  int accumulate;           /* backward: 1 adds to the parameters' gradients, 0 overwrites them        */
+} zl_block_norm;
+
+/* Forward. h, f [N, d]; post_w, post_b, pre_w, pre_b fp32 [d] (weights may be NULL: 1; biases only with
+ * ZL_NORM_LAYER, may be NULL: 0) -> h_out [N, d], n_out [N, d] (NULL if and only if pre_norm is
+ * ZL_NORM_NONE) and stats [4, N] fp32: mean and 1 / deviation of the post norm, then of the pre norm (a
+ * mean of 0 except for ZL_NORM_LAYER, 1 / deviation 1 without a norm). f_q, f_e and n_q, n_e (each pair
+ * NULL or not) receive f and n_out in 8 bits. h_out may be h. */
+zl_status zl_op_block_norm(const zl_block_norm* p, const void* h, const void* f, const float* post_w,
+                           const float* post_b, const float* gate, const float* pre_w, const float* pre_b, void* h_out,
+                           void* n_out, float* stats, uint8_t* f_q, uint8_t* f_e, uint8_t* n_q, uint8_t* n_e,
+                           void* stream);
+
+/* Backward, from h_out and stats of the forward and f in dtype (f) or in 8 bits (f_q, f_e; the other
+ * NULL). dn: gradient at n_out (NULL if and only if pre_norm is ZL_NORM_NONE); dh_out: the gradient that
+ * reaches h_out by the residual path (NULL: 0). Writes dh (gradient at h; may be dh_out; NULL: not
+ * formed), df (gradient at f), and where not NULL the fp32 gradients dpost_w, dpost_b [d] (with a post
+ * norm; the bias with ZL_NORM_LAYER), dgate (like gate) and dpre_w, dpre_b [d] (alike). Sums over rows
+ * have a fixed order. ws: zl_op_block_norm_bwd_bytes bytes, as for zl_op_act8_dw. */
+zl_status zl_op_block_norm_bwd_bytes(const zl_block_norm* p, size_t* bytes);
+zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const void* f, const uint8_t* f_q,
+                               const uint8_t* f_e, const float* post_w, const float* post_b, const float* gate,
+                               const float* pre_w, const float* stats, const void* dn, const void* dh_out, void* dh,
+                               void* df, float* dpost_w, float* dpost_b, float* dgate, float* dpre_w, float* dpre_b,
+                               void* ws, size_t ws_bytes, void* stream);
+
 /* Self-test of the bounded waits (no counterpart in the paper; failure detection without a GPU
  * fault). Every wait of the tcgen05 kernels on an mbarrier (a TMA copy landing, a product completing,
  * a tile drained) gives up after about 2 s of SM clock (longer at lower clocks), ORs

@@ -17,6 +17,9 @@ ZL_OK, ZL_ERR_ARG, ZL_ERR_CUDA, ZL_ERR_OOM, ZL_ERR_STATE, ZL_ERR_TIMEOUT, ZL_ERR
 ZL_ARCH_LLAMA, ZL_ARCH_GPT2 = 0, 1
 ZL_DEVERR_BAD_ID, ZL_DEVERR_BAD_LABEL, ZL_DEVERR_TIMEOUT = 1, 2, 4
 ZL_DTYPE_F32, ZL_DTYPE_BF16 = 0, 1
+ZL_ACT8_E4M3, ZL_ACT8_INT8 = 0, 1
+ZL_ACT_SWIGLU, ZL_ACT_GELU = 0, 1
+ZL_NORM_NONE, ZL_NORM_RMS, ZL_NORM_LAYER = 0, 1, 2
 ZL_NOALLOC_MAX_ROWS = 65536   # rows of zl_op_local_loss_noalloc's static scratch (include/zerolock.h)
 
 #: every symbol include/zerolock.h declares
@@ -24,7 +27,9 @@ EXPORTS = ["zl_create", "zl_free", "zl_set_stream", "zl_set_param", "zl_load_wei
            "zl_embed", "zl_forward_chunk", "zl_local_step", "zl_step", "zl_bp_step", "zl_eval_global_loss",
            "zl_read_losses", "zl_join", "zl_synchronize", "zl_peak_bytes", "zl_reset_peak", "zl_last_error",
            "zl_op_local_loss", "zl_op_local_loss_noalloc", "zl_op_head_loss", "zl_op_gemm", "zl_op_gemm_ex", "zl_op_qkv_rope", "zl_op_attention", "zl_op_attention_bwd", "zl_profile", "zl_profile_read", "zl_kernel_launches", "zl_chunk_state_bytes", "zl_chunk_save",
-           "zl_chunk_load", "zl_replay", "zl_wait_selftest"]
+           "zl_chunk_load", "zl_replay", "zl_wait_selftest", "zl_op_act8_store", "zl_op_act8_load", "zl_op_act8_act",
+           "zl_op_act8_act_bwd", "zl_op_act8_dw_bytes", "zl_op_act8_dw", "zl_op_block_norm", "zl_op_block_norm_bwd_bytes",
+           "zl_op_block_norm_bwd"]
 
 
 class zl_model_dims(C.Structure):
@@ -41,6 +46,12 @@ class zl_train_cfg(C.Structure):
                 ("lora_scale", C.c_float), ("replay_depth", C.c_int), ("adapter_dim", C.c_int),
                 ("graph", C.c_int), ("unfused_update", C.c_int), ("loss_rows", C.c_int), ("fuzz_delay_us", C.c_int),
                 ("fuzz_seed", C.c_uint)]
+
+
+class zl_block_norm(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("post_norm", C.c_int), ("pre_norm", C.c_int), ("N", C.c_int), ("d", C.c_int),
+                ("gate_rows", C.c_int), ("eps", C.c_float), ("res_scale", C.c_float), ("branch_scale", C.c_float),
+                ("fmt", C.c_int), ("accumulate", C.c_int)]
 
 
 class ZLError(RuntimeError):
@@ -91,6 +102,15 @@ def _load() -> C.CDLL:
         "zl_chunk_load": [vp, i, vp, sz],
         "zl_replay": [vp, i, C.POINTER(C.c_int), C.POINTER(f)],
         "zl_wait_selftest": [C.POINTER(C.c_uint)],
+        "zl_op_act8_store": [i, i, vp, i, i, i, vp, vp, vp],
+        "zl_op_act8_load": [i, i, vp, vp, i, i, i, vp, vp],
+        "zl_op_act8_act": [i, i, i, vp, i, i, vp, vp, vp, vp],
+        "zl_op_act8_act_bwd": [i, i, i, vp, vp, vp, i, i, vp, vp, vp],
+        "zl_op_act8_dw_bytes": [i, i, i, i, C.POINTER(sz)],
+        "zl_op_act8_dw": [i, i, i, i, i, vp, vp, vp, vp, i, vp, sz, vp],
+        "zl_op_block_norm": [C.POINTER(zl_block_norm)] + [vp] * 15,
+        "zl_op_block_norm_bwd_bytes": [C.POINTER(zl_block_norm), C.POINTER(sz)],
+        "zl_op_block_norm_bwd": [C.POINTER(zl_block_norm)] + [vp] * 19 + [sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -346,6 +366,112 @@ def zl_op_qkv_rope(dtype: int, M: int, N: int, K: int, A, B, Cm, cs, S: int, hd:
     _need_numel(cs, S * hd, "cs")
     _check(_lib.zl_op_qkv_rope(dtype, M, N, K, _p(A), _p(B), _p(Cm), _p(bias) if bias is not None else None, _p(cs),
                                S, hd, rot_cols, stream))
+
+
+def _operands(dtype: int, act, f32=(), codes=()) -> List[Optional[int]]:
+    """Checks the tensors of a call and gives their pointers in order. act, f32, codes: (tensor, elements, name) of the
+    compute dtype, fp32 and uint8; all dense (given with a row stride: (tensor, elements, name, rows, columns)) and on
+    one device, the current one."""
+    import torch
+    at = torch.bfloat16 if dtype == ZL_DTYPE_BF16 else torch.float32
+    cur, out = None, []
+    for group, want in ((act, at), (f32, torch.float32), (codes, torch.uint8)):
+        for t, n, name, *strided in group:
+            if t is None or isinstance(t, int):
+                out.append(t)
+                continue
+            if t.dtype != want:
+                raise TypeError(f"{name}: dtype {t.dtype}, expected {want}")
+            if cur is None:
+                cur = torch.cuda.current_device() if t.is_cuda else -1
+            if not t.is_cuda or t.get_device() != cur:
+                raise ZLError(ZL_ERR_ARG, f"{name}: on {t.device}, expected the current CUDA device")
+            if strided:   # rows of `columns` values, n apart
+                rows, cols = strided
+                if t.dim() != 2 or t.size(0) < rows or t.size(1) < cols or (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != n):
+                    raise ZLError(ZL_ERR_ARG, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, the call takes {rows} rows of {cols}, {n} apart")
+            elif not t.is_contiguous():
+                raise ZLError(ZL_ERR_ARG, f"{name}: not contiguous")
+            elif t.numel() < n:
+                raise ZLError(ZL_ERR_ARG, f"{name}: {t.numel()} elements, the call reads or writes {n}")
+            out.append(t.data_ptr())
+    return out
+
+
+def _codes(q, e, rows: int, d: int, what: str = ""):
+    g = (d + 31) // 32
+    return (q, rows * g * 32, what + "q"), (e, rows * g, what + "e")
+
+
+def zl_op_act8_store(dtype: int, fmt: int, x, N: int, d: int, ldx: int, q, e, stream: int = 0) -> None:
+    """x: 2-D, rows of d values ldx apart."""
+    px, pq, pe = _operands(dtype, [(x, ldx, "x", N, d)], codes=_codes(q, e, N, d))
+    _check(_lib.zl_op_act8_store(dtype, fmt, px, N, d, ldx, pq, pe, stream))
+
+
+def zl_op_act8_load(dtype: int, fmt: int, q, e, N: int, d: int, ldx: int, x, stream: int = 0) -> None:
+    px, pq, pe = _operands(dtype, [(x, ldx, "x", N, d)], codes=_codes(q, e, N, d))
+    _check(_lib.zl_op_act8_load(dtype, fmt, pq, pe, N, d, ldx, px, stream))
+
+
+def zl_op_act8_act(dtype: int, act: int, fmt: int, x, N: int, f: int, y, q, e, stream: int = 0) -> None:
+    w = 2 if act == ZL_ACT_SWIGLU else 1
+    px, py, pq, pe = _operands(dtype, [(x, w * N * f, "x"), (y, N * f, "y")], codes=_codes(q, e, w * N, f))
+    _check(_lib.zl_op_act8_act(dtype, act, fmt, px, N, f, py, pq, pe, stream))
+
+
+def zl_op_act8_act_bwd(dtype: int, act: int, fmt: int, q, e, dy, N: int, f: int, dx, y=None, stream: int = 0) -> None:
+    w = 2 if act == ZL_ACT_SWIGLU else 1
+    pdy, pdx, py, pq, pe = _operands(dtype, [(dy, N * f, "dy"), (dx, w * N * f, "dx"), (y, N * f, "y")],
+                                     codes=_codes(q, e, w * N, f))
+    _check(_lib.zl_op_act8_act_bwd(dtype, act, fmt, pq, pe, pdy, N, f, pdx, py, stream))
+
+
+def zl_op_act8_dw_bytes(dtype: int, M: int, N: int, K: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.zl_op_act8_dw_bytes(dtype, M, N, K, C.byref(n)))
+    return n.value
+
+
+def zl_op_act8_dw(dtype: int, fmt: int, M: int, N: int, K: int, A, q, e, Cm, accumulate: int, ws, stream: int = 0) -> None:
+    """ws: a uint8 tensor of at least zl_op_act8_dw_bytes(dtype, M, N, K) elements."""
+    pa, pc, pq, pe, pw = _operands(dtype, [(A, K * M, "A")], [(Cm, M * N, "C")], [*_codes(q, e, K, N), (ws, 0, "ws")])
+    _check(_lib.zl_op_act8_dw(dtype, fmt, M, N, K, pa, pq, pe, pc, accumulate, pw, 0 if ws is None else ws.numel(), stream))
+
+
+def _gate_numel(p: zl_block_norm) -> int:
+    return (-(-p.N // p.gate_rows) if p.gate_rows > 0 else 1) * p.d
+
+
+def zl_op_block_norm(p: zl_block_norm, h, f, post_w, post_b, gate, pre_w, pre_b, h_out, n_out, stats, f_q=None, f_e=None,
+                     n_q=None, n_e=None, stream: int = 0) -> None:
+    n, d = p.N * p.d, p.d
+    ph, pf, po, pn, *w = _operands(
+        p.dtype, [(h, n, "h"), (f, n, "f"), (h_out, n, "h_out"), (n_out, n, "n_out")],
+        [(post_w, d, "post_w"), (post_b, d, "post_b"), (gate, _gate_numel(p), "gate"), (pre_w, d, "pre_w"), (pre_b, d, "pre_b"),
+         (stats, 4 * p.N, "stats")],
+        [*_codes(f_q, f_e, p.N, d, "f_"), *_codes(n_q, n_e, p.N, d, "n_")])
+    _check(_lib.zl_op_block_norm(C.byref(p), ph, pf, *w[:5], po, pn, *w[5:], stream))
+
+
+def zl_op_block_norm_bwd_bytes(p: zl_block_norm) -> int:
+    n = C.c_size_t()
+    _check(_lib.zl_op_block_norm_bwd_bytes(C.byref(p), C.byref(n)))
+    return n.value
+
+
+def zl_op_block_norm_bwd(p: zl_block_norm, h_out, f, f_q, f_e, post_w, post_b, gate, pre_w, stats, dn, dh_out, dh, df,
+                         dpost_w, dpost_b, dgate, dpre_w, dpre_b, ws, stream: int = 0) -> None:
+    """ws: a uint8 tensor of at least zl_op_block_norm_bwd_bytes(p) elements."""
+    n, d = p.N * p.d, p.d
+    pho, pf, pdn, pdho, pdh, pdf, *w = _operands(
+        p.dtype, [(h_out, n, "h_out"), (f, n, "f"), (dn, n, "dn"), (dh_out, n, "dh_out"), (dh, n, "dh"), (df, n, "df")],
+        [(post_w, d, "post_w"), (post_b, d, "post_b"), (gate, _gate_numel(p), "gate"), (pre_w, d, "pre_w"), (stats, 4 * p.N, "stats"),
+         (dpost_w, d, "dpost_w"), (dpost_b, d, "dpost_b"), (dgate, _gate_numel(p), "dgate"), (dpre_w, d, "dpre_w"),
+         (dpre_b, d, "dpre_b")],
+        [*_codes(f_q, f_e, p.N, d, "f_"), (ws, 0, "ws")])
+    _check(_lib.zl_op_block_norm_bwd(C.byref(p), pho, pf, *w[10:12], *w[:5], pdn, pdho, pdh, pdf, *w[5:10], w[12],
+                                     0 if ws is None else ws.numel(), stream))
 
 
 def zl_profile(ctx, on: bool) -> None:
