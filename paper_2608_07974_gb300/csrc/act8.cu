@@ -145,11 +145,114 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
   if (y) store8(y + (size_t)r * f, c, f, vec, a);
 }
 
+// ------------------------------------------------------------------------------------------------
+// Weight gradient C = A^T X, X from its checkpoint, on the tensor cores in bf16. X is exactly a bf16 matrix, so it is read
+// from its codes once into a workspace (2 bytes a value, which stay in L2 for the product) and the library's GEMM does the
+// rest. An fp32 A is cut into three bf16 terms a = hi + mid + lo, each the leading 8 bits of what is left (truncated, so
+// that nothing overflows and 24 bits are covered exactly); X being exact, the three products in one fp32 accumulation are
+// the fp32 product, at a third of the bf16 rate instead of the fp32 units' (about 1/27 of it). The small terms go first.
+// ------------------------------------------------------------------------------------------------
+struct DwPlan {
+  int Mp, Np, Kp, parts;
+  bool copy_a, pad_c;        // A through the workspace; C through a padded one
+  size_t b, a, c, splits;    // bytes of the workspace's pieces
+};
+size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+DwPlan dw_plan(int dtype, int M, int N, int K) {
+  DwPlan p;
+  auto pad = [](int n) { return std::max(16, (n + 7) / 8 * 8); };
+  p.Mp = pad(M);
+  p.Np = pad(N);
+  p.Kp = (K + 63) / 64 * 64;
+  p.parts = dtype == ZL_DTYPE_F32 ? 3 : 1;
+  p.copy_a = p.parts > 1 || p.Mp != M;
+  p.pad_c = p.Mp != M || p.Np != N;
+  p.b = up256((size_t)K * p.Np * 2);
+  p.a = p.copy_a ? up256((size_t)p.parts * p.Kp * p.Mp * 2) : 0;
+  p.c = p.pad_c ? up256((size_t)p.Mp * p.Np * 4) : 0;
+  p.splits = up256(gemm_tc_dw_bytes(p.Mp, p.Np, K, p.parts));
+  return p;
+}
+
+struct DwPrep {
+  const uint2* q;
+  const uint8_t* e;
+  bf16* B;                   // [K, Np]
+  FastDiv brow;              // Np / 8
+  int gpitch;                // 8-column pieces of codes to a row
+  uint32_t nb, blocks_b;
+  const void* A;
+  bf16* Aw;                  // [parts, Kp, Mp], or NULL
+  FastDiv arow;              // Mp / 8
+  int M, K;
+  bool vec;
+  uint32_t na;               // pieces of one part
+};
+// X from its codes, and A padded or cut into terms; HBM- and L2-bound: 3 bytes a value of X in bf16, 10 of an fp32 A.
+template <typename T, int FMT>
+__global__ void __launch_bounds__(kThreads) dw_prep_k(const DwPrep p) {
+  pdl_wait();
+  pdl_trigger();
+  float f[8];
+  if (blockIdx.x < p.blocks_b) {
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+    if (i >= p.nb) return;
+    const uint32_t r = p.brow.quot(i);
+    const size_t at = (size_t)r * p.gpitch + (i - r * p.brow.d);
+    decode8<FMT>(p.q[at], p.e[at >> 2], f);
+    Vec8<bf16>::store(p.B + (size_t)i * 8, f);
+    return;
+  }
+  const uint32_t i = (blockIdx.x - p.blocks_b) * kThreads + threadIdx.x;
+  if (i >= p.na) return;
+  const uint32_t r = p.arow.quot(i);
+  const int c = (int)(i - r * p.arow.d) * 8;
+  if ((int)r < p.K) load8((const T*)p.A + (size_t)r * p.M, c, p.M, p.vec, f);
+  else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = 0.f;
+  }
+  if (sizeof(T) == 2) {
+    Vec8<bf16>::store(p.Aw + (size_t)i * 8, f);
+    return;
+  }
+  const size_t part = (size_t)p.na * 8;
+#pragma unroll
+  for (int t = 2; t >= 0; --t) {
+    float h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t u = __float_as_uint(f[k]);
+      const bool fin = (u & kInfBits) != kInfBits;
+      h[k] = fin ? __uint_as_float(u & 0xFFFF0000u) : f[k];   // a NaN or an infinity goes whole into the first term
+      f[k] = fin ? f[k] - h[k] : 0.f;
+    }
+    Vec8<bf16>::store(p.Aw + t * part + (size_t)i * 8, h);
+  }
+}
+
+// C [M, N] = or += W [., Np].
+__global__ void __launch_bounds__(kThreads) dw_out_k(const float* __restrict__ W, int Np, float* __restrict__ C, int N, uint32_t n, FastDiv row,
+                                                     int accumulate) {
+  pdl_wait();
+  pdl_trigger();
+  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n) return;
+  const uint32_t r = row.quot(i);   // a thread takes every row.d-th column of a row, neighbours neighbouring ones
+  const int c = (int)(i - r * row.d);
+  float* p = C + (size_t)r * N;
+  const float* w = W + (size_t)r * Np;
+  for (int k = c; k < N; k += (int)row.d) p[k] = accumulate ? p[k] + w[k] : w[k];
+}
+
 bool act_shape(int dtype, int fmt, int N, long long d) {
   return (dtype == ZL_DTYPE_F32 || dtype == ZL_DTYPE_BF16) && (fmt == ZL_ACT8_E4M3 || fmt == ZL_ACT8_INT8) && N >= 0 &&
          N <= ZL_ACT8_MAX_ROWS && d >= 1 && d <= ZL_ACT8_MAX_COLS && (long long)N * pitch((int)d) / 8 < (1ll << 31);
 }
-bool dw_shape(int dtype, int fmt, int M, int N, int K) { return act_shape(dtype, fmt, K, N) && act_shape(dtype, fmt, K, M); }
+// (the product's C is indexed as rows of pieces, too)
+bool dw_shape(int dtype, int fmt, int M, int N, int K) {
+  return act_shape(dtype, fmt, K, N) && act_shape(dtype, fmt, K, M) && act_shape(dtype, fmt, M, N);
+}
 const char* const kShapeMsg =
     "bad dtype, code format, activation or size (0 <= rows <= 2^24, 1 <= columns <= 2^20, rows x columns in whole groups below 2^34, "
     "row strides >= columns, accumulate 0 or 1)";
@@ -203,7 +306,10 @@ void act_bwd_by(int act, const uint8_t* q, const uint8_t* e, const void* dy, int
   else act_bwd_t<T, FMT, ZL_ACT_GELU>(q, e, dy, N, f, vec, dx, y, s);
 }
 
-size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+template <typename T, int FMT>
+void prep_t(const DwPrep& p, unsigned blocks, cudaStream_t s) {
+  launch_pdl(dw_prep_k<T, FMT>, blocks, kThreads, 0, s, p);
+}
 
 }  // namespace
 }  // namespace zl
@@ -265,7 +371,8 @@ zl_status zl_op_act8_act_bwd(int dtype, int act, int fmt, const uint8_t* q, cons
 zl_status zl_op_act8_dw_bytes(int dtype, int M, int N, int K, size_t* bytes) {
   return entry([&]() -> zl_status {
     if (!bytes || !dw_shape(dtype, ZL_ACT8_E4M3, M, N, K)) return fail(ZL_ERR_ARG, kShapeMsg);
-    *bytes = up256((size_t)K * N * dt_size(dtype));
+    const DwPlan p = dw_plan(dtype, M, N, K);
+    *bytes = K ? p.b + p.a + p.c + p.splits : 0;
     return ZL_OK;
   });
 }
@@ -274,17 +381,39 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
                         int accumulate, void* ws, size_t ws_bytes, void* stream) {
   return entry([&]() -> zl_status {
     if (!dw_shape(dtype, fmt, M, N, K) || (accumulate != 0 && accumulate != 1)) return fail(ZL_ERR_ARG, kShapeMsg);
-    if (!C || (K > 0 && (!A || !codes_ok(q, e)))) return fail(ZL_ERR_ARG, kPtrMsg);
-    size_t need = 0;
-    zl_op_act8_dw_bytes(dtype, M, N, K, &need);
-    if (need && (!ws || ((uintptr_t)ws & 255u) || ws_bytes < need))
-      return fail(ZL_ERR_ARG, "the workspace must be 256-byte aligned and hold zl_op_act8_dw_bytes() bytes");
     cudaStream_t s = (cudaStream_t)stream;
-    if (!accumulate && cudaMemsetAsync(C, 0, (size_t)M * N * 4, s) != cudaSuccess) return launched("zl_op_act8_dw");
-    if (K == 0) return ZL_OK;
+    if (K == 0) {
+      if (!C) return fail(ZL_ERR_ARG, kPtrMsg);
+      if (!accumulate) cudaMemsetAsync(C, 0, (size_t)M * N * 4, s);
+      return launched("zl_op_act8_dw");
+    }
+    if (!A || !C || !codes_ok(q, e) || ((uintptr_t)A & 15u) || ((uintptr_t)C & 15u))
+      return fail(ZL_ERR_ARG, "NULL pointer, or A, C or codes that are not 16-byte aligned");
+    const DwPlan p = dw_plan(dtype, M, N, K);
+    if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < p.b + p.a + p.c + p.splits)
+      return fail(ZL_ERR_ARG, "the workspace must be 256-byte aligned and hold zl_op_act8_dw_bytes() bytes");
+    uint8_t* w = (uint8_t*)ws;
+    DwPrep r = {};
+    r.q = (const uint2*)q; r.e = e; r.B = (bf16*)w; r.brow = FastDiv((uint32_t)p.Np / 8); r.gpitch = pitch(N) / 8;
+    r.nb = (uint32_t)((size_t)K * (p.Np / 8));
+    r.blocks_b = (r.nb + kThreads - 1) / kThreads;
+    r.A = A; r.Aw = (bf16*)(w + p.b); r.arow = FastDiv((uint32_t)p.Mp / 8); r.M = M; r.K = K;
+    r.vec = rows_aligned(A, (size_t)M, dtype);
+    r.na = p.copy_a ? (uint32_t)((size_t)p.Kp * (p.Mp / 8)) : 0;
     note_launch(1);
-    ZL_BY_TYPE(load_t, dtype, fmt, q, e, K, N, ws, (size_t)N, rows_aligned(ws, (size_t)N, dtype), s);
-    gemm(dtype, 2, M, N, K, A, ws, C, nullptr, nullptr, s);
+    ZL_BY_TYPE(prep_t, dtype, fmt, r, r.blocks_b + (r.na + kThreads - 1) / kThreads, s);
+    float* out = p.pad_c ? (float*)(w + p.b + p.a) : C;
+    const GemmDw dw{p.parts, p.pad_c || !accumulate, w + p.b + p.a + p.c, p.splits};
+    if (!gemm_tc_dw(p.Mp, p.Np, K, p.copy_a ? (const void*)r.Aw : A, r.B, out, dw, s)) {
+      const zl_status st = launched("zl_op_act8_dw");
+      return st != ZL_OK ? st : fail(ZL_ERR_CUDA, "zl_op_act8_dw: the tensor-core product could not be launched on this device");
+    }
+    if (p.pad_c) {
+      const uint32_t per_row = (uint32_t)(N + 7) / 8;
+      const uint32_t n = (uint32_t)((size_t)M * per_row);
+      note_launch(1);
+      launch_pdl(dw_out_k, (n + kThreads - 1) / kThreads, kThreads, 0, s, (const float*)out, p.Np, C, N, n, FastDiv(per_row), accumulate);
+    }
     return launched("zl_op_act8_dw");
   });
 }

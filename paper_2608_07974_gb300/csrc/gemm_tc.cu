@@ -20,6 +20,7 @@ namespace zl {
 namespace tc {
 
 constexpr int BM = 128, BK = 64;
+constexpr int kSegBlocks = 32;     // k blocks of one accumulation in the weight gradient from checkpoints (DW kernels)
 constexpr int kThreads = 192;      // TMA warp, MMA warp, four epilogue warps
 // Fused-update kernels (mode 4): warpgroup 0 = TMA warp, MMA warp and two idle warps on kRegsLow
 // registers each; then kUpdWarps epilogue warps (two per TMEM lane quadrant) on kRegsUpd, which hold the
@@ -118,6 +119,8 @@ struct Args {
   GemmUpdate u;               // mode 4
   const float2* rope_cs;      // mode 0: rotate-half RoPE of columns < rope_cols (heads of rope_hd = 64 or 128),
   int rope_S, rope_hd, rope_cols;   // row n by position n % rope_S (NULL: none)
+  int kB, kwrap;              // DW kernels: rows and k blocks of B; A holds several such ranges one after another, all against B
+  int kb_per_seg;             // DW kernels: k blocks that one accumulation in TMEM spans; a tile's segments meet in fp32 in C
   int nk2;                    // modes 0/1: further k blocks, of a second product A2 B2 into the same accumulator
                               // (A2 [M, K2] K-major, B2 [K2, N] MN-major; a map's rows past K2 are zeros)
 };
@@ -156,7 +159,12 @@ __device__ __forceinline__ void unit_tile(const Args& g, int unit, int num_tiles
 // first CTA issues read both CTAs' shared memory. What bounds the single-CTA mainloop is shared memory (128
 // bytes a cycle): a 128 x 256 x 64 block reads 48 KB and its copies write 48 KB, 768 cycles against 512 of
 // products. A pair's CTA reads and writes 32 KB each per 512 cycles, and six stages fit instead of four.
-template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false>
+// DW (a kernel of its own too, mode 2 or 3): the accumulation is cut into segments of kb_per_seg k blocks. The tensor cores
+// truncate as they add to an accumulator, an error that grows with the number of additions and always points to zero:
+// relative to an fp64 product 3.5e-6 over K = 8192 in one accumulation, 1.35e-5 over 65536 (an fp32 library product 3.5e-7
+// and 1e-6). Segments of at most 2048 are added to C by the TMA unit, which rounds to nearest: 9e-7 and less at any K. The
+// epilogue of a segment runs under the products of the next one, C's tiles stay in L2 meanwhile.
+template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false, bool DW = false>
 __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
     gemm_tc_k(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
               const __grid_constant__ CUtensorMap tcm, const __grid_constant__ CUtensorMap ta2,
@@ -241,6 +249,7 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
             // the second product's blocks follow the first's, from its own maps, B2 as an MN-major operand
             const bool ext = !A_MN && kb >= nk1;
             const int k0 = (ext ? kb - nk1 : kb) * BK;
+            const int k0b = DW ? kb % g.kwrap * BK : k0;
             const CUtensorMap* ma = ext ? &ta2 : &ta;
             const CUtensorMap* mb = ext ? &tb2 : &tb;
             const bool b_mn = B_MN || ext;
@@ -256,10 +265,10 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
                 tma2d_pair(sa + 8192, ma, bar, tm * BM + 64, k0);
               }
               if (!b_mn) {
-                tma2d_pair(sb, mb, bar, k0, n0);
+                tma2d_pair(sb, mb, bar, k0b, n0);
               } else {
   #pragma unroll
-                for (int j = 0; j < HB / 64; ++j) tma2d_pair(sb + j * 8192, mb, bar, n0 + 64 * j, k0);
+                for (int j = 0; j < HB / 64; ++j) tma2d_pair(sb + j * 8192, mb, bar, n0 + 64 * j, k0b);
               }
             } else {
               mbar_expect_tx(&full[stage], C_::STAGE_BYTES);
@@ -270,10 +279,10 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
                 tma2d(sa + 8192, ma, &full[stage], tm * BM + 64, k0);
               }
               if (!b_mn) {
-                tma2d(sb, mb, &full[stage], k0, tn * BN);
+                tma2d(sb, mb, &full[stage], k0b, tn * BN);
               } else {
   #pragma unroll
-                for (int j = 0; j < BN / 64; ++j) tma2d(sb + j * 8192, mb, &full[stage], tn * BN + 64 * j, k0);
+                for (int j = 0; j < BN / 64; ++j) tma2d(sb + j * 8192, mb, &full[stage], tn * BN + 64 * j, k0b);
               }
             }
           }
@@ -307,12 +316,15 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
       uint32_t phase = 0;
       bool ok = true;
       for (int unit = unit0; (!PAIR || crank == 0) && ok && unit < num_units; unit += ustride, ++it) {
+        int kb0 = (unit / num_tiles) * g.kb_per_split;
+        const int kbe = min(nk, kb0 + g.kb_per_split);
+        do {   // once, but for DW's segments
+        const int kb1 = DW ? min(kbe, kb0 + g.kb_per_seg) : kbe;
         const int acc = it & 1;
         const uint32_t aph = (uint32_t)(it >> 1) & 1u;
-        if (!uwait(&tempty[acc], aph ^ 1u, abort_flag, g.err)) break;
+        if (!uwait(&tempty[acc], aph ^ 1u, abort_flag, g.err)) { ok = false; break; }
         fence_after();
         const uint32_t d = tmem + (uint32_t)(acc * BN);
-        const int kb0 = (unit / num_tiles) * g.kb_per_split, kb1 = min(nk, kb0 + g.kb_per_split);
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!uwait(&full[stage], phase, abort_flag, g.err)) { ok = false; break; }
           fence_after();
@@ -339,6 +351,11 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
           else mma_commit(&tfull[acc]);
         }
         __syncwarp();
+        if (DW) {
+          kb0 = kb1;
+          if (kb0 < kbe) ++it;
+        }
+        } while (DW && ok && kb0 < kbe);
       }
       // all MMAs issued by the leader complete before TMEM is released
       if (leader) {
@@ -451,13 +468,16 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
       int tm, tn;
       unit_tile(g, unit, num_tiles, PAIR, crank, tm, tn);
       const int split = unit / num_tiles;
+      int ok = 1, left = DW ? min(nk - split * g.kb_per_split, g.kb_per_split) : 0;   // k blocks of the unit's segments to come
+      bool later = false;   // a later segment: added to what the first one wrote
+      do {   // once, but for DW's segments
       const int acc = it & 1;
       const uint32_t aph = (uint32_t)(it >> 1) & 1u;
-      int ok = 1;
       if (lane == 0) ok = mbar_wait(&tfull[acc], aph, abort_flag, g.err) ? 1 : 0;
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
       fence_after();
+      if (DW && later && lane == 0) bulk_wait_all();   // the segment before has reached C: the additions keep their order
       const int row0 = tm * BM + q * 32;
       const int m = row0 + lane;
       const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
@@ -588,6 +608,7 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
         if (lane == 0) {
           if (row0 < g.M && n0 < g.N) {
             if (g.mode == 2) tma_reduce_add2d(&tcm, sbuf, n0, row0);
+            else if (DW && later) tma_reduce_add3d(&tcm, sbuf, n0, row0, split);
             else if (g.mode == 3) tma_store3d(&tcm, sbuf, n0, row0, split);
             else tma_store2d(&tcm, sbuf, n0, row0);
           }
@@ -600,6 +621,13 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
         if (PAIR) mbar_arrive_cluster(tempty_addr + 8u * (uint32_t)acc);
         else mbar_arrive(&tempty[acc]);
       }
+      if (DW) {
+        left -= g.kb_per_seg;
+        later = true;
+        if (left > 0) ++it;
+      }
+      } while (DW && left > 0);
+      if (!ok) break;
     }
     if (lane == 0) bulk_wait_all();   // every store of this warp has landed in global memory
   }
@@ -630,7 +658,7 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
 }
 
 // Sums the split-K partials in split order (deterministic) and applies the epilogue (mode 4: the fused
-// optimizer step of `u`, as the fused epilogue does it).
+// optimizer step of `u`, as the fused epilogue does it; mode 3: the sum itself, fp32).
 __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M, int N, int mode, void* C,
                                 const float* __restrict__ bias, const bf16* R, float alpha, int rmode,
                                 const GemmUpdate u) {
@@ -671,6 +699,8 @@ __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M,
         const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         Vec8<float>::store(u.g + e, z);
       }
+    } else if (mode == 3) {
+      Vec8<float>::store((float*)C + e, acc);
     } else if (mode == 2) {
       float c[8];
       Vec8<float>::load((float*)C + e, c);
@@ -751,12 +781,12 @@ bool make_map_c(CUtensorMap* m, const Args& a) {
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false>
+template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false, bool DW = false>
 bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int ctas_per_sm, const GemmExt* ext = nullptr) {
   using C_ = Cfg<BN, UPD, PAIR>;
   static bool attr = false;
   static int max_pairs = 0;   // clusters of two that can be resident at once
-  auto kern = gemm_tc_k<BN, A_MN, B_MN, UPD, PAIR>;
+  auto kern = gemm_tc_k<BN, A_MN, B_MN, UPD, PAIR, DW>;
   if (!attr) {
     if (UPD) {   // the register split of the fused-update kernels must fit the pool the CTA is launched with
       cudaFuncAttributes fa;
@@ -790,7 +820,8 @@ bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int cta
   const bool okA = A_MN ? make_map(&ta, A, (uint64_t)a.M, (uint64_t)a.K, 64, 64)
                         : make_map(&ta, A, (uint64_t)a.K, (uint64_t)a.M, 64, BM);
   // a pair's CTA loads half of a K-major B tile (BN / 2 rows); MN-major B tiles are 64-column boxes
-  const bool okB = B_MN ? make_map(&tb, B, (uint64_t)a.N, (uint64_t)a.K, 64, 64)
+  const uint64_t kB = DW ? (uint64_t)a.kB : (uint64_t)a.K;
+  const bool okB = B_MN ? make_map(&tb, B, (uint64_t)a.N, kB, 64, 64)
                         : make_map(&tb, B, (uint64_t)a.K, (uint64_t)a.N, 64, PAIR ? BN / 2 : BN);
   CUtensorMap tcm;
   if (!okA || !okB || !make_map_c(&tcm, a)) return false;
@@ -841,6 +872,15 @@ bool launch_upd(int bn, bool pair, const Args& a, const void* A, const void* B, 
   return pair ? launch<128, true, true, true, true>(a, A, B, s, 1) : launch<128, true, true, true>(a, A, B, s, 1);
 }
 
+// The weight gradient from checkpoints (DW kernels).
+bool launch_dw(int bn, bool pair, const Args& a, const void* A, const void* B, cudaStream_t s) {
+  if (bn == 256)
+    return pair ? launch<256, true, true, false, true, true>(a, A, B, s, 1) : launch<256, true, true, false, false, true>(a, A, B, s, 1);
+  if (bn == 128)
+    return pair ? launch<128, true, true, false, true, true>(a, A, B, s, 1) : launch<128, true, true, false, false, true>(a, A, B, s, 1);
+  return launch<64, true, true, false, false, true>(a, A, B, s, 2);
+}
+
 // The plan of a product: tile width, split count, and whether CTA pairs run it.
 struct Plan {
   int bn, splits, pair;
@@ -873,6 +913,7 @@ Plan choose(int mode, int M, int N, int K, bool rotates = false) {
   };
   static const Kind kinds[] = {{256, 1, 0.295, 2.6}, {128, 1, 0.200, 2.1}, {256, 0, 0.350, 1.6}, {128, 0, 0.240, 1.4},
                                {64, 0, 0.330, 0.6}};
+  const int sms = g_sms > 0 ? g_sms : 152;   // (a workspace may be sized before the device is known)
   const double hbm = 6.0e6;                  // bytes / us
   const bool dw = mode == 2 || mode == 4;    // both operands MN-major
   const double off_a = (dw ? M : K) % 64 != 0, off_b = (mode == 0 ? K : N) % 64 != 0;   // rows off 128-byte lines
@@ -885,7 +926,7 @@ Plan choose(int mode, int M, int N, int K, bool rotates = false) {
     if (c.pair && M <= BM) continue;   // nothing to pair
     const long tm = (M + BM - 1) / BM, tn = (N + c.bn - 1) / c.bn;
     const long tiles = c.pair ? (tm + 1) / 2 * tn : tm * tn;
-    const long slots = c.pair ? g_sms / 2 : (long)g_sms * (c.bn == 64 ? 2 : 1);
+    const long slots = c.pair ? sms / 2 : (long)sms * (c.bn == 64 ? 2 : 1);
     // the update's epilogue per unit: 26 bytes for each element of a CTA's tile at about 85 bytes per ns and SM
     const double nb = c.pair ? c.bn / 2 : c.bn;   // a CTA copies 128 rows of A and these of B per k block
     const double kb = c.kb * (dw ? 1.06 : 1.0) * (1.0 + 0.3 * (BM * off_a + nb * off_b) / (BM + nb));
@@ -915,9 +956,9 @@ namespace {
 // is outside the kernel's rules.
 bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C, const float* bias, const void* R,
             unsigned* err, cudaStream_t s, cudaMemPool_t pool, float alpha, int rmode, const GemmUpdate* u,
-            const GemmRope* rope = nullptr, const GemmExt* ext = nullptr) {
+            const GemmRope* rope = nullptr, const GemmExt* ext = nullptr, const GemmDw* dw = nullptr) {
   if (!tc::init()) return false;
-  if (M < 16 || N < 16 || K < 16) return false;
+  if (M < 16 || N < 16 || (K < 16 && !dw)) return false;
   auto al16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
   if (!al16(A) || !al16(B) || !al16(C) || (R && !al16(R)) || (bias && !al16(bias))) return false;   // all read 16 bytes at a time
   // the fused update: 16-byte aligned state rows, a compute copy, no accumulated gradient
@@ -933,6 +974,8 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
   if (mode >= 2 && M % 8 != 0) return false;
   if (ext && (mode > 1 || ext->K2 < 16 || ext->K2 % 8 != 0 || !ext->A2 || !ext->B2 || !al16(ext->A2) || !al16(ext->B2)))
     return false;
+  const int kB = K, kblocks = (K + tc::BK - 1) / tc::BK;
+  if (dw && dw->parts > 1) K = dw->parts * kblocks * tc::BK;   // A's ranges, each of whole k blocks
   const tc::Plan plan = tc::choose(mode, M, N, K, rope != nullptr);
   int bn = plan.bn, splits = plan.splits, pair = plan.pair;
   if (const char* force = std::getenv("ZL_GEMM_TILE")) {   // test hook "BN:SPLITS[:PAIR]": forces the plan
@@ -965,13 +1008,19 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
   a.group_m = (a_bytes <= 48e6 || a_bytes <= b_bytes) ? a.tiles_m : std::min(8, a.tiles_m);
   if (pair) a.group_m = (a.group_m + 1) / 2;   // in pairs of tile rows
   a.nk2 = ext ? (ext->K2 + tc::BK - 1) / tc::BK : 0;
+  a.kwrap = kblocks;
+  a.kB = kB;
   const int nk = (K + tc::BK - 1) / tc::BK + a.nk2;
   a.kb_per_split = (nk + splits - 1) / splits;
   a.splits = (nk + a.kb_per_split - 1) / a.kb_per_split;   // no empty split (its slice would never be formed)
   float* ws = nullptr;
   if (a.splits > 1) {
     const size_t bytes = (size_t)a.splits * M * N * 4;
-    cudaError_t e = pool ? cudaMallocFromPoolAsync((void**)&ws, bytes, pool, s) : cudaMallocAsync((void**)&ws, bytes, s);
+    cudaError_t e;
+    if (dw) {   // the caller's workspace
+      ws = (float*)dw->ws;
+      e = bytes <= dw->ws_bytes ? cudaSuccess : cudaErrorMemoryAllocation;
+    } else e = pool ? cudaMallocFromPoolAsync((void**)&ws, bytes, pool, s) : cudaMallocAsync((void**)&ws, bytes, s);
     if (e != cudaSuccess) {   // no room for the partials: one split
       cudaGetLastError();
       ws = nullptr;
@@ -985,10 +1034,14 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
       a.alpha = 1.f;   // applied by the reduction
     }
   }
+  const int segs = (a.kb_per_split + tc::kSegBlocks - 1) / tc::kSegBlocks;   // of equal length
+  a.kb_per_seg = (a.kb_per_split + segs - 1) / segs;
+  if (dw && dw->overwrite && !ws) a.mode = 3;   // the tiles stored where the sums would be added (one slice)
   note_launch(1);
   bool ok;
   if (mode == 0) ok = tc::launch_bn<false, false>(bn, pair, a, A, B, s, ext);
   else if (mode == 1) ok = tc::launch_bn<false, true>(bn, pair, a, A, B, s, ext);
+  else if (dw) ok = tc::launch_dw(bn, pair, a, A, B, s);
   else if (a.mode == 4) ok = tc::launch_upd(bn, pair, a, A, B, s);
   else ok = tc::launch_bn<true, true>(bn, pair, a, A, B, s);
   if (ws) {
@@ -996,10 +1049,10 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
       note_launch(1);
       const size_t n8 = (size_t)M * N / 8;
       const int blocks = (int)std::min<size_t>((n8 + 255) / 256, (size_t)tc::g_sms * 8);
-      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, mode, C, bias, (const bf16*)R, alpha,
+      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, dw && dw->overwrite ? 3 : mode, C, bias, (const bf16*)R, alpha,
                  rmode, a.u);
     }
-    cudaFreeAsync(ws, s);
+    if (!dw) cudaFreeAsync(ws, s);
   }
   return ok;
 }
@@ -1010,6 +1063,16 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
 bool gemm_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C, const float* bias, const void* R,
              unsigned* err, cudaStream_t s, cudaMemPool_t pool, float alpha, int rmode) {
   return run_tc(mode, M, N, K, A, B, C, bias, R, err, s, pool, alpha, rmode, nullptr);
+}
+
+bool gemm_tc_dw(int M, int N, int K, const void* A, const void* B, float* C, const GemmDw& dw, cudaStream_t s) {
+  return run_tc(2, M, N, K, A, B, C, nullptr, nullptr, nullptr, s, nullptr, 1.f, 0, nullptr, nullptr, nullptr, &dw);
+}
+
+size_t gemm_tc_dw_bytes(int M, int N, int K, int parts) {
+  if (M < 16 || N < 16 || K < 1) return 0;
+  const int sp = tc::choose(2, M, N, parts > 1 ? parts * ((K + tc::BK - 1) / tc::BK * tc::BK) : K).splits;
+  return sp > 1 ? (size_t)sp * M * N * 4 : 0;
 }
 
 bool gemm_tc_update(int M, int N, int K, const void* A, const void* B, const GemmUpdate& u, unsigned* err,

@@ -101,7 +101,7 @@ def test_activations_refuse(B, bad):
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=-1), dict(fmt=2), dict(M=0), dict(N=0), dict(K=-1), dict(A=None), dict(q=None), dict(C=None),
-                                 dict(acc=2), dict(ws=None), dict(ws="small")])
+                                 dict(acc=2), dict(ws=None), dict(ws="small"), dict(A=P + 8), dict(C=P + 4)])
 def test_weight_gradient_refuses(B, bad):
     a = dict(dtype=1, fmt=0, M=32, N=64, K=16, A=P, q=P, e=P, C=P, acc=0, ws="ok") | bad
     n = B.zl_op_act8_dw_bytes(1, 32, 64, 16)
@@ -363,6 +363,39 @@ def test_weight_gradient(B, dtype, fmt, M, N, K):
     again = C0.cuda()
     B.zl_op_act8_dw(code(B, dtype), fmt, M, N, K, A.cuda(), q.cuda(), e.cuda(), again, 1, ws)
     assert torch.equal(C, again)
+
+
+@gpu
+@pytest.mark.parametrize("plan", ["", "256:1:1", "256:1:0", "128:1:1", "128:1:0", "64:1", "256:2:1", "64:3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [4096, 4500, 6145])
+def test_weight_gradient_over_many_tokens(B, monkeypatch, dtype, plan, K):
+    """Sums cut into segments of at most 2048 tokens (fp32: of 2048 rows of its three terms), under every kind of plan: the
+    truncation of one accumulation, at most a step for each of 2048 products and sums of |A| |X|, and a rounding for each
+    of the segments (at most 12) and splits; the products of 512 x 520 in blocks that the tiles do not divide."""
+    if plan:
+        monkeypatch.setenv("ZL_GEMM_TILE", plan)
+    M, N = 520, 328
+    g = torch.Generator(device="cuda").manual_seed(K)
+    A = (torch.randn(K, M, generator=g, device="cuda") + 0.5).to(R.DT[dtype])
+    x = (torch.randn(K, N, generator=g, device="cuda") + 0.5).to(R.DT[dtype])
+    q, e = empty_codes(K, N)
+    B.zl_op_act8_store(code(B, dtype), R.INT8, x, K, N, N, q, e)
+    X = torch.empty(K, N, device="cuda")
+    B.zl_op_act8_load(B.ZL_DTYPE_F32, R.INT8, q, e, K, N, N, X)
+    ref, scale = (A.double().T @ X.double()).cpu(), (A.double().abs().T @ X.double().abs()).cpu()
+    ws = torch.empty(B.zl_op_act8_dw_bytes(code(B, dtype), M, N, K), dtype=torch.uint8, device="cuda")
+    C = torch.full((M, N), float("nan"), device="cuda")
+    B.zl_op_act8_dw(code(B, dtype), R.INT8, M, N, K, A, q, e, C, 0, ws)
+    bound = (2048 + 64 + 16) * 2.0 ** -23 * scale
+    R.assert_close(C, ref, bound, "C")
+    C0 = torch.randn(M, N, generator=g, device="cuda")
+    outs = []
+    for _ in range(2):
+        outs.append(C0.clone())
+        B.zl_op_act8_dw(code(B, dtype), R.INT8, M, N, K, A, q, e, outs[-1], 1, ws)
+    R.assert_close(outs[0], ref + C0.cpu().double(), bound + 16 * 2.0 ** -23 * C0.cpu().double().abs(), "C +=")
+    assert torch.equal(*outs)
 
 
 @gpu
