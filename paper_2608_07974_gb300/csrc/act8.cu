@@ -23,8 +23,8 @@ struct Items {
 // ------------------------------------------------------------------------------------------------
 // Rows to 8 bits and back. HBM-bound: 3.03 bytes a value in bf16, 5.03 in fp32.
 // ------------------------------------------------------------------------------------------------
-template <typename T, int FMT>
-__global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, bool vec, Items it,
+template <typename T, int FMT, bool VEC>
+__global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it,
                                                     uint2* __restrict__ q, uint8_t* __restrict__ e) {
   pdl_wait();
   pdl_trigger();
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, siz
   float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (in) {
     const uint32_t r = it.row.quot(i);
-    load8(x + r * ldx, (int)(i - r * it.row.d) * 8, d, vec, f);
+    load8<VEC>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
   }
   uint2 w;
   const uint32_t b = encode_quarter<FMT>(f, w);
@@ -43,9 +43,9 @@ __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, siz
   }
 }
 
-template <typename T, int FMT>
+template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e, Items it,
-                                                   T* __restrict__ x, size_t ldx, int d, bool vec) {
+                                                   T* __restrict__ x, size_t ldx, int d) {
   pdl_wait();
   pdl_trigger();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, 
   const uint32_t r = it.row.quot(i);
   float f[8];
   decode8<FMT>(q[i], e[i >> 2], f);
-  store8(x + r * ldx, (int)(i - r * it.row.d) * 8, d, vec, f);
+  store8<VEC>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -70,8 +70,8 @@ __device__ __forceinline__ float sigm(float x) {
 constexpr float kGeluK = 0.7978845608028654f, kGeluC = 0.044715f;
 
 // x [N, f] (GELU) or [N, 2 f] (SwiGLU: gate, up); codes of the rows of f values: [N, D] or [N, 2 D], D = pitch(f).
-template <typename T, int FMT, int ACT>
-__global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, bool vec, Items it, T* __restrict__ y,
+template <typename T, int FMT, int ACT, bool VEC>
+__global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, Items it, T* __restrict__ y,
                                                   uint2* __restrict__ q, uint8_t* __restrict__ e) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
   pdl_wait();
@@ -80,12 +80,13 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
   const bool in = i < it.n;
   const uint32_t r = in ? it.row.quot(i) : 0, c8 = i - r * it.row.d;
   const int c = (int)c8 * 8;
-  float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (in) {
-    const T* xr = x + (size_t)r * W * f;
-    load8(xr, c, f, vec, g);
-    if (W == 2) load8(xr + f, c, f, vec, u);
-  }
+  const T* xr = x + (size_t)r * W * f;
+  const Raw8<T> rg = load_raw<VEC>(xr, c, in ? f : 0);
+  Raw8<T> ru;
+  if (W == 2) ru = load_raw<VEC>(xr + f, c, in ? f : 0);
+  float g[8], u[8];
+  floats(rg, g);
+  if (W == 2) floats(ru, u);
   uint2 w;
   uint32_t b = encode_quarter<FMT>(g, w);
   size_t at = (size_t)r * W * it.row.d + c8;
@@ -107,12 +108,12 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
     if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
     else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
   }
-  store8(y + (size_t)r * f, c, f, vec, g);
+  store8<VEC>(y + (size_t)r * f, c, f, g);
 }
 
-template <typename T, int FMT, int ACT>
+template <typename T, int FMT, int ACT, bool VEC>
 __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
-                                                      const T* __restrict__ dy, int f, bool vec, Items it,
+                                                      const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
   pdl_wait();
@@ -123,9 +124,13 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
   const int c = (int)c8 * 8;
   const size_t at = (size_t)r * W * it.row.d + c8;
   float g[8], u[8], t[8], a[8];
-  decode8<FMT>(q[at], e[at >> 2], g);
-  if (W == 2) decode8<FMT>(q[at + it.row.d], e[(at + it.row.d) >> 2], u);
-  load8(dy + (size_t)r * f, c, f, vec, t);
+  const size_t at2 = W == 2 ? at + it.row.d : at;
+  const Raw8<T> rt = load_raw<VEC>(dy + (size_t)r * f, c, f);
+  const uint2 qg = q[at], qu = q[at2];
+  const uint32_t eg = e[at >> 2], eu = e[at2 >> 2];
+  floats(rt, t);
+  decode8<FMT>(qg, eg, g);
+  if (W == 2) decode8<FMT>(qu, eu, u);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     if (W == 2) {
@@ -140,9 +145,9 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
     }
   }
   T* dr = dx + (size_t)r * W * f;
-  store8(dr, c, f, vec, g);
-  if (W == 2) store8(dr + f, c, f, vec, u);
-  if (y) store8(y + (size_t)r * f, c, f, vec, a);
+  store8<VEC>(dr, c, f, g);
+  if (W == 2) store8<VEC>(dr + f, c, f, u);
+  if (y) store8<VEC>(y + (size_t)r * f, c, f, a);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -207,7 +212,10 @@ __global__ void __launch_bounds__(kThreads) dw_prep_k(const DwPrep p) {
   if (i >= p.na) return;
   const uint32_t r = p.arow.quot(i);
   const int c = (int)(i - r * p.arow.d) * 8;
-  if ((int)r < p.K) load8((const T*)p.A + (size_t)r * p.M, c, p.M, p.vec, f);
+  if ((int)r < p.K) {
+    if (p.vec) load8<true>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
+    else load8<false>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
+  }
   else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] = 0.f;
@@ -265,22 +273,23 @@ unsigned blocks_of(const Items& it) { return (it.n + kThreads - 1) / kThreads; }
 template <typename T, int FMT>
 void store_t(const void* x, size_t ldx, int N, int d, bool vec, uint8_t* q, uint8_t* e, cudaStream_t s) {
   const Items it = items(N, d);
-  launch_pdl(store_k<T, FMT>, blocks_of(it), kThreads, 0, s, (const T*)x, ldx, d, vec, it, (uint2*)q, e);
+  launch_pdl(vec ? store_k<T, FMT, true> : store_k<T, FMT, false>, blocks_of(it), kThreads, 0, s, (const T*)x, ldx, d, it, (uint2*)q, e);
 }
 template <typename T, int FMT>
 void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, bool vec, cudaStream_t s) {
   const Items it = items(N, d);
-  launch_pdl(load_k<T, FMT>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, it, (T*)x, ldx, d, vec);
+  launch_pdl(vec ? load_k<T, FMT, true> : load_k<T, FMT, false>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, it, (T*)x, ldx, d);
 }
 template <typename T, int FMT, int ACT>
 void act_t(const void* x, int N, int f, bool vec, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
   const Items it = items(N, f);
-  launch_pdl(act_k<T, FMT, ACT>, blocks_of(it), kThreads, 0, s, (const T*)x, f, vec, it, (T*)y, (uint2*)q, e);
+  launch_pdl(vec ? act_k<T, FMT, ACT, true> : act_k<T, FMT, ACT, false>, blocks_of(it), kThreads, 0, s, (const T*)x, f, it, (T*)y, (uint2*)q, e);
 }
 template <typename T, int FMT, int ACT>
 void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, bool vec, void* dx, void* y, cudaStream_t s) {
   const Items it = items(N, f);
-  launch_pdl(act_bwd_k<T, FMT, ACT>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, vec, it, (T*)dx, (T*)y);
+  launch_pdl(vec ? act_bwd_k<T, FMT, ACT, true> : act_bwd_k<T, FMT, ACT, false>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, it, (T*)dx,
+             (T*)y);
 }
 
 // fn<T, FMT>(args) for the run-time dtype and format.

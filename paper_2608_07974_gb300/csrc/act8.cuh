@@ -47,16 +47,23 @@ __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)
 // The scale of a group byte.
 __device__ __forceinline__ float group_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Bits of the largest magnitude of N values that a group counts: finite ones, none above the top.
-template <int N>
-__device__ __forceinline__ uint32_t amax_bits(const float* x) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-  if (m > kTopBits) {   // hardly ever: a NaN, an infinity or a value beyond the top among them
+// max(|a|, |b|, |c|), a NaN if one is among them.
+__device__ __forceinline__ float absmax3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Bits of the largest magnitude of 8 values that a group counts: finite ones, none above the top; odd: others are among them.
+__device__ __forceinline__ uint32_t amax_bits(const float* x, bool& odd) {
+  float v = absmax3(x[0], x[1], x[2]);
+  v = absmax3(v, x[3], x[4]);
+  v = absmax3(v, x[5], x[6]);
+  uint32_t m = __float_as_uint(absmax3(v, x[7], x[7]));
+  odd = m > kTopBits;
+  if (odd) {   // hardly ever: a NaN, an infinity or a value beyond the top among them
     m = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < 8; ++i) {
       const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
       m = max(m, u < kInfBits ? min(u, kTopBits) : 0u);
     }
@@ -64,45 +71,42 @@ __device__ __forceinline__ uint32_t amax_bits(const float* x) {
   return m;
 }
 
-// Four codes of four values, given 2^-E of their group.
+// Four codes of four values, given 2^-E of their group. odd: a NaN, an infinity or a value beyond the top is among them.
+// Integer codes: adding 1.5 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits.
 template <int FMT>
-__device__ __forceinline__ uint32_t encode4(const float* x, float inv) {
-  const float top = __uint_as_float(kTopBits);
+__device__ __forceinline__ uint32_t encode4(const float* x, float inv, bool odd) {
   float y[4];
-  bool odd = false;   // a value that the plain conversion would not keep as it should
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = x[i] * inv;
-    odd |= (__float_as_uint(x[i]) & 0x7FFFFFFFu) > kTopBits;
-  }
+  for (int i = 0; i < 4; ++i) y[i] = x[i] * inv;
   if (odd) {
+    const float top = __uint_as_float(kTopBits);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
       y[i] = u >= kInfBits ? __uint_as_float(0x7FC00000u) : fminf(fmaxf(x[i], -top), top) * inv;
     }
   }
+  uint32_t w;
   if (FMT == ZL_ACT8_E4M3) {
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
-    uint32_t w = lo | (hi << 16);
-    if (odd) {   // one NaN code: the positive one
+    w = __byte_perm(lo, hi, 0x5410);
+  } else {
+    uint32_t b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (((w >> (8 * i)) & 0x7Fu) == 0x7Fu) w &= ~(0x80u << (8 * i));
-    }
-    return w;
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(y[i] + 12582912.f);
+    w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   }
-  uint32_t w = 0;
+  if (odd) {   // one NaN code
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = odd && y[i] != y[i] ? -128 : __float2int_rn(y[i]);
-    w |= ((uint32_t)c & 0xFFu) << (8 * i);
+    for (int i = 0; i < 4; ++i)
+      if (y[i] != y[i]) w = (w & ~(0xFFu << (8 * i))) | ((FMT == ZL_ACT8_E4M3 ? 0x7Fu : 0x80u) << (8 * i));
   }
   return w;
 }
 
-// The four values of four codes, given their group's 2^E.
+// The four values of four codes, given their group's 2^E. Integer codes: code + 128 as the low mantissa byte of 2^23, less
+// 2^23 + 128.
 template <int FMT>
 __device__ __forceinline__ void decode4(uint32_t w, float scale, float* x) {
   if (FMT == ZL_ACT8_E4M3) {
@@ -114,31 +118,83 @@ __device__ __forceinline__ void decode4(uint32_t w, float scale, float* x) {
       x[2 * i + 1] = f.y * scale;
     }
   } else {
+    const uint32_t v = w ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i)) * scale;
-    const uint32_t v = w ^ 0x80808080u;   // a zero byte where a code is -128
-    if ((v - 0x01010101u) & ~v & 0x80808080u) {
+    for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(v, 0x4B000000u, 0x7540 + i)) - 8388736.f) * scale;
+    if ((v - 0x01010101u) & ~v & 0x80808080u) {   // a zero byte: a code of -128
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (((w >> (8 * i)) & 0xFFu) == 0x80u) x[i] = __uint_as_float(0x7FC00000u);
+        if (((v >> (8 * i)) & 0xFFu) == 0u) x[i] = __uint_as_float(0x7FC00000u);
     }
   }
 }
 
-// 8 values of a row at column c of d: one or two wide accesses where the row is 16-byte aligned (vec) and has all eight,
-// else one value at a time; columns from d on read 0 and are not written.
+// 8 values of a row at column c of d. VEC: rows start on 16 bytes, and all but a row's last few values are read 16 bytes at
+// a time; else one value at a time. Columns from d on read 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread
+// are all under way before the first of them is waited for.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int c, int d, bool vec, float* f) {
-  if (vec && c + 8 <= d) {
-    Vec8<T>::load(p + c, f);
-    return;
+struct Raw8;
+template <>
+struct Raw8<bf16> {
+  uint4 u;
+  __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(const void* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void pairs(uint64_t* f) const {
+    f[0] = bf2_to_f2(u.x); f[1] = bf2_to_f2(u.y); f[2] = bf2_to_f2(u.z); f[3] = bf2_to_f2(u.w);
   }
+  __device__ __forceinline__ void put(int i, bf16 v) {
+    const uint32_t b = __bfloat16_as_ushort(v);
+    uint32_t& w = i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w;
+    w |= i & 1 ? b << 16 : b;
+  }
+};
+template <>
+struct Raw8<float> {
+  float4 u, v;
+  __device__ __forceinline__ void zero() { u = v = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(const void* p) {
+    u = reinterpret_cast<const float4*>(p)[0];
+    v = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void pairs(uint64_t* f) const { f[0] = f2(u.x, u.y); f[1] = f2(u.z, u.w); f[2] = f2(v.x, v.y); f[3] = f2(v.z, v.w); }
+  __device__ __forceinline__ void put(int i, float x) {
+    (i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : i == 3 ? u.w : i == 4 ? v.x : i == 5 ? v.y : i == 6 ? v.z : v.w) = x;
+  }
+};
+__device__ __forceinline__ void unpair(const uint64_t* p, float* f) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = c + i < d ? to_f(p[c + i]) : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = uf2(p[i]);
+    f[2 * i] = v.x;
+    f[2 * i + 1] = v.y;
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ Raw8<T> load_raw(const T* p, int c, int d) {
+  Raw8<T> r;
+  if (VEC && c + 8 <= d) {
+    r.get(p + c);
+  } else {
+    r.zero();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < d) r.put(i, p[c + i]);
+  }
+  return r;
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* p, int c, int d, bool vec, const float* f) {
-  if (vec && c + 8 <= d) {
+__device__ __forceinline__ void floats(const Raw8<T>& r, float* f) {
+  uint64_t p[4];
+  r.pairs(p);
+  unpair(p, f);
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(const T* p, int c, int d, float* f) {
+  floats(load_raw<VEC>(p, c, d), f);
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
+  if (VEC && c + 8 <= d) {
     Vec8<T>::store(p + c, f);
     return;
   }
@@ -151,13 +207,14 @@ __device__ __forceinline__ void store8(T* p, int c, int d, bool vec, const float
 // every lane of the warp calls): returns the codes in q and E + 127.
 template <int FMT>
 __device__ __forceinline__ uint32_t encode_quarter(const float* x, uint2& q) {
-  uint32_t m = amax_bits<8>(x);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  bool odd;
+  const uint32_t mine = amax_bits(x, odd);
+  uint32_t m = max(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
   const int E = group_exp<FMT>(m);
   const float inv = pow2(-E);
-  q.x = encode4<FMT>(x, inv);
-  q.y = encode4<FMT>(x + 4, inv);
+  q.x = encode4<FMT>(x, inv, odd);
+  q.y = encode4<FMT>(x + 4, inv, odd);
   return (uint32_t)(E + 127);
 }
 template <int FMT>
@@ -185,7 +242,7 @@ inline zl_status launched(const char* what) {
   return e == cudaSuccess ? ZL_OK : fail(ZL_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
 }
 
-// Whether rows of ld values from p can be read 16 bytes at a time.
+// Whether rows from p, ld values apart, start on 16 bytes (VEC).
 inline bool rows_aligned(const void* p, size_t ld, int dt) {
   return ((uintptr_t)p & 15u) == 0 && ld * (dt == ZL_DTYPE_BF16 ? 2 : 4) % 16 == 0;
 }

@@ -5,6 +5,7 @@
 
 #include "act8.cuh"
 #include "ops.h"
+#include "tcgen05.cuh"
 
 namespace zl {
 
@@ -37,126 +38,308 @@ __device__ __forceinline__ void put_codes(int fmt, const float* x, uint8_t* q, u
   if ((at & 31) == 0) e[at >> 5] = (uint8_t)b;
 }
 
-// A row in registers: a warp per row (WARP: D <= 1024) or a block (D <= 16384), thread t holding the 8-column vectors
-// t + j * (threads of the row). One read of h and f, one write of what is asked for; variances are of the centred
-// values.
-template <typename T, bool WARP, int VPT>
-__global__ void __launch_bounds__(WARP ? 256 : 512) fwd_reg_k(const Fwd a) {
+// ------------------------------------------------------------------------------------------------
+// Rows through a ring in shared memory, shared by forward and backward: a block (of as many threads as a row has 8-column
+// vectors, or half or a quarter of them) works through its rows one after another while the next rows' tensors are
+// copied in (bulk copies of whole rows on an mbarrier). What such a row costs a block is two block-wide sums, one after the
+// other, and no wait for memory; what bounds the kernel is then HBM.
+// BULK: rows start on 16 bytes; else the block copies a row itself, value by value and without running ahead.
+// ------------------------------------------------------------------------------------------------
+constexpr int kStages = 4;
+
+__device__ __forceinline__ void bulk_row(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(tc::su32(dst)),
+               "l"(src), "r"(bytes), "r"(tc::su32(bar))
+               : "memory");
+}
+
+// Sums over the block of one or two values; every thread gets them. The scratch alternates between two buffers, so one
+// barrier per sum is enough: who writes a buffer again has passed the barrier of the sum between, after which everyone
+// had read it. `ok` is and-ed over the block on the way.
+struct Reducer {
+  float (*sh)[2][16];
+  int turn;
+  __device__ __forceinline__ bool sum(float& x, float& y, bool two, bool ok) {
+    const int w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    x = warp_sum(x);
+    if (two) y = warp_sum(y);
+    float(*b)[16] = sh[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) {
+      b[0][w] = x;
+      if (two) b[1][w] = y;
+    }
+    ok = __syncthreads_and(ok);
+    x = 0.f;
+    for (int i = 0; i < nw; i += 4) {   // entries past nw are 0
+      const float4 v = *reinterpret_cast<const float4*>(&b[0][i]);
+      x += (v.x + v.y) + (v.z + v.w);
+    }
+    if (two) {
+      y = 0.f;
+      for (int i = 0; i < nw; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(&b[1][i]);
+        y += (v.x + v.y) + (v.z + v.w);
+      }
+    }
+    return ok;
+  }
+};
+
+// What a launch of a ring kernel is given besides its operands.
+struct Ring {
+  int stages, rows;   // rows: of a block, one after another
+  uint32_t pitch;     // bytes of a row of T in shared memory (whole groups)
+  uint32_t stage;     // bytes of a stage
+};
+
+// 8 columns of a parameter row as pairs: `none` where it is NULL, 0 past d.
+template <bool VEC>
+__device__ __forceinline__ void row8(const float* p, int c, int d, float none, uint64_t* w) {
+  if (p) load_raw<VEC>(p, c, d).pairs(w);
+  else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = f2(none, none);
+  }
+}
+// Sums of the two halves of pairs.
+__device__ __forceinline__ float fold(uint64_t v) {
+  const float2 f = uf2(v);
+  return f.x + f.y;
+}
+// Pairs with 0 in the columns from d on.
+__device__ __forceinline__ void cut(uint64_t* v, int c, int d) {
+  if (c + 8 <= d) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = uf2(v[i]);
+    v[i] = f2(c + 2 * i < d ? f.x : 0.f, c + 2 * i + 1 < d ? f.y : 0.f);
+  }
+}
+
+// The parameters of a thread's columns: a = beta gate w_post, b = beta gate b_post, w = w_pre, v = b_pre. They stay in
+// registers from row to row (a and b until the gate's row changes): read for every row they were 48 KB more a row than its
+// 32 KB of traffic (d = 4096, bf16), and their latency the longest part of it. BIAS: b and v exist.
+template <int VPT, bool VEC, bool BIAS>
+struct Params {
+  uint64_t a[VPT][4], b[BIAS ? VPT : 1][4], w[VPT][4], v[BIAS ? VPT : 1][4];
+  __device__ __forceinline__ void post(int j, int c, int d, const float* pw, const float* pb, const float* gate, float beta) {
+    uint64_t g[4];
+    row8<VEC>(gate, c, d, 1.f, g);
+    row8<VEC>(pw, c, d, 1.f, a[j]);
+    if (BIAS) row8<VEC>(pb, c, d, 0.f, b[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      g[i] = mul2(g[i], f2(beta, beta));
+      a[j][i] = mul2(a[j][i], g[i]);
+      if (BIAS) b[j][i] = mul2(b[j][i], g[i]);
+    }
+  }
+  __device__ __forceinline__ void pre(int j, int c, int d, const float* nw, const float* nb) {
+    row8<VEC>(nw, c, d, 1.f, w[j]);
+    if (BIAS) row8<VEC>(nb, c, d, 0.f, v[j]);
+  }
+};
+
+// VEC: rows start on 16 bytes; they come by bulk copies. KEEP: f or n are written in 8 bits.
+template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
+__global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t full[kStages];
+  __shared__ __align__(16) float sh[2][2][16];
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  const int t = threadIdx.x, nt = blockDim.x;
+  const int r0 = (int)blockIdx.x * g.rows, rows = min(g.rows, a.N - r0);
+  const uint32_t bytes = (uint32_t)a.d * sizeof(T);
+  if (t == 0) {
+    for (int i = 0; i < g.stages; ++i) tc::mbar_init(&full[i], 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = t; i < 64; i += nt) (&sh[0][0][0])[i] = 0.f;
+  for (int k = 0; k < 2 * g.stages; ++k)   // columns past d read 0
+    for (int c = a.d + t; c < a.D; c += nt) reinterpret_cast<T*>(ring + (k >> 1) * g.stage + (k & 1) * g.pitch)[c] = from_f<T>(0.f);
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
-  __shared__ float sh[32];
-  const int row = WARP ? (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5) : (int)blockIdx.x;
-  if (row >= a.N) return;
-  const int t = WARP ? (threadIdx.x & 31) : threadIdx.x, nt = WARP ? 32 : blockDim.x;
-  auto sum = [&](float v) { return WARP ? warp_sum(v) : block_sum(v, sh); };
-  const size_t o = (size_t)row * a.d;
-  const float inv_d = 1.f / a.d;
-  float f[VPT][8], h[VPT][8];
-#pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int c = (t + j * nt) * 8;
-    load8((const T*)a.f + o, c, a.d, a.vec, f[j]);
-    load8((const T*)a.h + o, c, a.d, a.vec, h[j]);
-  }
-  if (a.fq) {
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int c = (t + j * nt) * 8;
-      put_codes(a.fmt, f[j], a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
-    }
-  }
-  float mean = 0.f, rstd = 1.f;
-  auto stat = [&](float (&x)[VPT][8], int kind) {
-    mean = 0.f;
-    rstd = 1.f;
-    if (kind == ZL_NORM_NONE) return;
-    if (kind == ZL_NORM_LAYER) {
-      float s = 0.f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += x[j][i];
-      mean = sum(s) * inv_d;
-    }
-    float q = 0.f;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int c = (t + j * nt) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = c + i < a.d ? x[j][i] - mean : 0.f;
-        q += v * v;
+  auto fill = [&](int k) {   // row number k of this block
+    uint8_t* p = ring + (k % g.stages) * g.stage;
+    const size_t o = (size_t)(r0 + k) * a.d;
+    if (VEC) {
+      uint64_t* bar = &full[k % g.stages];
+      tc::mbar_expect_tx(bar, 2 * bytes);
+      bulk_row(p, (const T*)a.f + o, bytes, bar);
+      bulk_row(p + g.pitch, (const T*)a.h + o, bytes, bar);
+    } else {
+      for (int c = t; c < a.d; c += nt) {
+        reinterpret_cast<T*>(p)[c] = ((const T*)a.f)[o + c];
+        reinterpret_cast<T*>(p + g.pitch)[c] = ((const T*)a.h)[o + c];
       }
     }
-    rstd = 1.f / sqrtf(sum(q) * inv_d + a.eps);
   };
-  stat(f, a.post);
-  if (t == 0) {
-    a.stats[row] = mean;
-    a.stats[(size_t)a.N + row] = rstd;
-  }
-  const float* gr = a.gate ? a.gate + gate_row(row, a.gate_rows) * a.d : nullptr;
+  if (VEC && t == 0)
+    for (int k = 0; k < min(rows, g.stages); ++k) fill(k);
+  Params<VPT, VEC, BIAS> pa;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int c = (t + j * nt) * 8;
-    if (a.post) {
+  for (int j = 0; j < VPT; ++j) pa.pre(j, (t + j * nt) * 8, a.d, a.nw, a.nb);
+  size_t gate_at = ~(size_t)0;
+  Reducer red{sh, 0};
+  const float inv_d = 1.f / a.d;
+  const uint64_t alpha = f2(a.alpha, a.alpha);
+  int k = 0;
+  for (; k < rows; ++k) {
+    const int row = r0 + k, st = k % g.stages;
+    const size_t o = (size_t)row * a.d, gr = gate_row(row, a.gate_rows);
+    if (gr != gate_at) {
+      gate_at = gr;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[j][i] = (f[j][i] - mean) * rstd;
-      float w[8];
-      if (a.pw) {
-        load8(a.pw, c, a.d, a.wvec, w);
+      for (int j = 0; j < VPT; ++j) pa.post(j, (t + j * nt) * 8, a.d, a.pw, a.pb, a.gate ? a.gate + gr * a.d : nullptr, a.beta);
+    }
+    bool ok = true;
+    if (VEC) {
+      ok = tc::mbar_wait(&full[st], (uint32_t)(k / g.stages) & 1u, abort_flag, nullptr);
+    } else {
+      __syncthreads();
+      fill(k);
+      __syncthreads();
+    }
+    Raw8<T> rf[VPT], rh[VPT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[j][i] *= w[i];
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (t + j * nt) * 8;
+      rf[j].zero();
+      rh[j].zero();
+      if (c < a.D) {
+        rf[j].get(ring + st * g.stage + c * sizeof(T));
+        rh[j].get(ring + st * g.stage + g.pitch + c * sizeof(T));
       }
-      if (a.pb) {
-        load8(a.pb, c, a.d, a.wvec, w);
+    }
+    float unused = 0.f, mean = 0.f, rstd = 1.f;
+    uint64_t h[VPT][4];
+    // mean and 1 / deviation of the values val(j, x) of every vector; after the first barrier of a row everyone has it in
+    // registers, and its stage takes the row `stages` further on
+    auto stat = [&](int kind, auto&& val, bool first) {
+      mean = 0.f;
+      rstd = 1.f;
+      auto next = [&]() {
+        if (VEC && first && ok && t == 0 && k + g.stages < rows) fill(k + g.stages);
+        first = false;
+      };
+      if (kind == ZL_NORM_LAYER) {
+        uint64_t s = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[j][i] += w[i];
+        for (int j = 0; j < VPT; ++j) {
+          uint64_t x[4];
+          val(j, x);
+          s = add2(s, add2(add2(x[0], x[1]), add2(x[2], x[3])));
+        }
+        float m = fold(s);
+        ok = red.sum(m, unused, false, ok);
+        next();
+        mean = m * inv_d;
+      }
+      if (kind != ZL_NORM_NONE) {
+        const uint64_t mm = f2(mean, mean);
+        uint64_t q2 = 0;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (t + j * nt) * 8;
+          uint64_t x[4];
+          val(j, x);
+          if (kind == ZL_NORM_LAYER) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = sub2(x[i], mm);
+            cut(x, c, a.d);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q2 = fma2(x[i], x[i], q2);
+        }
+        float q = fold(q2);
+        ok = red.sum(q, unused, false, ok);
+        next();
+        rstd = 1.f / sqrtf(q * inv_d + a.eps);
+      } else if (first) {
+        ok = __syncthreads_and(ok);
+        next();
+      }
+    };
+    if (KEEP && a.fq) {
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        float x[8];
+        floats(rf[j], x);
+        put_codes(a.fmt, x, a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
       }
     }
-    if (gr) {
-      float w[8];
-      load8(gr, c, a.d, a.wvec, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[j][i] *= w[i];
+    stat(a.post, [&](int j, uint64_t* x) { rf[j].pairs(x); }, true);
+    if (!ok) break;
+    if (t == 0) {
+      a.stats[row] = mean;
+      a.stats[(size_t)a.N + row] = rstd;
     }
+    {
+      const uint64_t mm = f2(mean, mean), rr = f2(rstd, rstd);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[j][i] = c + i < a.d ? a.alpha * h[j][i] + a.beta * f[j][i] : 0.f;
-    store8((T*)a.ho + o, c, a.d, a.vec, h[j]);
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        uint64_t f[4];
+        rf[j].pairs(f);
+        rh[j].pairs(h[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (a.post == ZL_NORM_LAYER) f[i] = sub2(f[i], mm);
+          h[j][i] = fma2(mul2(f[i], rr), pa.a[j][i], mul2(alpha, h[j][i]));
+          if (BIAS) h[j][i] = add2(h[j][i], pa.b[j][i]);
+        }
+        cut(h[j], c, a.d);
+        float x[8];
+        unpair(h[j], x);
+        store8<VEC>((T*)a.ho + o, c, a.d, x);
+      }
+    }
+    stat(a.pre, [&](int j, uint64_t* x) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = h[j][i];
+    }, false);
+    if (t == 0) {
+      a.stats[2 * (size_t)a.N + row] = mean;
+      a.stats[3 * (size_t)a.N + row] = rstd;
+    }
+    if (!a.pre) continue;
+    const uint64_t mm = f2(mean, mean), rr = f2(rstd, rstd);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (t + j * nt) * 8;
+      float n[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (a.pre == ZL_NORM_LAYER) h[j][i] = sub2(h[j][i], mm);
+        h[j][i] = mul2(mul2(h[j][i], rr), pa.w[j][i]);
+        if (BIAS) h[j][i] = add2(h[j][i], pa.v[j][i]);
+      }
+      cut(h[j], c, a.d);
+      unpair(h[j], n);
+      store8<VEC>((T*)a.no + o, c, a.d, n);
+      if (KEEP && a.nq) {   // of n as it is stored
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] = to_f(from_f<T>(n[i]));
+        put_codes(a.fmt, n, a.nq, a.ne, (size_t)row * a.D + c, c < a.D);
+      }
+    }
   }
-  stat(h, a.pre);
-  if (t == 0) {
-    a.stats[2 * (size_t)a.N + row] = mean;
-    a.stats[3 * (size_t)a.N + row] = rstd;
-  }
-  if (!a.pre) return;
-#pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int c = (t + j * nt) * 8;
-    float w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[j][i] = (h[j][i] - mean) * rstd;
-    if (a.nw) {
-      load8(a.nw, c, a.d, a.wvec, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] *= w[i];
-    }
-    if (a.nb) {
-      load8(a.nb, c, a.d, a.wvec, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] += w[i];
-    }
-    store8((T*)a.no + o, c, a.d, a.vec, h[j]);
-    if (a.nq) {   // of n as it is stored
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] = c + i < a.d ? to_f(from_f<T>(h[j][i])) : 0.f;
-      put_codes(a.fmt, h[j], a.nq, a.ne, (size_t)row * a.D + c, c < a.D);
+  if (VEC && k < rows && t == 0) {   // a wait gave up: let the copies in flight land before the block ends
+    for (int i = k; i < min(rows, k + g.stages); ++i) {
+      const unsigned long long t0 = tc::gtimer();
+      while (!tc::mbar_test(&full[i % g.stages], (uint32_t)(i / g.stages) & 1u) && tc::gtimer() - t0 < 100000000ull) {
+      }
     }
   }
 }
 
 // Rows of any width: a block per row that reads it again for every sum.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   pdl_wait();
   pdl_trigger();
@@ -166,27 +349,27 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   const float inv_d = 1.f / a.d;
   const float* gr = a.gate ? a.gate + gate_row(row, a.gate_rows) * a.d : nullptr;
   float pm = 0.f, pr = 1.f, m = 0.f, r = 1.f;
-  auto fval = [&](int c, float* x) { load8((const T*)a.f + o, c, a.d, a.vec, x); };
+  auto fval = [&](int c, float* x) { load8<VEC>((const T*)a.f + o, c, a.d, x); };
   auto hval = [&](int c, float* x) {   // h' before its rounding
     float f[8], w[8];
     fval(c, f);
-    load8((const T*)a.h + o, c, a.d, a.vec, x);
+    load8<VEC>((const T*)a.h + o, c, a.d, x);
     if (a.post) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = (f[i] - pm) * pr;
       if (a.pw) {
-        load8(a.pw, c, a.d, a.wvec, w);
+        load8<VEC>(a.pw, c, a.d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] *= w[i];
       }
       if (a.pb) {
-        load8(a.pb, c, a.d, a.wvec, w);
+        load8<VEC>(a.pb, c, a.d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += w[i];
       }
     }
     if (gr) {
-      load8(gr, c, a.d, a.wvec, w);
+      load8<VEC>(gr, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] *= w[i];
     }
@@ -232,21 +415,21 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
       put_codes(a.fmt, x, a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
     }
     hval(c, x);
-    store8((T*)a.ho + o, c, a.d, a.vec, x);
+    store8<VEC>((T*)a.ho + o, c, a.d, x);
     if (!a.pre) continue;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (x[i] - m) * r;
     if (a.nw) {
-      load8(a.nw, c, a.d, a.wvec, w);
+      load8<VEC>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] *= w[i];
     }
     if (a.nb) {
-      load8(a.nb, c, a.d, a.wvec, w);
+      load8<VEC>(a.nb, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] += w[i];
     }
-    store8((T*)a.no + o, c, a.d, a.vec, x);
+    store8<VEC>((T*)a.no + o, c, a.d, x);
     if (a.nq) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = c + i < a.d ? to_f(from_f<T>(x[i])) : 0.f;
@@ -255,25 +438,60 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   }
 }
 
-template <typename T>
-void forward(const Fwd& a, cudaStream_t s) {
+// Blocks of a kernel (th threads, `smem` dynamic bytes) that an SM holds, from the registers that it was compiled with.
+struct Occupancy {
+  int regs = 0, fixed = 0;
+  bool ok = false;
+  template <typename K>
+  explicit Occupancy(K kern) {
+    cudaFuncAttributes fa;
+    ok = cudaFuncGetAttributes(&fa, kern) == cudaSuccess &&
+         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - (int)fa.sharedSizeBytes) == cudaSuccess;
+    regs = (fa.numRegs + 7) / 8 * 8;
+    fixed = (int)fa.sharedSizeBytes + 1024;
+  }
+  int blocks(int th, size_t smem) const {
+    return std::max(1, std::min({2048 / th, 65536 / (regs * th), (int)((kMaxSmem + 1024) / (smem + fixed)), 32}));
+  }
+  static constexpr int kMaxSmem = 232448;
+};
+
+template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
+bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
+  static const Occupancy occ(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>);
+  if (!occ.ok) return false;
+  Ring g;
+  g.pitch = (uint32_t)a.D * sizeof(T);
+  g.stage = 2 * g.pitch;
+  const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), 16}));   // blocks that the registers allow
+  const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, (size_t)occ.fixed) - occ.fixed;
+  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : 1;
+  if (VEC && (size_t)g.stages * g.stage + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
+  const size_t smem = (size_t)g.stages * g.stage;
+  if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
+  const int slots = sm_count() * occ.blocks(th, smem);
+  g.rows = (a.N + slots - 1) / slots;
+  return launch_pdl(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>, (a.N + g.rows - 1) / g.rows, th, smem, s, a, g) == cudaSuccess;
+}
+template <typename T, int VPT, bool VEC>
+bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
+  const bool bias = a.pb || a.nb, keep = a.fq || a.nq;
+  return bias ? keep ? fwd_ring<T, VPT, VEC, true, true>(a, th, s) : fwd_ring<T, VPT, VEC, true, false>(a, th, s)
+              : keep ? fwd_ring<T, VPT, VEC, false, true>(a, th, s) : fwd_ring<T, VPT, VEC, false, false>(a, th, s);
+}
+
+template <typename T, bool VEC>
+void forward_as(const Fwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
   note_launch(1);
-  if (nvec <= 128) {
-    const int blocks = (a.N + 7) / 8;
-    if (nvec <= 32) launch_pdl(fwd_reg_k<T, true, 1>, blocks, 256, 0, s, a);
-    else if (nvec <= 64) launch_pdl(fwd_reg_k<T, true, 2>, blocks, 256, 0, s, a);
-    else launch_pdl(fwd_reg_k<T, true, 4>, blocks, 256, 0, s, a);
-  } else if (nvec <= 2048) {
-    int vpt = 1;
-    while (vpt < 4 && (nvec + vpt - 1) / vpt > 128) vpt *= 2;
-    const int th = ((nvec + vpt - 1) / vpt + 31) / 32 * 32;
-    if (vpt == 1) launch_pdl(fwd_reg_k<T, false, 1>, a.N, th, 0, s, a);
-    else if (vpt == 2) launch_pdl(fwd_reg_k<T, false, 2>, a.N, th, 0, s, a);
-    else launch_pdl(fwd_reg_k<T, false, 4>, a.N, th, 0, s, a);
-  } else {
-    launch_pdl(fwd_any_k<T>, a.N, 512, 0, s, a);
-  }
+  if (nvec <= 512 && fwd_ring_by<T, 1, VEC>(a, (nvec + 31) / 32 * 32, s)) return;
+  if (nvec > 512 && nvec <= 1024 && fwd_ring_by<T, 2, VEC>(a, (nvec + 63) / 64 * 32, s)) return;
+  launch_pdl(fwd_any_k<T, VEC>, a.N, 512, 0, s, a);
+}
+template <typename T>
+void forward(const Fwd& a, cudaStream_t s) {
+  if (a.vec && a.wvec) forward_as<T, true>(a, s);
+  else forward_as<T, false>(a, s);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -315,7 +533,7 @@ __host__ __device__ __forceinline__ void chunk_rows(int k, int N, int gate_rows,
 }
 
 // f of row n, columns c .. c + 7.
-template <typename T>
+template <typename T, bool VEC>
 __device__ __forceinline__ void f8(const Bwd& a, int n, int c, float* x) {
   if (a.fq) {
     const size_t at = (size_t)n * a.D + c;
@@ -328,24 +546,24 @@ __device__ __forceinline__ void f8(const Bwd& a, int n, int c, float* x) {
       for (int i = 0; i < 8; ++i) x[i] = 0.f;
     }
   } else {
-    load8((const T*)a.f + (size_t)n * a.d, c, a.d, a.vec, x);
+    load8<VEC>((const T*)a.f + (size_t)n * a.d, c, a.d, x);
   }
 }
 
 // G of row n, columns c .. (0 past d).
-template <typename T>
+template <typename T, bool VEC>
 __device__ __forceinline__ void grad8(const Bwd& a, int n, int c, float s1, float s2, float* G) {
   const size_t o = (size_t)n * a.d;
 #pragma unroll
   for (int i = 0; i < 8; ++i) G[i] = 0.f;
-  if (a.dho) load8((const T*)a.dho + o, c, a.d, a.vec, G);
+  if (a.dho) load8<VEC>((const T*)a.dho + o, c, a.d, G);
   if (a.pre) {
     const float m = a.stats[2 * (size_t)a.N + n], r = a.stats[3 * (size_t)a.N + n];
     float u[8], x[8], w[8];
-    load8((const T*)a.dn + o, c, a.d, a.vec, u);
-    load8((const T*)a.ho + o, c, a.d, a.vec, x);
+    load8<VEC>((const T*)a.dn + o, c, a.d, u);
+    load8<VEC>((const T*)a.ho + o, c, a.d, x);
     if (a.nw) {
-      load8(a.nw, c, a.d, a.wvec, w);
+      load8<VEC>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] *= w[i];
     }
@@ -355,7 +573,7 @@ __device__ __forceinline__ void grad8(const Bwd& a, int n, int c, float s1, floa
 }
 
 // mean(u) (LayerNorm) and mean(u xh) of every row.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) bwd_sums_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
@@ -366,10 +584,10 @@ __global__ void __launch_bounds__(256) bwd_sums_k(const Bwd a) {
   float s1 = 0.f, s2 = 0.f;
   for (int c = threadIdx.x * 8; c < a.d; c += blockDim.x * 8) {
     float u[8], x[8], w[8];
-    load8((const T*)a.dn + o, c, a.d, a.vec, u);
-    load8((const T*)a.ho + o, c, a.d, a.vec, x);
+    load8<VEC>((const T*)a.dn + o, c, a.d, u);
+    load8<VEC>((const T*)a.ho + o, c, a.d, x);
     if (a.nw) {
-      load8(a.nw, c, a.d, a.wvec, w);
+      load8<VEC>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] *= w[i];
     }
@@ -388,7 +606,7 @@ __global__ void __launch_bounds__(256) bwd_sums_k(const Bwd a) {
 }
 
 // Partial column sums of a chunk: 32 vectors of columns x 8 row lanes a block, the lanes' sums added in order.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
@@ -417,25 +635,25 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
   for (int g0 = r0; g0 < r1; g0 += gr) {
     for (int n = g0 + ty; n < min(g0 + gr, r1) && c < a.d; n += 8) {
       float G[8], w[8], x[8];
-      grad8<T>(a, n, c, a.pre ? a.s12[n] : 0.f, a.pre ? a.s12[(size_t)a.N + n] : 0.f, G);
+      grad8<T, VEC>(a, n, c, a.pre ? a.s12[n] : 0.f, a.pre ? a.s12[(size_t)a.N + n] : 0.f, G);
       if (a.pre) {
         const float m = a.stats[2 * (size_t)a.N + n], r = a.stats[3 * (size_t)a.N + n];
-        load8((const T*)a.dn + (size_t)n * a.d, c, a.d, a.vec, w);
-        load8((const T*)a.ho + (size_t)n * a.d, c, a.d, a.vec, x);
+        load8<VEC>((const T*)a.dn + (size_t)n * a.d, c, a.d, w);
+        load8<VEC>((const T*)a.ho + (size_t)n * a.d, c, a.d, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           acc[0][i] += w[i] * ((x[i] - m) * r);
           acc[1][i] += w[i];
         }
       }
-      f8<T>(a, n, c, x);
+      f8<T, VEC>(a, n, c, x);
       const float pm = a.stats[n], pr = a.stats[(size_t)a.N + n];
       float gt[8], b[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) { gt[i] = 1.f; w[i] = 1.f; b[i] = 0.f; }
-      if (a.gate) load8(a.gate + gate_row(n, a.gate_rows) * a.d, c, a.d, a.wvec, gt);
-      if (a.pw) load8(a.pw, c, a.d, a.wvec, w);
-      if (a.pb) load8(a.pb, c, a.d, a.wvec, b);
+      if (a.gate) load8<VEC>(a.gate + gate_row(n, a.gate_rows) * a.d, c, a.d, gt);
+      if (a.pw) load8<VEC>(a.pw, c, a.d, w);
+      if (a.pb) load8<VEC>(a.pb, c, a.d, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float fh = a.post ? (x[i] - pm) * pr : x[i], q = a.beta * G[i];
@@ -462,25 +680,8 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
   }
 }
 
-// The chunks' partial sums in order: blockIdx.y 0..3 the parameters, 4 + g gate group g.
-__global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
-  pdl_wait();
-  pdl_trigger();
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.d) return;
-  for (int y = blockIdx.y; y < 4 + (a.per_group ? a.chunks / a.per_group : 0); y += gridDim.y) {
-    const int k = min(y, 4);
-    if (!a.out[k]) continue;
-    const int b0 = k < 4 ? 0 : (y - 4) * a.per_group, b1 = k < 4 ? a.chunks : b0 + a.per_group;
-    float s = 0.f;
-    for (int b = b0; b < b1; ++b) s += a.part[((size_t)b * 5 + k) * a.d + c];
-    float* p = a.out[k] + (k < 4 ? 0 : (size_t)(y - 4) * a.d) + c;
-    *p = a.accumulate ? *p + s : s;
-  }
-}
-
 // dh and df of every row.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
@@ -493,21 +694,21 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
   // G, v and fh of columns c ..
   auto vals = [&](int c, float* G, float* v, float* fh) {
     float w[8];
-    grad8<T>(a, n, c, s1, s2, G);
+    grad8<T, VEC>(a, n, c, s1, s2, G);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = a.beta * G[i];
     if (gr) {
-      load8(gr, c, a.d, a.wvec, w);
+      load8<VEC>(gr, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= w[i];
     }
     if (!a.post) return;
     if (a.pw) {
-      load8(a.pw, c, a.d, a.wvec, w);
+      load8<VEC>(a.pw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= w[i];
     }
-    f8<T>(a, n, c, fh);
+    f8<T, VEC>(a, n, c, fh);
 #pragma unroll
     for (int i = 0; i < 8; ++i) fh[i] = (fh[i] - pm) * pr;
   };
@@ -533,42 +734,445 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
       G[i] *= a.alpha;
       if (a.post) v[i] = pr * (v[i] - t1 - fh[i] * t2);
     }
-    if (a.dh) store8((T*)a.dh + o, c, a.d, a.vec, G);
-    store8((T*)a.df + o, c, a.d, a.vec, v);
+    if (a.dh) store8<VEC>((T*)a.dh + o, c, a.d, G);
+    store8<VEC>((T*)a.df + o, c, a.d, v);
   }
 }
 
-constexpr int kChunkRows = 64;
+// ------------------------------------------------------------------------------------------------
+// Backward in one pass over the rows: a block takes a chunk of neighbouring rows through the ring (dn, dh', h', f of a row a
+// stage) and keeps its columns' sums over them in registers. With s = sum G fh and z = sum G over rows of one gate row,
+//   dgate = beta (w_post s + b_post z),  dw_post = beta gate s,  db_post = beta gate z
+// so two sums (four with a LayerNorm's bias) are kept for five gradients. Per row two block-wide sums in turn: those of the
+// pre norm give G, those of the post norm, which needs G, give df.
+// ------------------------------------------------------------------------------------------------
+// The 8 values of f at column c of a row in shared memory (a row of T, or of codes).
+template <typename T>
+__device__ __forceinline__ void f_pairs(const Bwd& a, const uint8_t* row, uint32_t e, int c, uint64_t* f) {
+  if (a.fq) {
+    const uint2 w = *reinterpret_cast<const uint2*>(row + c);
+    float x[8];
+    if (a.fmt == ZL_ACT8_E4M3) decode8<ZL_ACT8_E4M3>(w, e, x);
+    else decode8<ZL_ACT8_INT8>(w, e, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = f2(x[2 * i], x[2 * i + 1]);
+  } else {
+    Raw8<T> r;
+    r.get(row + c * sizeof(T));
+    r.pairs(f);
+  }
+}
 
-void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
-  const int gr = p.gate_rows && p.gate_rows < p.N ? p.gate_rows : std::max(p.N, 1);
-  if (gr > kChunkRows) {
-    per_group = (gr + kChunkRows - 1) / kChunkRows;
+template <typename T, int VPT, bool VEC, bool BIAS>
+__global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t full[kStages];
+  __shared__ __align__(16) float sh[2][2][16];
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  const int t = threadIdx.x, nt = blockDim.x;
+  const int gate_rows = a.gate_rows ? a.gate_rows : a.N;
+  int r0, r1;
+  chunk_rows(blockIdx.x, a.N, gate_rows, a.rows, a.per_group, r0, r1);
+  const int rows = r1 - r0;
+  const uint32_t bytes = (uint32_t)a.d * sizeof(T);
+  if (t == 0) {
+    for (int i = 0; i < g.stages; ++i) tc::mbar_init(&full[i], 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = t; i < 64; i += nt) (&sh[0][0][0])[i] = 0.f;
+  for (int k = 0; k < 4 * g.stages; ++k)   // columns past d, and tensors that are not given, read 0
+    for (int c = ((k & 3) == 0 && a.dn) || ((k & 3) == 1 && a.dho) || ((k & 3) == 2 && a.pre) || ((k & 3) == 3 && !a.fq) ? a.d + t : t;
+         c < ((k & 3) == 3 && a.fq ? 0 : a.D); c += nt)
+      reinterpret_cast<T*>(ring + (k >> 2) * g.stage + (k & 3) * g.pitch)[c] = from_f<T>(0.f);
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  auto fill = [&](int k) {
+    uint8_t* p = ring + (k % g.stages) * g.stage;
+    const int n = r0 + k;
+    const size_t o = (size_t)n * a.d;
+    if (VEC) {
+      uint64_t* bar = &full[k % g.stages];
+      tc::mbar_expect_tx(bar, bytes * ((a.pre ? 2 : 0) + (a.dho ? 1 : 0) + (a.fq ? 0 : 1)) + (a.fq ? (uint32_t)a.D : 0u));
+      if (a.pre) {
+        bulk_row(p, (const T*)a.dn + o, bytes, bar);
+        bulk_row(p + 2 * g.pitch, (const T*)a.ho + o, bytes, bar);
+      }
+      if (a.dho) bulk_row(p + g.pitch, (const T*)a.dho + o, bytes, bar);
+      if (a.fq) bulk_row(p + 3 * g.pitch, a.fq + (size_t)n * a.D, (uint32_t)a.D, bar);
+      else bulk_row(p + 3 * g.pitch, (const T*)a.f + o, bytes, bar);
+    } else {
+      for (int c = t; c < a.d; c += nt) {
+        if (a.pre) {
+          reinterpret_cast<T*>(p)[c] = ((const T*)a.dn)[o + c];
+          reinterpret_cast<T*>(p + 2 * g.pitch)[c] = ((const T*)a.ho)[o + c];
+        }
+        if (a.dho) reinterpret_cast<T*>(p + g.pitch)[c] = ((const T*)a.dho)[o + c];
+        if (!a.fq) reinterpret_cast<T*>(p + 3 * g.pitch)[c] = ((const T*)a.f)[o + c];
+      }
+      if (a.fq)
+        for (int c = t; c < a.D / 16; c += nt)
+          reinterpret_cast<uint4*>(p + 3 * g.pitch)[c] = reinterpret_cast<const uint4*>(a.fq + (size_t)n * a.D)[c];
+    }
+  };
+  if (VEC && t == 0)
+    for (int k = 0; k < min(rows, g.stages); ++k) fill(k);
+  uint64_t w[VPT][4], pw[VPT][4], gt[VPT][4];            // w_pre; w_post; beta gate
+  uint64_t s[VPT][4], z[BIAS ? VPT : 1][4];              // sums G fh, G of the gate row at hand
+  uint64_t dw[VPT][4], db[BIAS ? VPT : 1][4];            // sums dn xh, dn
+  float unused = 0.f;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const int c = (t + j * nt) * 8;
+    row8<VEC>(a.nw, c, a.d, 1.f, w[j]);
+    row8<VEC>(a.pw, c, a.d, 1.f, pw[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[j][i] = dw[j][i] = 0;
+      if (BIAS) z[j][i] = db[j][i] = 0;
+    }
+  }
+  // the sums over a gate row's rows [.., n] go to where their gradients are formed: dgate itself where the chunk knows all of
+  // its rows, else the chunk's part; and the post norm's sums, of gate rows one after another, to the chunk's part
+  float* const part = a.part + (size_t)blockIdx.x * 5 * a.d;
+  bool fresh = true;
+  auto flush = [&](int n) {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (t + j * nt) * 8;
+      if (c >= a.d) continue;
+      float sv[8], zv[8], x[8], y[8];
+      unpair(s[j], sv);
+      if (a.out[4]) {
+        uint64_t b[4];
+        if (BIAS) row8<VEC>(a.pb, c, a.d, 0.f, b);
+        uint64_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = mul2(pw[j][i], s[j][i]);
+          if (BIAS) v[i] = fma2(b[i], z[j][i], v[i]);
+          v[i] = mul2(v[i], f2(a.beta, a.beta));
+        }
+        unpair(v, x);
+        float* q = a.per_group ? part + 4 * (size_t)a.d : a.out[4] + gate_row(n, a.gate_rows) * a.d;
+        if (!a.per_group && a.accumulate) {
+          load8<VEC>((const float*)q, c, a.d, y);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] += y[i];
+        }
+        store8<VEC>(q, c, a.d, x);
+      }
+      float gv[8];
+      unpair(gt[j], gv);
+      if (BIAS) unpair(z[j], zv);
+#pragma unroll
+      for (int k = 0; k < (BIAS ? 2 : 1); ++k) {
+        if (!a.out[2 + k]) continue;
+        float* q = part + (2 + k) * (size_t)a.d;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = gv[i] * (k ? zv[i] : sv[i]);
+        if (!fresh) {
+          load8<VEC>((const float*)q, c, a.d, y);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] += y[i];
+        }
+        store8<VEC>(q, c, a.d, x);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[j][i] = 0;
+        if (BIAS) z[j][i] = 0;
+      }
+    }
+    fresh = false;
+  };
+  Reducer red{sh, 0};
+  const float inv_d = 1.f / a.d;
+  const uint64_t alpha = f2(a.alpha, a.alpha);
+  // statistics and group bytes of the next row, read a row ahead
+  float st4[4];
+  uint32_t eb[VPT];
+  auto ahead = [&](int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st4[i] = a.stats[(size_t)i * a.N + n];
+    if (a.fq) {
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        eb[j] = c < a.D ? a.fe[((size_t)n * a.D + c) >> 5] : 0u;
+      }
+    }
+  };
+  if (rows > 0) ahead(r0);
+  bool new_gate = true;
+  int k = 0;
+  for (; k < rows; ++k) {
+    const int n = r0 + k, st = k % g.stages;
+    const size_t o = (size_t)n * a.d;
+    const uint8_t* p = ring + st * g.stage;
+    if (new_gate) {
+      const float* gr = a.gate ? a.gate + gate_row(n, a.gate_rows) * a.d : nullptr;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        row8<VEC>(gr, (t + j * nt) * 8, a.d, 1.f, gt[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gt[j][i] = mul2(gt[j][i], f2(a.beta, a.beta));
+      }
+      new_gate = false;
+    }
+    const float pm = st4[0], pr = st4[1], m = st4[2], r = st4[3];
+    uint32_t e[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) e[j] = eb[j];
+    if (k + 1 < rows) ahead(n + 1);
+    bool ok = true;
+    if (VEC) {
+      ok = tc::mbar_wait(&full[st], (uint32_t)(k / g.stages) & 1u, abort_flag, nullptr);
+    } else {
+      __syncthreads();
+      fill(k);
+      __syncthreads();
+    }
+    // u and xh of the pre norm, then G; v and fh of the post norm
+    uint64_t u[VPT][4], x[VPT][4];
+    float s1 = 0.f, s2 = 0.f;
+    if (a.pre) {
+      const uint64_t mm = f2(m, m), rr = f2(r, r);
+      uint64_t t1 = 0, t2 = 0;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        Raw8<T> rn, rx;
+        rn.zero();
+        rx.zero();
+        if (c < a.D) {
+          rn.get(p + c * sizeof(T));
+          rx.get(p + 2 * g.pitch + c * sizeof(T));
+        }
+        rn.pairs(u[j]);
+        rx.pairs(x[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (a.pre == ZL_NORM_LAYER) x[j][i] = sub2(x[j][i], mm);
+          x[j][i] = mul2(x[j][i], rr);
+          dw[j][i] = fma2(u[j][i], x[j][i], dw[j][i]);
+          if (BIAS) db[j][i] = add2(db[j][i], u[j][i]);
+          u[j][i] = mul2(u[j][i], w[j][i]);
+          t2 = fma2(u[j][i], x[j][i], t2);
+          if (a.pre == ZL_NORM_LAYER) t1 = add2(t1, u[j][i]);
+        }
+      }
+      s1 = fold(t1);
+      s2 = fold(t2);
+      ok = a.pre == ZL_NORM_LAYER ? red.sum(s2, s1, true, ok) : red.sum(s2, unused, false, ok);
+      s1 *= inv_d;
+      s2 *= inv_d;
+    }
+    float q1 = 0.f, q2 = 0.f;
+    {
+      const uint64_t rr = f2(r, r), n1 = f2(-s1, -s1), n2 = f2(-s2, -s2), pmm = f2(pm, pm), prr = f2(pr, pr);
+      uint64_t t1 = 0, t2 = 0;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        uint64_t G[4];
+        Raw8<T> rd;
+        rd.zero();
+        if (c < a.D) rd.get(p + g.pitch + c * sizeof(T));
+        rd.pairs(G);
+        if (a.pre) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) G[i] = fma2(rr, fma2(x[j][i], n2, add2(u[j][i], n1)), G[i]);
+          cut(G, c, a.d);
+        }
+        if (c < a.D) f_pairs<T>(a, p + 3 * g.pitch, e[j], c, x[j]);
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[j][i] = 0;
+        uint64_t dh[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (a.post == ZL_NORM_LAYER) x[j][i] = sub2(x[j][i], pmm);
+          if (a.post) x[j][i] = mul2(x[j][i], prr);
+          s[j][i] = fma2(G[i], x[j][i], s[j][i]);
+          if (BIAS) z[j][i] = add2(z[j][i], G[i]);
+          dh[i] = mul2(G[i], alpha);
+          u[j][i] = mul2(mul2(G[i], gt[j][i]), pw[j][i]);
+          t2 = fma2(u[j][i], x[j][i], t2);
+          if (a.post == ZL_NORM_LAYER) t1 = add2(t1, u[j][i]);
+        }
+        if (a.dh) {
+          float y[8];
+          unpair(dh, y);
+          store8<VEC>((T*)a.dh + o, c, a.d, y);
+        }
+      }
+      q1 = fold(t1);
+      q2 = fold(t2);
+    }
+    if (a.post == ZL_NORM_LAYER) ok = red.sum(q2, q1, true, ok);
+    else if (a.post) ok = red.sum(q2, unused, false, ok);
+    else ok = __syncthreads_and(ok);
+    if (!ok) break;
+    if (VEC && t == 0 && k + g.stages < rows) fill(k + g.stages);   // everyone has read the row
+    {
+      const uint64_t prr = f2(pr, pr), n1 = f2(-q1 * inv_d, -q1 * inv_d), n2 = f2(-q2 * inv_d, -q2 * inv_d);
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        if (a.post) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[j][i] = mul2(prr, fma2(x[j][i], n2, add2(u[j][i], n1)));
+        }
+        float y[8];
+        unpair(u[j], y);
+        store8<VEC>((T*)a.df + o, c, a.d, y);
+      }
+    }
+    if (k + 1 == rows || (!a.per_group && (n + 1) % gate_rows == 0)) {
+      flush(n);
+      new_gate = true;
+    }
+  }
+  if (k == rows) {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (t + j * nt) * 8;
+      if (c >= a.d) continue;
+      float x[8];
+      unpair(dw[j], x);
+      if (a.out[0]) store8<VEC>(part, c, a.d, x);
+      if (BIAS && a.out[1]) {
+        unpair(db[j], x);
+        store8<VEC>(part + a.d, c, a.d, x);
+      }
+      if (rows == 0) {   // a chunk past its gate group's end
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        for (int i = 2; i < 5; ++i)
+          if (a.out[i]) store8<VEC>(part + i * (size_t)a.d, c, a.d, x);
+      }
+    }
+  }
+  if (VEC && k < rows && t == 0) {   // a wait gave up: let the copies in flight land before the block ends
+    for (int i = k; i < min(rows, k + g.stages); ++i) {
+      const unsigned long long t0 = tc::gtimer();
+      while (!tc::mbar_test(&full[i % g.stages], (uint32_t)(i / g.stages) & 1u) && tc::gtimer() - t0 < 100000000ull) {
+      }
+    }
+  }
+}
+
+// The chunks' partial sums: a block takes 32 columns of one gradient (blockIdx.y 0..3 the parameters, 4 + g gate row g), 8
+// lanes of rows each adding every 8th chunk, the lanes' sums then in order.
+__global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float sh[8][32];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+  for (int y = blockIdx.y; y < 4 + (a.per_group ? a.chunks / a.per_group : 0); y += gridDim.y) {
+    const int k = min(y, 4);
+    if (!a.out[k]) continue;
+    const int b0 = k < 4 ? 0 : (y - 4) * a.per_group, b1 = k < 4 ? a.chunks : b0 + a.per_group;
+    float s = 0.f;
+    if (c < a.d) {
+#pragma unroll 8
+      for (int b = b0 + ty; b < b1; b += 8) s += a.part[((size_t)b * 5 + k) * a.d + c];
+    }
+    __syncthreads();
+    sh[ty][tx] = s;
+    __syncthreads();
+    if (ty == 0 && c < a.d) {
+#pragma unroll
+      for (int i = 1; i < 8; ++i) s += sh[i][tx];
+      float* p = a.out[k] + (k < 4 ? 0 : (size_t)(y - 4) * a.d) + c;
+      *p = a.accumulate ? *p + s : s;
+    }
+  }
+}
+
+// Chunks of rows for the partial sums, `rows` long where gate groups are longer, else of whole groups.
+void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, int& chunks) {
+  const int gr = gate_rows && gate_rows < N ? gate_rows : std::max(N, 1);
+  if (gr > target) {
+    per_group = (gr + target - 1) / target;
     rows = (gr + per_group - 1) / per_group;
-    chunks = (p.N + gr - 1) / gr * per_group;
+    chunks = (N + gr - 1) / gr * per_group;
   } else {
     per_group = 0;
-    rows = kChunkRows / gr * gr;
-    chunks = (p.N + rows - 1) / rows;
+    rows = target / gr * gr;
+    chunks = (N + rows - 1) / rows;
   }
 }
+constexpr int kAnyRows = 64;      // rows of a chunk of bwd_cols_k
+constexpr int kRingCols = 8192;   // the widest row of bwd_ring_k
+// Rows of a chunk of bwd_ring_k: enough chunks for the blocks that fit on 152 SMs, but not so short that their partial sums
+// (written once and read once, 8 bytes a column and sum) weigh as much as the rows.
+int ring_rows(int N, int d) {
+  const int th = (pitch(d) / 8 + 31) / 32 * 32, per_sm = std::max(1, std::min(8, 512 / th));
+  return std::max(4, (N + 152 * per_sm - 1) / (152 * per_sm));
+}
+void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
+  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d) : kAnyRows, rows, per_group, chunks);
+}
 
-template <typename T>
-void backward(const Bwd& a, cudaStream_t s) {
+template <typename T, int VPT, bool VEC, bool BIAS>
+bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
+  static const Occupancy occ(bwd_ring_k<T, VPT, VEC, BIAS>);
+  if (!occ.ok) return false;
+  Ring g = {};
+  g.pitch = (uint32_t)a.D * sizeof(T);
+  g.stage = 3 * g.pitch + (a.fq ? (uint32_t)a.D : g.pitch);
+  const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), (a.chunks + sm_count() - 1) / sm_count()}));
+  const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, (size_t)occ.fixed) - occ.fixed;
+  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : 1;
+  if ((size_t)g.stages * g.stage + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
+  const size_t smem = (size_t)g.stages * g.stage;
+  if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
+  return launch_pdl(bwd_ring_k<T, VPT, VEC, BIAS>, a.chunks, th, smem, s, a, g) == cudaSuccess;
+}
+
+template <typename T, bool VEC>
+bool backward_as(const Bwd& a, cudaStream_t s) {
+  const int nvec = a.D / 8;
+  bool sums = false, parts = false;
+  for (int k = 0; k < 5; ++k) {
+    sums |= a.out[k] != nullptr;
+    parts |= a.out[k] && (k < 4 || a.per_group);
+  }
+  const int ys = 4 + (a.per_group ? a.chunks / a.per_group : 0);
+  const dim3 join((a.d + 31) / 32, std::min(ys, 65535));
+  if (a.d <= kRingCols) {
+    const bool bias = a.out[1] || a.out[3] || a.pb;
+    note_launch(parts ? 2 : 1);
+    if (nvec <= 512) {
+      const int th = (nvec + 31) / 32 * 32;
+      if (!(bias ? bwd_ring<T, 1, VEC, true>(a, th, s) : bwd_ring<T, 1, VEC, false>(a, th, s))) return false;
+    } else {
+      const int th = (nvec + 63) / 64 * 32;
+      if (!(bias ? bwd_ring<T, 2, VEC, true>(a, th, s) : bwd_ring<T, 2, VEC, false>(a, th, s))) return false;
+    }
+    if (parts) launch_pdl(bwd_join_k, join, 256, 0, s, a);
+    return true;
+  }
   if (a.pre) {
     note_launch(1);
-    launch_pdl(bwd_sums_k<T>, a.N, 256, 0, s, a);
+    launch_pdl(bwd_sums_k<T, VEC>, a.N, 256, 0, s, a);
   }
-  bool sums = false;
-  for (float* o : a.out) sums |= o != nullptr;
   if (sums) {   // before dh, which may overwrite dh_out
     note_launch(2);
-    launch_pdl(bwd_cols_k<T>, dim3(a.chunks, (a.d + 255) / 256), 256, 0, s, a);
-    const int ys = 4 + (a.per_group ? a.chunks / a.per_group : 0);
-    launch_pdl(bwd_join_k, dim3((a.d + 255) / 256, std::min(ys, 65535)), 256, 0, s, a);
+    launch_pdl(bwd_cols_k<T, VEC>, dim3(a.chunks, (a.d + 255) / 256), 256, 0, s, a);
+    launch_pdl(bwd_join_k, join, 256, 0, s, a);
   }
   note_launch(1);
-  launch_pdl(bwd_rows_k<T>, a.N, 256, 0, s, a);
+  launch_pdl(bwd_rows_k<T, VEC>, a.N, 256, 0, s, a);
+  return true;
+}
+template <typename T>
+bool backward(const Bwd& a, cudaStream_t s) {
+  return a.vec && a.wvec ? backward_as<T, true>(a, s) : backward_as<T, false>(a, s);
 }
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
@@ -670,10 +1274,10 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     plan_chunks(*p, a.rows, a.per_group, a.chunks);
     a.vec = true;
     for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df}) a.vec &= !t || rows_aligned(t, d, p->dtype);
-    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && (!gate || rows_aligned(gate, d, ZL_DTYPE_F32));
-    if (p->dtype == ZL_DTYPE_BF16) backward<bf16>(a, s);
-    else backward<float>(a, s);
-    return launched("zl_op_block_norm_bwd");
+    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(dgate) && (!gate || rows_aligned(gate, d, ZL_DTYPE_F32));
+    const bool done = p->dtype == ZL_DTYPE_BF16 ? backward<bf16>(a, s) : backward<float>(a, s);
+    const zl_status st = launched("zl_op_block_norm_bwd");
+    return done || st != ZL_OK ? st : act8::fail(ZL_ERR_CUDA, "zl_op_block_norm_bwd: the kernel cannot be launched on this device");
   });
 }
 
