@@ -23,7 +23,7 @@ struct Items {
 // ------------------------------------------------------------------------------------------------
 // Rows to 8 bits and back. HBM-bound: 3.03 bytes a value in bf16, 5.03 in fp32.
 // ------------------------------------------------------------------------------------------------
-template <typename T, int FMT, bool VEC>
+template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it,
                                                     uint2* __restrict__ q, uint8_t* __restrict__ e) {
   pdl_wait();
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, siz
   float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (in) {
     const uint32_t r = it.row.quot(i);
-    load8<VEC>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
+    load8<MODE>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
   }
   uint2 w;
   const uint32_t b = encode_quarter<FMT>(f, w);
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, siz
   }
 }
 
-template <typename T, int FMT, bool VEC>
+template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e, Items it,
                                                    T* __restrict__ x, size_t ldx, int d) {
   pdl_wait();
@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, 
   const uint32_t r = it.row.quot(i);
   float f[8];
   decode8<FMT>(q[i], e[i >> 2], f);
-  store8<VEC>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
+  store8<MODE>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -70,7 +70,7 @@ __device__ __forceinline__ float sigm(float x) {
 constexpr float kGeluK = 0.7978845608028654f, kGeluC = 0.044715f;
 
 // x [N, f] (GELU) or [N, 2 f] (SwiGLU: gate, up); codes of the rows of f values: [N, D] or [N, 2 D], D = pitch(f).
-template <typename T, int FMT, int ACT, bool VEC>
+template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, Items it, T* __restrict__ y,
                                                   uint2* __restrict__ q, uint8_t* __restrict__ e) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
@@ -81,9 +81,9 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
   const uint32_t r = in ? it.row.quot(i) : 0, c8 = i - r * it.row.d;
   const int c = (int)c8 * 8;
   const T* xr = x + (size_t)r * W * f;
-  const Raw8<T> rg = load_raw<VEC>(xr, c, in ? f : 0);
+  const Raw8<T> rg = load_raw<MODE>(xr, c, in ? f : 0);
   Raw8<T> ru;
-  if (W == 2) ru = load_raw<VEC>(xr + f, c, in ? f : 0);
+  if (W == 2) ru = load_raw<MODE>(xr + f, c, in ? f : 0);
   float g[8], u[8];
   floats(rg, g);
   if (W == 2) floats(ru, u);
@@ -108,10 +108,10 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
     if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
     else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
   }
-  store8<VEC>(y + (size_t)r * f, c, f, g);
+  store8<MODE>(y + (size_t)r * f, c, f, g);
 }
 
-template <typename T, int FMT, int ACT, bool VEC>
+template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
                                                       const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
   const size_t at = (size_t)r * W * it.row.d + c8;
   float g[8], u[8], t[8], a[8];
   const size_t at2 = W == 2 ? at + it.row.d : at;
-  const Raw8<T> rt = load_raw<VEC>(dy + (size_t)r * f, c, f);
+  const Raw8<T> rt = load_raw<MODE>(dy + (size_t)r * f, c, f);
   const uint2 qg = q[at], qu = q[at2];
   const uint32_t eg = e[at >> 2], eu = e[at2 >> 2];
   floats(rt, t);
@@ -145,9 +145,9 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
     }
   }
   T* dr = dx + (size_t)r * W * f;
-  store8<VEC>(dr, c, f, g);
-  if (W == 2) store8<VEC>(dr + f, c, f, u);
-  if (y) store8<VEC>(y + (size_t)r * f, c, f, a);
+  store8<MODE>(dr, c, f, g);
+  if (W == 2) store8<MODE>(dr + f, c, f, u);
+  if (y) store8<MODE>(y + (size_t)r * f, c, f, a);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(kThreads) dw_prep_k(const DwPrep p) {
   const uint32_t r = p.arow.quot(i);
   const int c = (int)(i - r * p.arow.d) * 8;
   if ((int)r < p.K) {
-    if (p.vec) load8<true>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
-    else load8<false>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
+    if (p.vec) load8<kTail>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
+    else load8<kSingle>((const T*)p.A + (size_t)r * p.M, c, p.M, f);
   }
   else {
 #pragma unroll
@@ -271,24 +271,24 @@ Items items(int N, int d) { return Items{(uint32_t)((size_t)N * (pitch(d) / 8)),
 unsigned blocks_of(const Items& it) { return (it.n + kThreads - 1) / kThreads; }
 
 template <typename T, int FMT>
-void store_t(const void* x, size_t ldx, int N, int d, bool vec, uint8_t* q, uint8_t* e, cudaStream_t s) {
+void store_t(const void* x, size_t ldx, int N, int d, int mode, uint8_t* q, uint8_t* e, cudaStream_t s) {
   const Items it = items(N, d);
-  launch_pdl(vec ? store_k<T, FMT, true> : store_k<T, FMT, false>, blocks_of(it), kThreads, 0, s, (const T*)x, ldx, d, it, (uint2*)q, e);
+  launch_pdl(mode == kWhole ? store_k<T, FMT, kWhole> : mode == kTail ? store_k<T, FMT, kTail> : store_k<T, FMT, kSingle>, blocks_of(it), kThreads, 0, s, (const T*)x, ldx, d, it, (uint2*)q, e);
 }
 template <typename T, int FMT>
-void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, bool vec, cudaStream_t s) {
+void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, int mode, cudaStream_t s) {
   const Items it = items(N, d);
-  launch_pdl(vec ? load_k<T, FMT, true> : load_k<T, FMT, false>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, it, (T*)x, ldx, d);
+  launch_pdl(mode == kWhole ? load_k<T, FMT, kWhole> : mode == kTail ? load_k<T, FMT, kTail> : load_k<T, FMT, kSingle>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, it, (T*)x, ldx, d);
 }
 template <typename T, int FMT, int ACT>
-void act_t(const void* x, int N, int f, bool vec, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
+void act_t(const void* x, int N, int f, int mode, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
   const Items it = items(N, f);
-  launch_pdl(vec ? act_k<T, FMT, ACT, true> : act_k<T, FMT, ACT, false>, blocks_of(it), kThreads, 0, s, (const T*)x, f, it, (T*)y, (uint2*)q, e);
+  launch_pdl(mode == kWhole ? act_k<T, FMT, ACT, kWhole> : mode == kTail ? act_k<T, FMT, ACT, kTail> : act_k<T, FMT, ACT, kSingle>, blocks_of(it), kThreads, 0, s, (const T*)x, f, it, (T*)y, (uint2*)q, e);
 }
 template <typename T, int FMT, int ACT>
-void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, bool vec, void* dx, void* y, cudaStream_t s) {
+void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, int mode, void* dx, void* y, cudaStream_t s) {
   const Items it = items(N, f);
-  launch_pdl(vec ? act_bwd_k<T, FMT, ACT, true> : act_bwd_k<T, FMT, ACT, false>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, it, (T*)dx,
+  launch_pdl(mode == kWhole ? act_bwd_k<T, FMT, ACT, kWhole> : mode == kTail ? act_bwd_k<T, FMT, ACT, kTail> : act_bwd_k<T, FMT, ACT, kSingle>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, it, (T*)dx,
              (T*)y);
 }
 
@@ -305,14 +305,14 @@ void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f,
   } while (0)
 
 template <typename T, int FMT>
-void act_by(int act, const void* x, int N, int f, bool vec, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  if (act == ZL_ACT_SWIGLU) act_t<T, FMT, ZL_ACT_SWIGLU>(x, N, f, vec, y, q, e, s);
-  else act_t<T, FMT, ZL_ACT_GELU>(x, N, f, vec, y, q, e, s);
+void act_by(int act, const void* x, int N, int f, int mode, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
+  if (act == ZL_ACT_SWIGLU) act_t<T, FMT, ZL_ACT_SWIGLU>(x, N, f, mode, y, q, e, s);
+  else act_t<T, FMT, ZL_ACT_GELU>(x, N, f, mode, y, q, e, s);
 }
 template <typename T, int FMT>
-void act_bwd_by(int act, const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, bool vec, void* dx, void* y, cudaStream_t s) {
-  if (act == ZL_ACT_SWIGLU) act_bwd_t<T, FMT, ZL_ACT_SWIGLU>(q, e, dy, N, f, vec, dx, y, s);
-  else act_bwd_t<T, FMT, ZL_ACT_GELU>(q, e, dy, N, f, vec, dx, y, s);
+void act_bwd_by(int act, const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, int mode, void* dx, void* y, cudaStream_t s) {
+  if (act == ZL_ACT_SWIGLU) act_bwd_t<T, FMT, ZL_ACT_SWIGLU>(q, e, dy, N, f, mode, dx, y, s);
+  else act_bwd_t<T, FMT, ZL_ACT_GELU>(q, e, dy, N, f, mode, dx, y, s);
 }
 
 template <typename T, int FMT>
@@ -325,7 +325,7 @@ void prep_t(const DwPrep& p, unsigned blocks, cudaStream_t s) {
 
 using namespace zl;
 using zl::act8::entry;
-using zl::act8::rows_aligned;
+using zl::act8::row_mode;
 
 extern "C" {
 
@@ -335,7 +335,7 @@ zl_status zl_op_act8_store(int dtype, int fmt, const void* x, int N, int d, int 
     if (N == 0) return ZL_OK;
     if (!x || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     note_launch(1);
-    ZL_BY_TYPE(store_t, dtype, fmt, x, (size_t)ldx, N, d, rows_aligned(x, (size_t)ldx, dtype), q, e, (cudaStream_t)stream);
+    ZL_BY_TYPE(store_t, dtype, fmt, x, (size_t)ldx, N, d, row_mode(x, (size_t)d, (size_t)ldx, dtype), q, e, (cudaStream_t)stream);
     return launched("zl_op_act8_store");
   });
 }
@@ -346,7 +346,7 @@ zl_status zl_op_act8_load(int dtype, int fmt, const uint8_t* q, const uint8_t* e
     if (N == 0) return ZL_OK;
     if (!x || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     note_launch(1);
-    ZL_BY_TYPE(load_t, dtype, fmt, q, e, N, d, x, (size_t)ldx, rows_aligned(x, (size_t)ldx, dtype), (cudaStream_t)stream);
+    ZL_BY_TYPE(load_t, dtype, fmt, q, e, N, d, x, (size_t)ldx, row_mode(x, (size_t)d, (size_t)ldx, dtype), (cudaStream_t)stream);
     return launched("zl_op_act8_load");
   });
 }
@@ -356,9 +356,9 @@ zl_status zl_op_act8_act(int dtype, int act, int fmt, const void* x, int N, int 
     if ((act != ZL_ACT_SWIGLU && act != ZL_ACT_GELU) || !act_shape(dtype, fmt, N, f)) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
     if (!x || !y || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
-    const bool vec = rows_aligned(x, (size_t)f, dtype) && rows_aligned(y, (size_t)f, dtype);
+    const int mode = std::min(row_mode(x, f, f, dtype), row_mode(y, f, f, dtype));
     note_launch(1);
-    ZL_BY_TYPE(act_by, dtype, fmt, act, x, N, f, vec, y, q, e, (cudaStream_t)stream);
+    ZL_BY_TYPE(act_by, dtype, fmt, act, x, N, f, mode, y, q, e, (cudaStream_t)stream);
     return launched("zl_op_act8_act");
   });
 }
@@ -369,10 +369,9 @@ zl_status zl_op_act8_act_bwd(int dtype, int act, int fmt, const uint8_t* q, cons
     if ((act != ZL_ACT_SWIGLU && act != ZL_ACT_GELU) || !act_shape(dtype, fmt, N, f)) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
     if (!dy || !dx || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
-    const bool vec = rows_aligned(dy, (size_t)f, dtype) && rows_aligned(dx, (size_t)f, dtype) &&
-                     (!y || rows_aligned(y, (size_t)f, dtype));
+    const int mode = std::min({row_mode(dy, f, f, dtype), row_mode(dx, f, f, dtype), y ? row_mode(y, f, f, dtype) : kWhole});
     note_launch(1);
-    ZL_BY_TYPE(act_bwd_by, dtype, fmt, act, q, e, dy, N, f, vec, dx, y, (cudaStream_t)stream);
+    ZL_BY_TYPE(act_bwd_by, dtype, fmt, act, q, e, dy, N, f, mode, dx, y, (cudaStream_t)stream);
     return launched("zl_op_act8_act_bwd");
   });
 }
@@ -407,7 +406,7 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
     r.nb = (uint32_t)((size_t)K * (p.Np / 8));
     r.blocks_b = (r.nb + kThreads - 1) / kThreads;
     r.A = A; r.Aw = (bf16*)(w + p.b); r.arow = FastDiv((uint32_t)p.Mp / 8); r.M = M; r.K = K;
-    r.vec = rows_aligned(A, (size_t)M, dtype);
+    r.vec = row_mode(A, M, M, dtype) != kSingle;
     r.na = p.copy_a ? (uint32_t)((size_t)p.Kp * (p.Mp / 8)) : 0;
     note_launch(1);
     ZL_BY_TYPE(prep_t, dtype, fmt, r, r.blocks_b + (r.na + kThreads - 1) / kThreads, s);

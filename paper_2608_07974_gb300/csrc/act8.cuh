@@ -105,22 +105,22 @@ __device__ __forceinline__ uint32_t encode4(const float* x, float inv, bool odd)
   return w;
 }
 
-// The four values of four codes, given their group's 2^E. Integer codes: code + 128 as the low mantissa byte of 2^23, less
-// 2^23 + 128.
+// The four numbers that four codes are (not yet times 2^E). Integer codes: code + 128 as the low mantissa byte of 2^23,
+// less 2^23 + 128.
 template <int FMT>
-__device__ __forceinline__ void decode4(uint32_t w, float scale, float* x) {
+__device__ __forceinline__ void codes4(uint32_t w, float* x) {
   if (FMT == ZL_ACT8_E4M3) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * i)), __NV_E4M3);
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      x[2 * i] = f.x * scale;
-      x[2 * i + 1] = f.y * scale;
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
     }
   } else {
     const uint32_t v = w ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(v, 0x4B000000u, 0x7540 + i)) - 8388736.f) * scale;
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7540 + i)) - 8388736.f;
     if ((v - 0x01010101u) & ~v & 0x80808080u) {   // a zero byte: a code of -128
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -129,9 +129,10 @@ __device__ __forceinline__ void decode4(uint32_t w, float scale, float* x) {
   }
 }
 
-// 8 values of a row at column c of d. VEC: rows start on 16 bytes, and all but a row's last few values are read 16 bytes at
-// a time; else one value at a time. Columns from d on read 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread
+// 8 values of a row at column c of d. MODE kWhole: rows start on 16 bytes and d is a multiple of 8; kTail: rows start on 16
+// bytes, and all but a row's last few values are read 16 bytes at a time; kSingle: one value at a time. Columns from d on read 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread
 // are all under way before the first of them is waited for.
+enum { kSingle = 0, kTail = 1, kWhole = 2 };
 template <typename T>
 struct Raw8;
 template <>
@@ -169,10 +170,13 @@ __device__ __forceinline__ void unpair(const uint64_t* p, float* f) {
     f[2 * i + 1] = v.y;
   }
 }
-template <bool VEC, typename T>
+template <int MODE, typename T>
 __device__ __forceinline__ Raw8<T> load_raw(const T* p, int c, int d) {
   Raw8<T> r;
-  if (VEC && c + 8 <= d) {
+  if (MODE == kWhole) {
+    if (c < d) r.get(p + c);
+    else r.zero();
+  } else if (MODE == kTail && c + 8 <= d) {
     r.get(p + c);
   } else {
     r.zero();
@@ -188,16 +192,17 @@ __device__ __forceinline__ void floats(const Raw8<T>& r, float* f) {
   r.pairs(p);
   unpair(p, f);
 }
-template <bool VEC, typename T>
+template <int MODE, typename T>
 __device__ __forceinline__ void load8(const T* p, int c, int d, float* f) {
-  floats(load_raw<VEC>(p, c, d), f);
+  floats(load_raw<MODE>(p, c, d), f);
 }
-template <bool VEC, typename T>
+template <int MODE, typename T>
 __device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
-  if (VEC && c + 8 <= d) {
+  if (MODE == kWhole ? c < d : MODE == kTail && c + 8 <= d) {
     Vec8<T>::store(p + c, f);
     return;
   }
+  if (MODE == kWhole) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (c + i < d) p[c + i] = from_f<T>(f[i]);
@@ -220,8 +225,10 @@ __device__ __forceinline__ uint32_t encode_quarter(const float* x, uint2& q) {
 template <int FMT>
 __device__ __forceinline__ void decode8(uint2 q, uint32_t e, float* x) {
   const float s = group_scale(e);
-  decode4<FMT>(q.x, s, x);
-  decode4<FMT>(q.y, s, x + 4);
+  codes4<FMT>(q.x, x);
+  codes4<FMT>(q.y, x + 4);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] *= s;
 }
 
 // Runs the body of a C entry point: no exception leaves it.
@@ -242,9 +249,10 @@ inline zl_status launched(const char* what) {
   return e == cudaSuccess ? ZL_OK : fail(ZL_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
 }
 
-// Whether rows from p, ld values apart, start on 16 bytes (VEC).
-inline bool rows_aligned(const void* p, size_t ld, int dt) {
-  return ((uintptr_t)p & 15u) == 0 && ld * (dt == ZL_DTYPE_BF16 ? 2 : 4) % 16 == 0;
+// The mode of rows of d values from p, ld apart.
+inline int row_mode(const void* p, size_t d, size_t ld, int dt) {
+  if (((uintptr_t)p & 15u) || ld * (dt == ZL_DTYPE_BF16 ? 2 : 4) % 16) return kSingle;
+  return d % 8 ? kTail : kWhole;
 }
 
 }  // namespace act8

@@ -12,6 +12,9 @@ namespace zl {
 namespace {
 using namespace act8;
 
+// VEC: rows start on 16 bytes and are whole 8-column vectors.
+constexpr int mode_of(bool vec) { return vec ? kWhole : kSingle; }
+
 // ------------------------------------------------------------------------------------------------
 // Forward
 // ------------------------------------------------------------------------------------------------
@@ -53,38 +56,99 @@ __device__ __forceinline__ void bulk_row(void* dst, const void* src, uint32_t by
                : "memory");
 }
 
-// Sums over the block of one or two values; every thread gets them. The scratch alternates between two buffers, so one
-// barrier per sum is enough: who writes a buffer again has passed the barrier of the sum between, after which everyone
-// had read it. `ok` is and-ed over the block on the way.
+// Sums over the block of one or two values; every thread gets them. The scratch (zeroed before, for the warps that do not
+// exist) alternates between two buffers, so one barrier per sum is enough: who writes a buffer again has passed the barrier
+// of the sum between, after which everyone had read it.
 struct Reducer {
   float (*sh)[2][16];
   int turn;
-  __device__ __forceinline__ bool sum(float& x, float& y, bool two, bool ok) {
-    const int w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  __device__ __forceinline__ static float total(const float* b) {
+    uint64_t v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 f = reinterpret_cast<const float4*>(b)[i];
+      v[2 * i] = f2(f.x, f.y);
+      v[2 * i + 1] = f2(f.z, f.w);
+    }
+#pragma unroll
+    for (int i = 4; i > 0; i >>= 1)
+#pragma unroll
+      for (int k = 0; k < i; ++k) v[k] = add2(v[k], v[k + i]);
+    const float2 f = uf2(v[0]);
+    return f.x + f.y;
+  }
+  __device__ __forceinline__ void sum(float& x) {
+    float* b = sh[turn][0];
+    turn ^= 1;
     x = warp_sum(x);
-    if (two) y = warp_sum(y);
+    if ((threadIdx.x & 31) == 0) b[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = total(b);
+  }
+  // Four sums at once (b: 64 floats of scratch, warps that do not exist zero). Within a warp each step hands half of the
+  // values to the other half of the lanes, so that every lane ends with one value; then the lanes take the warps' results.
+  __device__ __forceinline__ static float lanes4(const float* x) {
+    const int lane = threadIdx.x & 31;
+    const bool hi = lane & 16, q = lane & 8;
+    const float a = hi ? x[2] : x[0], b = hi ? x[3] : x[1];
+    const float a2 = a + __shfl_xor_sync(0xffffffffu, hi ? x[0] : x[2], 16);
+    const float b2 = b + __shfl_xor_sync(0xffffffffu, hi ? x[1] : x[3], 16);
+    float v = (q ? b2 : a2) + __shfl_xor_sync(0xffffffffu, q ? a2 : b2, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;   // of value lane / 8
+  }
+  __device__ __forceinline__ static void warps4(const float* b, float* x) {
+    const int lane = threadIdx.x & 31;
+    float v = b[(lane >> 3) * 16 + (lane & 7)] + b[(lane >> 3) * 16 + 8 + (lane & 7)];
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __shfl_sync(0xffffffffu, v, 8 * i);
+  }
+  __device__ __forceinline__ void sum(float& x, float& y) {
     float(*b)[16] = sh[turn];
     turn ^= 1;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      x += __shfl_xor_sync(0xffffffffu, x, o);
+      y += __shfl_xor_sync(0xffffffffu, y, o);
+    }
     if ((threadIdx.x & 31) == 0) {
-      b[0][w] = x;
-      if (two) b[1][w] = y;
+      b[0][threadIdx.x >> 5] = x;
+      b[1][threadIdx.x >> 5] = y;
     }
-    ok = __syncthreads_and(ok);
-    x = 0.f;
-    for (int i = 0; i < nw; i += 4) {   // entries past nw are 0
-      const float4 v = *reinterpret_cast<const float4*>(&b[0][i]);
-      x += (v.x + v.y) + (v.z + v.w);
-    }
-    if (two) {
-      y = 0.f;
-      for (int i = 0; i < nw; i += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(&b[1][i]);
-        y += (v.x + v.y) + (v.z + v.w);
-      }
-    }
-    return ok;
+    __syncthreads();
+    x = total(b[0]);
+    y = total(b[1]);
   }
 };
+
+// The ring's place of the row at hand.
+struct Turn {
+  int st = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int stages) {
+    if (++st == stages) {
+      st = 0;
+      phase ^= 1u;
+    }
+  }
+};
+// Waits for the row at hand. A wait that gives up (its limit is about 2 s) raises the block's flag, which every thread sees
+// after its next barrier.
+__device__ __forceinline__ void wait_row(uint64_t* full, const Turn& at, volatile int* abort_flag) {
+  tc::mbar_wait(&full[at.st], at.phase, abort_flag, nullptr);
+}
+// After a wait that gave up: lets the copies in flight land before the block ends (n of them, from the row at hand on).
+__device__ __forceinline__ void drain(uint64_t* full, Turn at, int stages, int n) {
+  for (int i = 0; i < n; ++i) {
+    const unsigned long long t0 = tc::gtimer();
+    while (!tc::mbar_test(&full[at.st], at.phase) && tc::gtimer() - t0 < 100000000ull) {
+    }
+    at.next(stages);
+  }
+}
 
 // What a launch of a ring kernel is given besides its operands.
 struct Ring {
@@ -96,11 +160,26 @@ struct Ring {
 // 8 columns of a parameter row as pairs: `none` where it is NULL, 0 past d.
 template <bool VEC>
 __device__ __forceinline__ void row8(const float* p, int c, int d, float none, uint64_t* w) {
-  if (p) load_raw<VEC>(p, c, d).pairs(w);
+  if (p) load_raw<mode_of(VEC)>(p, c, d).pairs(w);
   else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = f2(none, none);
   }
+}
+// 8 fp32 columns of a row in shared memory as pairs, the row as two planes (columns 0-3 and 4-7 of every vector), so that the
+// 16-byte accesses of neighbouring lanes are neighbours.
+__device__ __forceinline__ void get_pairs(const float* p, int c, int D, uint64_t* v) {
+  const float4 lo = *reinterpret_cast<const float4*>(p + c / 2), hi = *reinterpret_cast<const float4*>(p + D / 2 + c / 2);
+  v[0] = f2(lo.x, lo.y);
+  v[1] = f2(lo.z, lo.w);
+  v[2] = f2(hi.x, hi.y);
+  v[3] = f2(hi.z, hi.w);
+}
+__device__ __forceinline__ void put_pairs(float* p, int c, int D, const uint64_t* v) {
+  float f[8];
+  unpair(v, f);
+  *reinterpret_cast<float4*>(p + c / 2) = make_float4(f[0], f[1], f[2], f[3]);
+  *reinterpret_cast<float4*>(p + D / 2 + c / 2) = make_float4(f[4], f[5], f[6], f[7]);
 }
 // Sums of the two halves of pairs.
 __device__ __forceinline__ float fold(uint64_t v) {
@@ -143,7 +222,7 @@ struct Params {
 
 // VEC: rows start on 16 bytes; they come by bulk copies. KEEP: f or n are written in 8 bits.
 template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
-__global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
+__global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][2][16];
@@ -163,11 +242,11 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  auto fill = [&](int k) {   // row number k of this block
-    uint8_t* p = ring + (k % g.stages) * g.stage;
+  auto fill = [&](int k, int st) {   // row number k of this block into a stage
+    uint8_t* p = ring + st * g.stage;
     const size_t o = (size_t)(r0 + k) * a.d;
     if (VEC) {
-      uint64_t* bar = &full[k % g.stages];
+      uint64_t* bar = &full[st];
       tc::mbar_expect_tx(bar, 2 * bytes);
       bulk_row(p, (const T*)a.f + o, bytes, bar);
       bulk_row(p + g.pitch, (const T*)a.h + o, bytes, bar);
@@ -179,29 +258,31 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
     }
   };
   if (VEC && t == 0)
-    for (int k = 0; k < min(rows, g.stages); ++k) fill(k);
+    for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
   Params<VPT, VEC, BIAS> pa;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) pa.pre(j, (t + j * nt) * 8, a.d, a.nw, a.nb);
-  size_t gate_at = ~(size_t)0;
+  int gate_left = 0;   // rows of the gate row at hand that are still to come
   Reducer red{sh, 0};
+  Turn at;
   const float inv_d = 1.f / a.d;
   const uint64_t alpha = f2(a.alpha, a.alpha);
   int k = 0;
-  for (; k < rows; ++k) {
-    const int row = r0 + k, st = k % g.stages;
-    const size_t o = (size_t)row * a.d, gr = gate_row(row, a.gate_rows);
-    if (gr != gate_at) {
-      gate_at = gr;
+  for (; k < rows; ++k, at.next(g.stages)) {
+    const int row = r0 + k, st = at.st;
+    const size_t o = (size_t)row * a.d;
+    if (gate_left == 0) {
+      const size_t gr = gate_row(row, a.gate_rows);
+      gate_left = a.gate_rows ? a.gate_rows - row % a.gate_rows : a.N;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) pa.post(j, (t + j * nt) * 8, a.d, a.pw, a.pb, a.gate ? a.gate + gr * a.d : nullptr, a.beta);
     }
-    bool ok = true;
+    --gate_left;
     if (VEC) {
-      ok = tc::mbar_wait(&full[st], (uint32_t)(k / g.stages) & 1u, abort_flag, nullptr);
+      wait_row(full, at, abort_flag);
     } else {
       __syncthreads();
-      fill(k);
+      fill(k, 0);
       __syncthreads();
     }
     Raw8<T> rf[VPT], rh[VPT];
@@ -215,7 +296,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
         rh[j].get(ring + st * g.stage + g.pitch + c * sizeof(T));
       }
     }
-    float unused = 0.f, mean = 0.f, rstd = 1.f;
+    float mean = 0.f, rstd = 1.f;
     uint64_t h[VPT][4];
     // mean and 1 / deviation of the values val(j, x) of every vector; after the first barrier of a row everyone has it in
     // registers, and its stage takes the row `stages` further on
@@ -223,7 +304,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
       mean = 0.f;
       rstd = 1.f;
       auto next = [&]() {
-        if (VEC && first && ok && t == 0 && k + g.stages < rows) fill(k + g.stages);
+        if (VEC && first && t == 0 && k + g.stages < rows && !*abort_flag) fill(k + g.stages, st);
         first = false;
       };
       if (kind == ZL_NORM_LAYER) {
@@ -235,7 +316,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
           s = add2(s, add2(add2(x[0], x[1]), add2(x[2], x[3])));
         }
         float m = fold(s);
-        ok = red.sum(m, unused, false, ok);
+        red.sum(m);
         next();
         mean = m * inv_d;
       }
@@ -256,11 +337,11 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
           for (int i = 0; i < 4; ++i) q2 = fma2(x[i], x[i], q2);
         }
         float q = fold(q2);
-        ok = red.sum(q, unused, false, ok);
+        red.sum(q);
         next();
         rstd = 1.f / sqrtf(q * inv_d + a.eps);
       } else if (first) {
-        ok = __syncthreads_and(ok);
+        __syncthreads();
         next();
       }
     };
@@ -274,7 +355,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
       }
     }
     stat(a.post, [&](int j, uint64_t* x) { rf[j].pairs(x); }, true);
-    if (!ok) break;
+    if (VEC && *abort_flag) break;
     if (t == 0) {
       a.stats[row] = mean;
       a.stats[(size_t)a.N + row] = rstd;
@@ -296,7 +377,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
         cut(h[j], c, a.d);
         float x[8];
         unpair(h[j], x);
-        store8<VEC>((T*)a.ho + o, c, a.d, x);
+        store8<mode_of(VEC)>((T*)a.ho + o, c, a.d, x);
       }
     }
     stat(a.pre, [&](int j, uint64_t* x) {
@@ -321,7 +402,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
       }
       cut(h[j], c, a.d);
       unpair(h[j], n);
-      store8<VEC>((T*)a.no + o, c, a.d, n);
+      store8<mode_of(VEC)>((T*)a.no + o, c, a.d, n);
       if (KEEP && a.nq) {   // of n as it is stored
 #pragma unroll
         for (int i = 0; i < 8; ++i) n[i] = to_f(from_f<T>(n[i]));
@@ -329,13 +410,7 @@ __global__ void __launch_bounds__(512) fwd_ring_k(const Fwd a, const Ring g) {
       }
     }
   }
-  if (VEC && k < rows && t == 0) {   // a wait gave up: let the copies in flight land before the block ends
-    for (int i = k; i < min(rows, k + g.stages); ++i) {
-      const unsigned long long t0 = tc::gtimer();
-      while (!tc::mbar_test(&full[i % g.stages], (uint32_t)(i / g.stages) & 1u) && tc::gtimer() - t0 < 100000000ull) {
-      }
-    }
-  }
+  if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
 }
 
 // Rows of any width: a block per row that reads it again for every sum.
@@ -349,27 +424,27 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   const float inv_d = 1.f / a.d;
   const float* gr = a.gate ? a.gate + gate_row(row, a.gate_rows) * a.d : nullptr;
   float pm = 0.f, pr = 1.f, m = 0.f, r = 1.f;
-  auto fval = [&](int c, float* x) { load8<VEC>((const T*)a.f + o, c, a.d, x); };
+  auto fval = [&](int c, float* x) { load8<mode_of(VEC)>((const T*)a.f + o, c, a.d, x); };
   auto hval = [&](int c, float* x) {   // h' before its rounding
     float f[8], w[8];
     fval(c, f);
-    load8<VEC>((const T*)a.h + o, c, a.d, x);
+    load8<mode_of(VEC)>((const T*)a.h + o, c, a.d, x);
     if (a.post) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = (f[i] - pm) * pr;
       if (a.pw) {
-        load8<VEC>(a.pw, c, a.d, w);
+        load8<mode_of(VEC)>(a.pw, c, a.d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] *= w[i];
       }
       if (a.pb) {
-        load8<VEC>(a.pb, c, a.d, w);
+        load8<mode_of(VEC)>(a.pb, c, a.d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += w[i];
       }
     }
     if (gr) {
-      load8<VEC>(gr, c, a.d, w);
+      load8<mode_of(VEC)>(gr, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] *= w[i];
     }
@@ -415,21 +490,21 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
       put_codes(a.fmt, x, a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
     }
     hval(c, x);
-    store8<VEC>((T*)a.ho + o, c, a.d, x);
+    store8<mode_of(VEC)>((T*)a.ho + o, c, a.d, x);
     if (!a.pre) continue;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (x[i] - m) * r;
     if (a.nw) {
-      load8<VEC>(a.nw, c, a.d, w);
+      load8<mode_of(VEC)>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] *= w[i];
     }
     if (a.nb) {
-      load8<VEC>(a.nb, c, a.d, w);
+      load8<mode_of(VEC)>(a.nb, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] += w[i];
     }
-    store8<VEC>((T*)a.no + o, c, a.d, x);
+    store8<mode_of(VEC)>((T*)a.no + o, c, a.d, x);
     if (a.nq) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = c + i < a.d ? to_f(from_f<T>(x[i])) : 0.f;
@@ -455,6 +530,10 @@ struct Occupancy {
   }
   static constexpr int kMaxSmem = 232448;
 };
+
+constexpr int kRingCols = 8192;   // the widest row of the ring kernels
+// Threads of a block for a row of nvec vectors, one vector a thread or two.
+int ring_threads(int nvec) { return nvec <= 224 ? (nvec + 31) / 32 * 32 : (nvec + 63) / 64 * 32; }
 
 template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
 bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
@@ -484,8 +563,10 @@ template <typename T, bool VEC>
 void forward_as(const Fwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
   note_launch(1);
-  if (nvec <= 512 && fwd_ring_by<T, 1, VEC>(a, (nvec + 31) / 32 * 32, s)) return;
-  if (nvec > 512 && nvec <= 1024 && fwd_ring_by<T, 2, VEC>(a, (nvec + 63) / 64 * 32, s)) return;
+  if (a.d <= kRingCols) {
+    const int th = ring_threads(nvec);
+    if (th >= nvec ? fwd_ring_by<T, 1, VEC>(a, th, s) : fwd_ring_by<T, 2, VEC>(a, th, s)) return;
+  }
   launch_pdl(fwd_any_k<T, VEC>, a.N, 512, 0, s, a);
 }
 template <typename T>
@@ -546,7 +627,7 @@ __device__ __forceinline__ void f8(const Bwd& a, int n, int c, float* x) {
       for (int i = 0; i < 8; ++i) x[i] = 0.f;
     }
   } else {
-    load8<VEC>((const T*)a.f + (size_t)n * a.d, c, a.d, x);
+    load8<mode_of(VEC)>((const T*)a.f + (size_t)n * a.d, c, a.d, x);
   }
 }
 
@@ -556,14 +637,14 @@ __device__ __forceinline__ void grad8(const Bwd& a, int n, int c, float s1, floa
   const size_t o = (size_t)n * a.d;
 #pragma unroll
   for (int i = 0; i < 8; ++i) G[i] = 0.f;
-  if (a.dho) load8<VEC>((const T*)a.dho + o, c, a.d, G);
+  if (a.dho) load8<mode_of(VEC)>((const T*)a.dho + o, c, a.d, G);
   if (a.pre) {
     const float m = a.stats[2 * (size_t)a.N + n], r = a.stats[3 * (size_t)a.N + n];
     float u[8], x[8], w[8];
-    load8<VEC>((const T*)a.dn + o, c, a.d, u);
-    load8<VEC>((const T*)a.ho + o, c, a.d, x);
+    load8<mode_of(VEC)>((const T*)a.dn + o, c, a.d, u);
+    load8<mode_of(VEC)>((const T*)a.ho + o, c, a.d, x);
     if (a.nw) {
-      load8<VEC>(a.nw, c, a.d, w);
+      load8<mode_of(VEC)>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] *= w[i];
     }
@@ -584,10 +665,10 @@ __global__ void __launch_bounds__(256) bwd_sums_k(const Bwd a) {
   float s1 = 0.f, s2 = 0.f;
   for (int c = threadIdx.x * 8; c < a.d; c += blockDim.x * 8) {
     float u[8], x[8], w[8];
-    load8<VEC>((const T*)a.dn + o, c, a.d, u);
-    load8<VEC>((const T*)a.ho + o, c, a.d, x);
+    load8<mode_of(VEC)>((const T*)a.dn + o, c, a.d, u);
+    load8<mode_of(VEC)>((const T*)a.ho + o, c, a.d, x);
     if (a.nw) {
-      load8<VEC>(a.nw, c, a.d, w);
+      load8<mode_of(VEC)>(a.nw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] *= w[i];
     }
@@ -638,8 +719,8 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
       grad8<T, VEC>(a, n, c, a.pre ? a.s12[n] : 0.f, a.pre ? a.s12[(size_t)a.N + n] : 0.f, G);
       if (a.pre) {
         const float m = a.stats[2 * (size_t)a.N + n], r = a.stats[3 * (size_t)a.N + n];
-        load8<VEC>((const T*)a.dn + (size_t)n * a.d, c, a.d, w);
-        load8<VEC>((const T*)a.ho + (size_t)n * a.d, c, a.d, x);
+        load8<mode_of(VEC)>((const T*)a.dn + (size_t)n * a.d, c, a.d, w);
+        load8<mode_of(VEC)>((const T*)a.ho + (size_t)n * a.d, c, a.d, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           acc[0][i] += w[i] * ((x[i] - m) * r);
@@ -651,9 +732,9 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
       float gt[8], b[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) { gt[i] = 1.f; w[i] = 1.f; b[i] = 0.f; }
-      if (a.gate) load8<VEC>(a.gate + gate_row(n, a.gate_rows) * a.d, c, a.d, gt);
-      if (a.pw) load8<VEC>(a.pw, c, a.d, w);
-      if (a.pb) load8<VEC>(a.pb, c, a.d, b);
+      if (a.gate) load8<mode_of(VEC)>(a.gate + gate_row(n, a.gate_rows) * a.d, c, a.d, gt);
+      if (a.pw) load8<mode_of(VEC)>(a.pw, c, a.d, w);
+      if (a.pb) load8<mode_of(VEC)>(a.pb, c, a.d, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float fh = a.post ? (x[i] - pm) * pr : x[i], q = a.beta * G[i];
@@ -698,13 +779,13 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = a.beta * G[i];
     if (gr) {
-      load8<VEC>(gr, c, a.d, w);
+      load8<mode_of(VEC)>(gr, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= w[i];
     }
     if (!a.post) return;
     if (a.pw) {
-      load8<VEC>(a.pw, c, a.d, w);
+      load8<mode_of(VEC)>(a.pw, c, a.d, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= w[i];
     }
@@ -734,8 +815,8 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
       G[i] *= a.alpha;
       if (a.post) v[i] = pr * (v[i] - t1 - fh[i] * t2);
     }
-    if (a.dh) store8<VEC>((T*)a.dh + o, c, a.d, G);
-    store8<VEC>((T*)a.df + o, c, a.d, v);
+    if (a.dh) store8<mode_of(VEC)>((T*)a.dh + o, c, a.d, G);
+    store8<mode_of(VEC)>((T*)a.df + o, c, a.d, v);
   }
 }
 
@@ -743,31 +824,52 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
 // Backward in one pass over the rows: a block takes a chunk of neighbouring rows through the ring (dn, dh', h', f of a row a
 // stage) and keeps its columns' sums over them in registers. With s = sum G fh and z = sum G over rows of one gate row,
 //   dgate = beta (w_post s + b_post z),  dw_post = beta gate s,  db_post = beta gate z
-// so two sums (four with a LayerNorm's bias) are kept for five gradients. Per row two block-wide sums in turn: those of the
-// pre norm give G, those of the post norm, which needs G, give df.
+// so two sums (four with a LayerNorm's bias) are kept for five gradients.
+// G = dh' + r (u - m1 - xh m2) needs the row's means m1 of u and m2 of u xh, df the means of v = A G (A = beta gate w_post)
+// and of v fh. These are linear in m1 and m2: with g = dh' + r u,
+//   sum v fh = sum A fh g - r m1 sum A fh - r m2 sum A fh xh,   sum v = sum A g - r m1 sum A - r m2 sum A xh
+// so one barrier a row yields every mean: three sums with RMS norms, eight at most.
 // ------------------------------------------------------------------------------------------------
-// The 8 values of f at column c of a row in shared memory (a row of T, or of codes).
-template <typename T>
-__device__ __forceinline__ void f_pairs(const Bwd& a, const uint8_t* row, uint32_t e, int c, uint64_t* f) {
+// The normalised f, (f - pm) pr, at column c of a row in shared memory (a row of T, or of codes whose group byte is e).
+template <typename T, bool LN>
+__device__ __forceinline__ void norm_f(const Bwd& a, const uint8_t* row, uint32_t e, int c, float pm, float pr, uint64_t* f) {
+  float sc = 1.f;
   if (a.fq) {
     const uint2 w = *reinterpret_cast<const uint2*>(row + c);
     float x[8];
-    if (a.fmt == ZL_ACT8_E4M3) decode8<ZL_ACT8_E4M3>(w, e, x);
-    else decode8<ZL_ACT8_INT8>(w, e, x);
+    if (a.fmt == ZL_ACT8_E4M3) {
+      codes4<ZL_ACT8_E4M3>(w.x, x);
+      codes4<ZL_ACT8_E4M3>(w.y, x + 4);
+    } else {
+      codes4<ZL_ACT8_INT8>(w.x, x);
+      codes4<ZL_ACT8_INT8>(w.y, x + 4);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = f2(x[2 * i], x[2 * i + 1]);
+    sc = group_scale(e);
   } else {
     Raw8<T> r;
     r.get(row + c * sizeof(T));
     r.pairs(f);
   }
+  if (LN) {   // the product with a power of two is exact
+    const uint64_t ss = f2(sc, sc), mm = f2(-pm, -pm), rr = f2(pr, pr);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = mul2(fma2(f[i], ss, mm), rr);
+  } else {
+    // (a group's scale is at most the row's largest value, pr its deviation's inverse: their product does not overflow)
+    const uint64_t rr = f2(sc * pr, sc * pr);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = mul2(f[i], rr);
+  }
 }
 
-template <typename T, int VPT, bool VEC, bool BIAS>
+// LN: one of the norms is a LayerNorm (its sums of u, v and A, and the biases' gradients).
+template <typename T, int VPT, bool VEC, bool LN>
 __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
-  __shared__ __align__(16) float sh[2][2][16];
+  __shared__ __align__(16) float sh[2][LN ? 2 : 1][64];
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
   const int t = threadIdx.x, nt = blockDim.x;
@@ -781,7 +883,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = t; i < 64; i += nt) (&sh[0][0][0])[i] = 0.f;
+  for (int i = t; i < (LN ? 256 : 128); i += nt) (&sh[0][0][0])[i] = 0.f;
   for (int k = 0; k < 4 * g.stages; ++k)   // columns past d, and tensors that are not given, read 0
     for (int c = ((k & 3) == 0 && a.dn) || ((k & 3) == 1 && a.dho) || ((k & 3) == 2 && a.pre) || ((k & 3) == 3 && !a.fq) ? a.d + t : t;
          c < ((k & 3) == 3 && a.fq ? 0 : a.D); c += nt)
@@ -789,12 +891,12 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  auto fill = [&](int k) {
-    uint8_t* p = ring + (k % g.stages) * g.stage;
+  auto fill = [&](int k, int st) {   // row number k of this block into a stage
+    uint8_t* p = ring + st * g.stage;
     const int n = r0 + k;
     const size_t o = (size_t)n * a.d;
     if (VEC) {
-      uint64_t* bar = &full[k % g.stages];
+      uint64_t* bar = &full[st];
       tc::mbar_expect_tx(bar, bytes * ((a.pre ? 2 : 0) + (a.dho ? 1 : 0) + (a.fq ? 0 : 1)) + (a.fq ? (uint32_t)a.D : 0u));
       if (a.pre) {
         bulk_row(p, (const T*)a.dn + o, bytes, bar);
@@ -818,20 +920,21 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
     }
   };
   if (VEC && t == 0)
-    for (int k = 0; k < min(rows, g.stages); ++k) fill(k);
-  uint64_t w[VPT][4], pw[VPT][4], gt[VPT][4];            // w_pre; w_post; beta gate
-  uint64_t s[VPT][4], z[BIAS ? VPT : 1][4];              // sums G fh, G of the gate row at hand
-  uint64_t dw[VPT][4], db[BIAS ? VPT : 1][4];            // sums dn xh, dn
-  float unused = 0.f;
+    for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
+  // w_pre and A = beta gate w_post of the block's columns, behind the ring (every thread reads what it wrote)
+  float* const prm = reinterpret_cast<float*>(ring + g.stages * g.stage);
+  uint64_t s[VPT][4], z[LN ? VPT : 1][4];                // sums G fh, G of the gate row at hand
+  uint64_t dw[VPT][4], db[LN ? VPT : 1][4];              // sums dn xh, dn
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int c = (t + j * nt) * 8;
-    row8<VEC>(a.nw, c, a.d, 1.f, w[j]);
-    row8<VEC>(a.pw, c, a.d, 1.f, pw[j]);
+    uint64_t w[4];
+    row8<VEC>(a.nw, c, a.d, 1.f, w);
+    if (c < a.D) put_pairs(prm, c, a.D, w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       s[j][i] = dw[j][i] = 0;
-      if (BIAS) z[j][i] = db[j][i] = 0;
+      if (LN) z[j][i] = db[j][i] = 0;
     }
   }
   // the sums over a gate row's rows [.., n] go to where their gradients are formed: dgate itself where the chunk knows all of
@@ -839,56 +942,56 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   float* const part = a.part + (size_t)blockIdx.x * 5 * a.d;
   bool fresh = true;
   auto flush = [&](int n) {
+    const float* gr = a.gate ? a.gate + gate_row(n, a.gate_rows) * a.d : nullptr;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
       if (c >= a.d) continue;
-      float sv[8], zv[8], x[8], y[8];
-      unpair(s[j], sv);
+      uint64_t p[4], v[4], gt[4], pb[4];
+      float x[8], y[8];
+      row8<VEC>(a.pw, c, a.d, 1.f, p);   // every load first
+      row8<VEC>(gr, c, a.d, 1.f, gt);
+      if (LN) row8<VEC>(a.pb, c, a.d, 0.f, pb);
       if (a.out[4]) {
-        uint64_t b[4];
-        if (BIAS) row8<VEC>(a.pb, c, a.d, 0.f, b);
-        uint64_t v[4];
+        float* q = a.per_group ? part + 4 * (size_t)a.d : a.out[4] + gate_row(n, a.gate_rows) * a.d;
+        const bool add = !a.per_group && a.accumulate;
+        if (add) load8<mode_of(VEC)>((const float*)q, c, a.d, y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          v[i] = mul2(pw[j][i], s[j][i]);
-          if (BIAS) v[i] = fma2(b[i], z[j][i], v[i]);
+          v[i] = mul2(p[i], s[j][i]);
+          if (LN) v[i] = fma2(pb[i], z[j][i], v[i]);
           v[i] = mul2(v[i], f2(a.beta, a.beta));
         }
         unpair(v, x);
-        float* q = a.per_group ? part + 4 * (size_t)a.d : a.out[4] + gate_row(n, a.gate_rows) * a.d;
-        if (!a.per_group && a.accumulate) {
-          load8<VEC>((const float*)q, c, a.d, y);
+        if (add) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] += y[i];
         }
-        store8<VEC>(q, c, a.d, x);
+        store8<mode_of(VEC)>(q, c, a.d, x);
       }
-      float gv[8];
-      unpair(gt[j], gv);
-      if (BIAS) unpair(z[j], zv);
 #pragma unroll
-      for (int k = 0; k < (BIAS ? 2 : 1); ++k) {
+      for (int k = 0; k < (LN ? 2 : 1); ++k) {
         if (!a.out[2 + k]) continue;
         float* q = part + (2 + k) * (size_t)a.d;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = gv[i] * (k ? zv[i] : sv[i]);
+        for (int i = 0; i < 4; ++i) v[i] = mul2(mul2(gt[i], f2(a.beta, a.beta)), k ? z[j][i] : s[j][i]);
+        unpair(v, x);
         if (!fresh) {
-          load8<VEC>((const float*)q, c, a.d, y);
+          load8<mode_of(VEC)>((const float*)q, c, a.d, y);
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] += y[i];
         }
-        store8<VEC>(q, c, a.d, x);
+        store8<mode_of(VEC)>(q, c, a.d, x);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         s[j][i] = 0;
-        if (BIAS) z[j][i] = 0;
+        if (LN) z[j][i] = 0;
       }
     }
     fresh = false;
   };
-  Reducer red{sh, 0};
+  int turn = 0;
   const float inv_d = 1.f / a.d;
   const uint64_t alpha = f2(a.alpha, a.alpha);
   // statistics and group bytes of the next row, read a row ahead
@@ -907,18 +1010,25 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   };
   if (rows > 0) ahead(r0);
   bool new_gate = true;
+  int gate_left = a.per_group ? rows : gate_rows - r0 % gate_rows;   // rows of the gate row at hand to come, this one among them
+  Turn at;
   int k = 0;
-  for (; k < rows; ++k) {
-    const int n = r0 + k, st = k % g.stages;
+  for (; k < rows; ++k, at.next(g.stages)) {
+    const int n = r0 + k, st = at.st;
     const size_t o = (size_t)n * a.d;
     const uint8_t* p = ring + st * g.stage;
     if (new_gate) {
       const float* gr = a.gate ? a.gate + gate_row(n, a.gate_rows) * a.d : nullptr;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
-        row8<VEC>(gr, (t + j * nt) * 8, a.d, 1.f, gt[j]);
+        const int c = (t + j * nt) * 8;
+        uint64_t A[4], p[4];
+        row8<VEC>(gr, c, a.d, 1.f, A);
+        row8<VEC>(a.pw, c, a.d, 1.f, p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) gt[j][i] = mul2(gt[j][i], f2(a.beta, a.beta));
+        for (int i = 0; i < 4; ++i) A[i] = mul2(mul2(A[i], f2(a.beta, a.beta)), p[i]);
+        cut(A, c, a.d);
+        if (c < a.D) put_pairs(prm + a.D, c, a.D, A);
       }
       new_gate = false;
     }
@@ -927,113 +1037,126 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) e[j] = eb[j];
     if (k + 1 < rows) ahead(n + 1);
-    bool ok = true;
     if (VEC) {
-      ok = tc::mbar_wait(&full[st], (uint32_t)(k / g.stages) & 1u, abort_flag, nullptr);
+      wait_row(full, at, abort_flag);
     } else {
       __syncthreads();
-      fill(k);
+      fill(k, 0);
       __syncthreads();
     }
-    // u and xh of the pre norm, then G; v and fh of the post norm
-    uint64_t u[VPT][4], x[VPT][4];
-    float s1 = 0.f, s2 = 0.f;
-    if (a.pre) {
-      const uint64_t mm = f2(m, m), rr = f2(r, r);
-      uint64_t t1 = 0, t2 = 0;
+    // g, xh and fh of the row, and its sums
+    uint64_t G[VPT][4], xh[VPT][4], fh[VPT][4];
+    {
+      const uint64_t mm = f2(m, m), rr = f2(r, r), prr = f2(pr, pr);
+      uint64_t ux = 0, vf = 0, fx = 0, u1 = 0, v1 = 0, af = 0, ax = 0, a1 = 0;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (t + j * nt) * 8;
-        Raw8<T> rn, rx;
-        rn.zero();
-        rx.zero();
-        if (c < a.D) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) G[j][i] = xh[j][i] = fh[j][i] = 0;
+        if (c >= a.D) continue;
+        Raw8<T> rd, rn, rx;
+        rd.get(p + g.pitch + c * sizeof(T));
+        uint64_t u[4], w[4], A[4];
+        get_pairs(prm + a.D, c, a.D, A);
+        norm_f<T, LN>(a, p + 3 * g.pitch, e[j], c, pm, pr, fh[j]);
+        rd.pairs(G[j]);
+        if (a.pre) {
           rn.get(p + c * sizeof(T));
           rx.get(p + 2 * g.pitch + c * sizeof(T));
+          get_pairs(prm, c, a.D, w);
+          rn.pairs(u);
+          rx.pairs(xh[j]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (LN) {
+              xh[j][i] = sub2(xh[j][i], mm);
+              db[j][i] = add2(db[j][i], u[i]);
+            }
+            xh[j][i] = mul2(xh[j][i], rr);
+            dw[j][i] = fma2(u[i], xh[j][i], dw[j][i]);
+            u[i] = mul2(u[i], w[i]);
+            ux = fma2(u[i], xh[j][i], ux);
+            if (LN) u1 = add2(u1, u[i]);
+            G[j][i] = fma2(rr, u[i], G[j][i]);
+          }
         }
-        rn.pairs(u[j]);
-        rx.pairs(x[j]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (a.pre == ZL_NORM_LAYER) x[j][i] = sub2(x[j][i], mm);
-          x[j][i] = mul2(x[j][i], rr);
-          dw[j][i] = fma2(u[j][i], x[j][i], dw[j][i]);
-          if (BIAS) db[j][i] = add2(db[j][i], u[j][i]);
-          u[j][i] = mul2(u[j][i], w[j][i]);
-          t2 = fma2(u[j][i], x[j][i], t2);
-          if (a.pre == ZL_NORM_LAYER) t1 = add2(t1, u[j][i]);
+          const uint64_t y = mul2(A[i], fh[j][i]);
+          vf = fma2(y, G[j][i], vf);
+          fx = fma2(y, xh[j][i], fx);
+          if (LN) {
+            af = add2(af, y);
+            v1 = fma2(A[i], G[j][i], v1);
+            ax = fma2(A[i], xh[j][i], ax);
+            a1 = add2(a1, A[i]);
+          }
         }
       }
-      s1 = fold(t1);
-      s2 = fold(t2);
-      ok = a.pre == ZL_NORM_LAYER ? red.sum(s2, s1, true, ok) : red.sum(s2, unused, false, ok);
-      s1 *= inv_d;
-      s2 *= inv_d;
-    }
-    float q1 = 0.f, q2 = 0.f;
-    {
-      const uint64_t rr = f2(r, r), n1 = f2(-s1, -s1), n2 = f2(-s2, -s2), pmm = f2(pm, pm), prr = f2(pr, pr);
-      uint64_t t1 = 0, t2 = 0;
+      float* const b = &sh[turn][0][0];
+      turn ^= 1;
+      const float x4[4] = {fold(ux), fold(vf), fold(fx), LN ? fold(u1) : 0.f};
+      const float v4 = Reducer::lanes4(x4);
+      if ((t & 7) == 0) b[((t & 31) >> 3) * 16 + (t >> 5)] = v4;
+      if (LN) {
+        const float y4[4] = {fold(v1), fold(af), fold(ax), fold(a1)};
+        const float w4 = Reducer::lanes4(y4);
+        if ((t & 7) == 0) b[64 + ((t & 31) >> 3) * 16 + (t >> 5)] = w4;
+      }
+      __syncthreads();
+      if (VEC && *abort_flag) break;
+      // everyone has the row in registers
+      if (VEC && t == 0 && k + g.stages < rows) fill(k + g.stages, st);
+      float sx[4], sy[4];
+      Reducer::warps4(b, sx);
+      if (LN) Reducer::warps4(b + 64, sy);
+      const float m2 = a.pre ? sx[0] * inv_d : 0.f, m1 = a.pre == ZL_NORM_LAYER ? sx[3] * inv_d : 0.f;
+      float q2 = a.post ? (sx[1] - r * m2 * sx[2]) * inv_d : 0.f, q1 = 0.f;
+      if (LN) {
+        q2 = a.post ? (sx[1] - r * (m1 * sy[1] + m2 * sx[2])) * inv_d : 0.f;
+        q1 = a.post == ZL_NORM_LAYER ? (sy[0] - r * (m1 * sy[3] + m2 * sy[2])) * inv_d : 0.f;
+      }
+      const uint64_t c1 = f2(-r * m1, -r * m1), c2 = f2(-r * m2, -r * m2), d1 = f2(-q1, -q1), d2 = f2(-q2, -q2);
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (t + j * nt) * 8;
-        uint64_t G[4];
-        Raw8<T> rd;
-        rd.zero();
-        if (c < a.D) rd.get(p + g.pitch + c * sizeof(T));
-        rd.pairs(G);
+        if (c >= a.d) continue;
+        uint64_t v[4], A[4];
+        float y[8];
+        get_pairs(prm + a.D, c, a.D, A);
         if (a.pre) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) G[i] = fma2(rr, fma2(x[j][i], n2, add2(u[j][i], n1)), G[i]);
-          cut(G, c, a.d);
+          for (int i = 0; i < 4; ++i) {
+            G[j][i] = fma2(xh[j][i], c2, G[j][i]);
+            if (LN) G[j][i] = add2(G[j][i], c1);
+          }
+          cut(G[j], c, a.d);
         }
-        if (c < a.D) f_pairs<T>(a, p + 3 * g.pitch, e[j], c, x[j]);
-        else
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[j][i] = 0;
-        uint64_t dh[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (a.post == ZL_NORM_LAYER) x[j][i] = sub2(x[j][i], pmm);
-          if (a.post) x[j][i] = mul2(x[j][i], prr);
-          s[j][i] = fma2(G[i], x[j][i], s[j][i]);
-          if (BIAS) z[j][i] = add2(z[j][i], G[i]);
-          dh[i] = mul2(G[i], alpha);
-          u[j][i] = mul2(mul2(G[i], gt[j][i]), pw[j][i]);
-          t2 = fma2(u[j][i], x[j][i], t2);
-          if (a.post == ZL_NORM_LAYER) t1 = add2(t1, u[j][i]);
+          s[j][i] = fma2(G[j][i], fh[j][i], s[j][i]);
+          if (LN) z[j][i] = add2(z[j][i], G[j][i]);
+          v[i] = mul2(G[j][i], alpha);
         }
         if (a.dh) {
-          float y[8];
-          unpair(dh, y);
-          store8<VEC>((T*)a.dh + o, c, a.d, y);
+          unpair(v, y);
+          store8<mode_of(VEC)>((T*)a.dh + o, c, a.d, y);
         }
-      }
-      q1 = fold(t1);
-      q2 = fold(t2);
-    }
-    if (a.post == ZL_NORM_LAYER) ok = red.sum(q2, q1, true, ok);
-    else if (a.post) ok = red.sum(q2, unused, false, ok);
-    else ok = __syncthreads_and(ok);
-    if (!ok) break;
-    if (VEC && t == 0 && k + g.stages < rows) fill(k + g.stages);   // everyone has read the row
-    {
-      const uint64_t prr = f2(pr, pr), n1 = f2(-q1 * inv_d, -q1 * inv_d), n2 = f2(-q2 * inv_d, -q2 * inv_d);
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int c = (t + j * nt) * 8;
-        if (a.post) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) u[j][i] = mul2(prr, fma2(x[j][i], n2, add2(u[j][i], n1)));
+        for (int i = 0; i < 4; ++i) {
+          v[i] = fma2(fh[j][i], d2, mul2(A[i], G[j][i]));
+          if (LN) v[i] = add2(v[i], d1);
+          v[i] = mul2(v[i], prr);
         }
-        float y[8];
-        unpair(u[j], y);
-        store8<VEC>((T*)a.df + o, c, a.d, y);
+        unpair(v, y);
+        store8<mode_of(VEC)>((T*)a.df + o, c, a.d, y);
       }
     }
-    if (k + 1 == rows || (!a.per_group && (n + 1) % gate_rows == 0)) {
+    if (--gate_left == 0 || k + 1 == rows) {
       flush(n);
       new_gate = true;
+      gate_left = gate_rows;
     }
   }
   if (k == rows) {
@@ -1043,34 +1166,28 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       if (c >= a.d) continue;
       float x[8];
       unpair(dw[j], x);
-      if (a.out[0]) store8<VEC>(part, c, a.d, x);
-      if (BIAS && a.out[1]) {
+      if (a.out[0]) store8<mode_of(VEC)>(part, c, a.d, x);
+      if (LN && a.out[1]) {
         unpair(db[j], x);
-        store8<VEC>(part + a.d, c, a.d, x);
+        store8<mode_of(VEC)>(part + a.d, c, a.d, x);
       }
       if (rows == 0) {   // a chunk past its gate group's end
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.f;
         for (int i = 2; i < 5; ++i)
-          if (a.out[i]) store8<VEC>(part + i * (size_t)a.d, c, a.d, x);
+          if (a.out[i]) store8<mode_of(VEC)>(part + i * (size_t)a.d, c, a.d, x);
       }
     }
   }
-  if (VEC && k < rows && t == 0) {   // a wait gave up: let the copies in flight land before the block ends
-    for (int i = k; i < min(rows, k + g.stages); ++i) {
-      const unsigned long long t0 = tc::gtimer();
-      while (!tc::mbar_test(&full[i % g.stages], (uint32_t)(i / g.stages) & 1u) && tc::gtimer() - t0 < 100000000ull) {
-      }
-    }
-  }
+  if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
 }
 
-// The chunks' partial sums: a block takes 32 columns of one gradient (blockIdx.y 0..3 the parameters, 4 + g gate row g), 8
-// lanes of rows each adding every 8th chunk, the lanes' sums then in order.
-__global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
+// The chunks' partial sums: a block takes 32 columns of one gradient (blockIdx.y 0..3 the parameters, 4 + g gate row g), 32
+// lanes of rows each adding every 32nd chunk, the lanes' sums then in order.
+__global__ void __launch_bounds__(1024) bwd_join_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float sh[8][32];
+  __shared__ float sh[32][33];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
   for (int y = blockIdx.y; y < 4 + (a.per_group ? a.chunks / a.per_group : 0); y += gridDim.y) {
     const int k = min(y, 4);
@@ -1079,15 +1196,15 @@ __global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
     float s = 0.f;
     if (c < a.d) {
 #pragma unroll 8
-      for (int b = b0 + ty; b < b1; b += 8) s += a.part[((size_t)b * 5 + k) * a.d + c];
+      for (int b = b0 + ty; b < b1; b += 32) s += a.part[((size_t)b * 5 + k) * a.d + c];
     }
     __syncthreads();
     sh[ty][tx] = s;
     __syncthreads();
-    if (ty == 0 && c < a.d) {
-#pragma unroll
-      for (int i = 1; i < 8; ++i) s += sh[i][tx];
-      float* p = a.out[k] + (k < 4 ? 0 : (size_t)(y - 4) * a.d) + c;
+    s = warp_sum(sh[tx][ty]);   // column blockIdx.x * 32 + ty
+    const int col = blockIdx.x * 32 + ty;
+    if (tx == 0 && col < a.d) {
+      float* p = a.out[k] + (k < 4 ? 0 : (size_t)(y - 4) * a.d) + col;
       *p = a.accumulate ? *p + s : s;
     }
   }
@@ -1107,31 +1224,33 @@ void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, in
   }
 }
 constexpr int kAnyRows = 64;      // rows of a chunk of bwd_cols_k
-constexpr int kRingCols = 8192;   // the widest row of bwd_ring_k
+// (LayerNorm's sums leave no room for two vectors a thread up to 512 threads)
+int bwd_threads(int nvec, bool ln) { return ln && nvec <= 512 ? (nvec + 31) / 32 * 32 : ring_threads(nvec); }
 // Rows of a chunk of bwd_ring_k: enough chunks for the blocks that fit on 152 SMs, but not so short that their partial sums
 // (written once and read once, 8 bytes a column and sum) weigh as much as the rows.
-int ring_rows(int N, int d) {
-  const int th = (pitch(d) / 8 + 31) / 32 * 32, per_sm = std::max(1, std::min(8, 512 / th));
+int ring_rows(int N, int d, bool ln) {
+  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
   return std::max(4, (N + 152 * per_sm - 1) / (152 * per_sm));
 }
 void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
-  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d) : kAnyRows, rows, per_group, chunks);
+  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d, p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER) : kAnyRows, rows, per_group, chunks);
 }
 
-template <typename T, int VPT, bool VEC, bool BIAS>
+template <typename T, int VPT, bool VEC, bool LN>
 bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
-  static const Occupancy occ(bwd_ring_k<T, VPT, VEC, BIAS>);
+  static const Occupancy occ(bwd_ring_k<T, VPT, VEC, LN>);
   if (!occ.ok) return false;
   Ring g = {};
+  const size_t prm = (size_t)a.D * 8;   // the parameters behind the ring
   g.pitch = (uint32_t)a.D * sizeof(T);
   g.stage = 3 * g.pitch + (a.fq ? (uint32_t)a.D : g.pitch);
   const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), (a.chunks + sm_count() - 1) / sm_count()}));
-  const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, (size_t)occ.fixed) - occ.fixed;
+  const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, occ.fixed + prm) - occ.fixed - prm;
   g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : 1;
-  if ((size_t)g.stages * g.stage + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
-  const size_t smem = (size_t)g.stages * g.stage;
+  if ((size_t)g.stages * g.stage + prm + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
+  const size_t smem = (size_t)g.stages * g.stage + prm;
   if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
-  return launch_pdl(bwd_ring_k<T, VPT, VEC, BIAS>, a.chunks, th, smem, s, a, g) == cudaSuccess;
+  return launch_pdl(bwd_ring_k<T, VPT, VEC, LN>, a.chunks, th, smem, s, a, g) == cudaSuccess;
 }
 
 template <typename T, bool VEC>
@@ -1145,16 +1264,15 @@ bool backward_as(const Bwd& a, cudaStream_t s) {
   const int ys = 4 + (a.per_group ? a.chunks / a.per_group : 0);
   const dim3 join((a.d + 31) / 32, std::min(ys, 65535));
   if (a.d <= kRingCols) {
-    const bool bias = a.out[1] || a.out[3] || a.pb;
+    const bool ln = a.pre == ZL_NORM_LAYER || a.post == ZL_NORM_LAYER;
     note_launch(parts ? 2 : 1);
-    if (nvec <= 512) {
-      const int th = (nvec + 31) / 32 * 32;
-      if (!(bias ? bwd_ring<T, 1, VEC, true>(a, th, s) : bwd_ring<T, 1, VEC, false>(a, th, s))) return false;
+    const int th = bwd_threads(nvec, ln);
+    if (th >= nvec) {
+      if (!(ln ? bwd_ring<T, 1, VEC, true>(a, th, s) : bwd_ring<T, 1, VEC, false>(a, th, s))) return false;
     } else {
-      const int th = (nvec + 63) / 64 * 32;
-      if (!(bias ? bwd_ring<T, 2, VEC, true>(a, th, s) : bwd_ring<T, 2, VEC, false>(a, th, s))) return false;
+      if (!(ln ? bwd_ring<T, 2, VEC, true>(a, th, s) : bwd_ring<T, 2, VEC, false>(a, th, s))) return false;
     }
-    if (parts) launch_pdl(bwd_join_k, join, 256, 0, s, a);
+    if (parts) launch_pdl(bwd_join_k, join, 1024, 0, s, a);
     return true;
   }
   if (a.pre) {
@@ -1164,7 +1282,7 @@ bool backward_as(const Bwd& a, cudaStream_t s) {
   if (sums) {   // before dh, which may overwrite dh_out
     note_launch(2);
     launch_pdl(bwd_cols_k<T, VEC>, dim3(a.chunks, (a.d + 255) / 256), 256, 0, s, a);
-    launch_pdl(bwd_join_k, join, 256, 0, s, a);
+    launch_pdl(bwd_join_k, join, 1024, 0, s, a);
   }
   note_launch(1);
   launch_pdl(bwd_rows_k<T, VEC>, a.N, 256, 0, s, a);
@@ -1195,7 +1313,8 @@ bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 using namespace zl;
 using zl::act8::entry;
 using zl::act8::launched;
-using zl::act8::rows_aligned;
+using zl::act8::kWhole;
+using zl::act8::row_mode;
 
 extern "C" {
 
@@ -1218,8 +1337,8 @@ zl_status zl_op_block_norm(const zl_block_norm* p, const void* h, const void* f,
     a.N = p->N; a.d = p->d; a.D = act8::pitch(p->d); a.post = p->post_norm; a.pre = p->pre_norm; a.gate_rows = p->gate_rows;
     a.eps = p->eps; a.alpha = p->res_scale; a.beta = p->branch_scale; a.fmt = p->fmt;
     a.vec = true;
-    for (const void* t : {h, f, (const void*)h_out, (const void*)n_out}) a.vec &= !t || rows_aligned(t, p->d, p->dtype);
-    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(pre_b) && (!gate || rows_aligned(gate, p->d, ZL_DTYPE_F32));
+    for (const void* t : {h, f, (const void*)h_out, (const void*)n_out}) a.vec &= !t || row_mode(t, p->d, p->d, p->dtype) == kWhole;
+    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(pre_b) && al16(gate);
     if (p->dtype == ZL_DTYPE_BF16) forward<bf16>(a, (cudaStream_t)stream);
     else forward<float>(a, (cudaStream_t)stream);
     return launched("zl_op_block_norm");
@@ -1273,8 +1392,8 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     a.alpha = p->res_scale; a.beta = p->branch_scale; a.fmt = p->fmt; a.accumulate = p->accumulate;
     plan_chunks(*p, a.rows, a.per_group, a.chunks);
     a.vec = true;
-    for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df}) a.vec &= !t || rows_aligned(t, d, p->dtype);
-    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(dgate) && (!gate || rows_aligned(gate, d, ZL_DTYPE_F32));
+    for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df}) a.vec &= !t || row_mode(t, d, d, p->dtype) == kWhole;
+    a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(dgate) && al16(gate);
     const bool done = p->dtype == ZL_DTYPE_BF16 ? backward<bf16>(a, s) : backward<float>(a, s);
     const zl_status st = launched("zl_op_block_norm_bwd");
     return done || st != ZL_OK ? st : act8::fail(ZL_ERR_CUDA, "zl_op_block_norm_bwd: the kernel cannot be launched on this device");
