@@ -34,18 +34,17 @@ struct FastDiv {
   __device__ __forceinline__ uint32_t quot(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
 };
 
-// E of a group from the bits of its largest magnitude (448 = 1.75 2^8, 127 = 1.984375 2^6).
+// E + 127 of a group from the bits of its largest magnitude (448 = 1.75 2^8, 127 = 1.984375 2^6): the exponent, one up
+// where the mantissa is above Q's, which the addition carries into it.
 template <int FMT>
-__device__ __forceinline__ int group_exp(uint32_t amax_bits) {
-  const int ex = (int)(amax_bits >> 23) - 127;
-  const uint32_t man = amax_bits & 0x7FFFFFu;
-  const int e = FMT == ZL_ACT8_E4M3 ? ex - 8 + (man > 0x600000u) : ex - 6 + (man > 0x7E0000u);
-  return max(e, -117);
+__device__ __forceinline__ uint32_t group_byte(uint32_t amax_bits) {
+  const int e = FMT == ZL_ACT8_E4M3 ? (int)((amax_bits + 0x1FFFFFu) >> 23) - 8 : (int)((amax_bits + 0x1FFFFu) >> 23) - 6;
+  return (uint32_t)max(e, 10);
 }
-// 2^k, -126 <= k <= 127.
-__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 // The scale of a group byte.
 __device__ __forceinline__ float group_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+// And its inverse (bytes 10 .. 249).
+__device__ __forceinline__ float group_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
 // max(|a|, |b|, |c|), a NaN if one is among them.
 __device__ __forceinline__ float absmax3(float a, float b, float c) {
@@ -53,56 +52,25 @@ __device__ __forceinline__ float absmax3(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// Bits of the largest magnitude of 8 values that a group counts: finite ones, none above the top; odd: others are among them.
-__device__ __forceinline__ uint32_t amax_bits(const float* x, bool& odd) {
+// Bits of the largest magnitude of 8 values (of a NaN if one is among them).
+__device__ __forceinline__ uint32_t amax_bits(const float* x) {
   float v = absmax3(x[0], x[1], x[2]);
   v = absmax3(v, x[3], x[4]);
   v = absmax3(v, x[5], x[6]);
-  uint32_t m = __float_as_uint(absmax3(v, x[7], x[7]));
-  odd = m > kTopBits;
-  if (odd) {   // hardly ever: a NaN, an infinity or a value beyond the top among them
-    m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
-      m = max(m, u < kInfBits ? min(u, kTopBits) : 0u);
-    }
-  }
-  return m;
+  return __float_as_uint(absmax3(v, x[7], x[7]));
 }
-
-// Four codes of four values, given 2^-E of their group. odd: a NaN, an infinity or a value beyond the top is among them.
-// Integer codes: adding 1.5 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits.
+// Four codes of four numbers. Integer codes: adding 1.5 2^23 rounds to the nearest integer, ties to even, and leaves it in
+// the low bits.
 template <int FMT>
-__device__ __forceinline__ uint32_t encode4(const float* x, float inv, bool odd) {
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = x[i] * inv;
-  if (odd) {
-    const float top = __uint_as_float(kTopBits);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
-      y[i] = u >= kInfBits ? __uint_as_float(0x7FC00000u) : fminf(fmaxf(x[i], -top), top) * inv;
-    }
-  }
-  uint32_t w;
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
   if (FMT == ZL_ACT8_E4M3) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
-    w = __byte_perm(lo, hi, 0x5410);
-  } else {
-    uint32_t b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(y[i] + 12582912.f);
-    w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return __byte_perm(lo, hi, 0x5410);
   }
-  if (odd) {   // one NaN code
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (y[i] != y[i]) w = (w & ~(0xFFu << (8 * i))) | ((FMT == ZL_ACT8_E4M3 ? 0x7Fu : 0x80u) << (8 * i));
-  }
-  return w;
+  const uint32_t x = __float_as_uint(a + 12582912.f), y = __float_as_uint(b + 12582912.f);
+  const uint32_t z = __float_as_uint(c + 12582912.f), w = __float_as_uint(d + 12582912.f);
+  return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
 }
 
 // The four numbers that four codes are (not yet times 2^E). Integer codes: code + 128 as the low mantissa byte of 2^23,
@@ -140,6 +108,7 @@ struct Raw8<bf16> {
   uint4 u;
   __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void get(const void* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void set(void* p) const { *reinterpret_cast<uint4*>(p) = u; }
   __device__ __forceinline__ void pairs(uint64_t* f) const {
     f[0] = bf2_to_f2(u.x); f[1] = bf2_to_f2(u.y); f[2] = bf2_to_f2(u.z); f[3] = bf2_to_f2(u.w);
   }
@@ -156,6 +125,10 @@ struct Raw8<float> {
   __device__ __forceinline__ void get(const void* p) {
     u = reinterpret_cast<const float4*>(p)[0];
     v = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void set(void* p) const {
+    reinterpret_cast<float4*>(p)[0] = u;
+    reinterpret_cast<float4*>(p)[1] = v;
   }
   __device__ __forceinline__ void pairs(uint64_t* f) const { f[0] = f2(u.x, u.y); f[1] = f2(u.z, u.w); f[2] = f2(v.x, v.y); f[3] = f2(v.z, v.w); }
   __device__ __forceinline__ void put(int i, float x) {
@@ -186,6 +159,20 @@ __device__ __forceinline__ Raw8<T> load_raw(const T* p, int c, int d) {
   }
   return r;
 }
+// Rounds pairs to T.
+__device__ __forceinline__ void pack8(const uint64_t* v, Raw8<bf16>& r) {
+  auto two = [](uint64_t p) {
+    const float2 f = uf2(p);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  };
+  r.u = make_uint4(two(v[0]), two(v[1]), two(v[2]), two(v[3]));
+}
+__device__ __forceinline__ void pack8(const uint64_t* v, Raw8<float>& r) {
+  const float2 a = uf2(v[0]), b = uf2(v[1]), c = uf2(v[2]), d = uf2(v[3]);
+  r.u = make_float4(a.x, a.y, b.x, b.y);
+  r.v = make_float4(c.x, c.y, d.x, d.y);
+}
 template <typename T>
 __device__ __forceinline__ void floats(const Raw8<T>& r, float* f) {
   uint64_t p[4];
@@ -195,6 +182,19 @@ __device__ __forceinline__ void floats(const Raw8<T>& r, float* f) {
 template <int MODE, typename T>
 __device__ __forceinline__ void load8(const T* p, int c, int d, float* f) {
   floats(load_raw<MODE>(p, c, d), f);
+}
+template <int MODE, typename T>
+__device__ __forceinline__ void store_raw(T* p, int c, int d, const Raw8<T>& r) {
+  if (MODE == kWhole ? c < d : MODE == kTail && c + 8 <= d) {
+    r.set(p + c);
+    return;
+  }
+  if (MODE == kWhole) return;
+  float f[8];
+  floats(r, f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + i < d) p[c + i] = from_f<T>(f[i]);
 }
 template <int MODE, typename T>
 __device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
@@ -209,18 +209,40 @@ __device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
 }
 
 // Encodes this thread's 8 values as its quarter of a group (the four lanes 4 g .. 4 g + 3 of the warp hold the group,
-// every lane of the warp calls): returns the codes in q and E + 127.
+// every lane of the warp calls): the codes in q, returns E + 127.
 template <int FMT>
 __device__ __forceinline__ uint32_t encode_quarter(const float* x, uint2& q) {
-  bool odd;
-  const uint32_t mine = amax_bits(x, odd);
+  const uint32_t mine = amax_bits(x);
   uint32_t m = max(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const int E = group_exp<FMT>(m);
-  const float inv = pow2(-E);
-  q.x = encode4<FMT>(x, inv, odd);
-  q.y = encode4<FMT>(x + 4, inv, odd);
-  return (uint32_t)(E + 127);
+  if (__any_sync(0xffffffffu, m > kTopBits)) {   // hardly ever: a NaN, an infinity or a value beyond the top in the warp
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+      v = max(v, u < kInfBits ? min(u, kTopBits) : 0u);
+    }
+    v = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    v = max(v, __shfl_xor_sync(0xffffffffu, v, 2));
+    const uint32_t byte = group_byte<FMT>(v);
+    const float inv = group_inverse(byte), top = __uint_as_float(kTopBits);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(x[i], -top), top) * inv;
+    uint32_t w[2] = {encode4<FMT>(y[0], y[1], y[2], y[3]), encode4<FMT>(y[4], y[5], y[6], y[7])};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if ((__float_as_uint(x[i]) & 0x7FFFFFFFu) >= kInfBits)
+        w[i >> 2] = (w[i >> 2] & ~(0xFFu << (8 * (i & 3)))) | ((FMT == ZL_ACT8_E4M3 ? 0x7Fu : 0x80u) << (8 * (i & 3)));
+    }
+    q = make_uint2(w[0], w[1]);
+    return byte;
+  }
+  const uint32_t byte = group_byte<FMT>(m);
+  const float inv = group_inverse(byte);
+  q.x = encode4<FMT>(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  q.y = encode4<FMT>(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+  return byte;
 }
 template <int FMT>
 __device__ __forceinline__ void decode8(uint2 q, uint32_t e, float* x) {

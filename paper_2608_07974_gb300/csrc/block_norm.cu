@@ -33,12 +33,14 @@ struct Fwd {
 
 __device__ __forceinline__ size_t gate_row(int n, int gate_rows) { return gate_rows ? (size_t)(n / gate_rows) : 0; }
 
-__device__ __forceinline__ void put_codes(int fmt, const float* x, uint8_t* q, uint8_t* e, size_t at, bool in) {
+// 8 values at column c of a row of D columns as codes (every lane of the warp calls).
+template <int FMT>
+__device__ __forceinline__ void put_codes(const float* x, uint8_t* q, uint8_t* e, int c, int D) {
   uint2 w;
-  const uint32_t b = fmt == ZL_ACT8_E4M3 ? encode_quarter<ZL_ACT8_E4M3>(x, w) : encode_quarter<ZL_ACT8_INT8>(x, w);
-  if (!in) return;
-  reinterpret_cast<uint2*>(q)[at >> 3] = w;
-  if ((at & 31) == 0) e[at >> 5] = (uint8_t)b;
+  const uint32_t byte = encode_quarter<FMT>(x, w);
+  if (c >= D) return;
+  *reinterpret_cast<uint2*>(q + c) = w;
+  if ((c & 31) == 0) e[c >> 5] = (uint8_t)byte;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -186,8 +188,14 @@ __device__ __forceinline__ float fold(uint64_t v) {
   const float2 f = uf2(v);
   return f.x + f.y;
 }
-// Pairs with 0 in the columns from d on.
+// Pairs with 0 in the columns from d on (VEC: d is a multiple of 8).
+template <bool VEC>
 __device__ __forceinline__ void cut(uint64_t* v, int c, int d) {
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c < d ? v[i] : 0;
+    return;
+  }
   if (c + 8 <= d) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -220,9 +228,9 @@ struct Params {
   }
 };
 
-// VEC: rows start on 16 bytes; they come by bulk copies. KEEP: f or n are written in 8 bits.
-template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
-__global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, const Ring g) {
+// VEC: rows start on 16 bytes; they come by bulk copies. KEEP: the format that f or n are written in, -1: neither is.
+template <typename T, int VPT, bool VEC, bool BIAS, int KEEP>
+__global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80) fwd_ring_k(const Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][2][16];
@@ -331,7 +339,7 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, 
           if (kind == ZL_NORM_LAYER) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = sub2(x[i], mm);
-            cut(x, c, a.d);
+            cut<VEC>(x, c, a.d);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) q2 = fma2(x[i], x[i], q2);
@@ -345,13 +353,12 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, 
         next();
       }
     };
-    if (KEEP && a.fq) {
+    if (KEEP >= 0 && a.fq) {
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
-        const int c = (t + j * nt) * 8;
         float x[8];
         floats(rf[j], x);
-        put_codes(a.fmt, x, a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
+        put_codes<KEEP < 0 ? 0 : KEEP>(x, a.fq + (size_t)row * a.D, a.fe + (size_t)row * (a.D >> 5), (t + j * nt) * 8, a.D);
       }
     }
     stat(a.post, [&](int j, uint64_t* x) { rf[j].pairs(x); }, true);
@@ -374,10 +381,10 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, 
           h[j][i] = fma2(mul2(f[i], rr), pa.a[j][i], mul2(alpha, h[j][i]));
           if (BIAS) h[j][i] = add2(h[j][i], pa.b[j][i]);
         }
-        cut(h[j], c, a.d);
-        float x[8];
-        unpair(h[j], x);
-        store8<mode_of(VEC)>((T*)a.ho + o, c, a.d, x);
+        cut<VEC>(h[j], c, a.d);
+        Raw8<T> out;
+        pack8(h[j], out);
+        store_raw<mode_of(VEC)>((T*)a.ho + o, c, a.d, out);
       }
     }
     stat(a.pre, [&](int j, uint64_t* x) {
@@ -393,24 +400,29 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) fwd_ring_k(const Fwd a, 
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
-      float n[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (a.pre == ZL_NORM_LAYER) h[j][i] = sub2(h[j][i], mm);
         h[j][i] = mul2(mul2(h[j][i], rr), pa.w[j][i]);
         if (BIAS) h[j][i] = add2(h[j][i], pa.v[j][i]);
       }
-      cut(h[j], c, a.d);
-      unpair(h[j], n);
-      store8<mode_of(VEC)>((T*)a.no + o, c, a.d, n);
-      if (KEEP && a.nq) {   // of n as it is stored
-#pragma unroll
-        for (int i = 0; i < 8; ++i) n[i] = to_f(from_f<T>(n[i]));
-        put_codes(a.fmt, n, a.nq, a.ne, (size_t)row * a.D + c, c < a.D);
+      cut<VEC>(h[j], c, a.d);
+      Raw8<T> out;
+      pack8(h[j], out);
+      store_raw<mode_of(VEC)>((T*)a.no + o, c, a.d, out);
+      if (KEEP >= 0 && a.nq) {   // of n as it is stored
+        float n[8];
+        floats(out, n);
+        put_codes<KEEP < 0 ? 0 : KEEP>(n, a.nq + (size_t)row * a.D, a.ne + (size_t)row * (a.D >> 5), c, a.D);
       }
     }
   }
   if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
+}
+
+__device__ __forceinline__ void put_any(int fmt, const float* x, uint8_t* q, uint8_t* e, size_t row, int c, int D) {
+  if (fmt == ZL_ACT8_E4M3) put_codes<ZL_ACT8_E4M3>(x, q + row * D, e + row * (D >> 5), c, D);
+  else put_codes<ZL_ACT8_INT8>(x, q + row * D, e + row * (D >> 5), c, D);
 }
 
 // Rows of any width: a block per row that reads it again for every sum.
@@ -487,7 +499,7 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
     float x[8], w[8];
     if (a.fq) {
       fval(c, x);
-      put_codes(a.fmt, x, a.fq, a.fe, (size_t)row * a.D + c, c < a.D);
+      put_any(a.fmt, x, a.fq, a.fe, (size_t)row, c, a.D);
     }
     hval(c, x);
     store8<mode_of(VEC)>((T*)a.ho + o, c, a.d, x);
@@ -508,7 +520,7 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
     if (a.nq) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = c + i < a.d ? to_f(from_f<T>(x[i])) : 0.f;
-      put_codes(a.fmt, x, a.nq, a.ne, (size_t)row * a.D + c, c < a.D);
+      put_any(a.fmt, x, a.nq, a.ne, (size_t)row, c, a.D);
     }
   }
 }
@@ -535,7 +547,7 @@ constexpr int kRingCols = 8192;   // the widest row of the ring kernels
 // Threads of a block for a row of nvec vectors, one vector a thread or two.
 int ring_threads(int nvec) { return nvec <= 224 ? (nvec + 31) / 32 * 32 : (nvec + 63) / 64 * 32; }
 
-template <typename T, int VPT, bool VEC, bool BIAS, bool KEEP>
+template <typename T, int VPT, bool VEC, bool BIAS, int KEEP>
 bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
   static const Occupancy occ(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>);
   if (!occ.ok) return false;
@@ -554,9 +566,11 @@ bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
 }
 template <typename T, int VPT, bool VEC>
 bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
-  const bool bias = a.pb || a.nb, keep = a.fq || a.nq;
-  return bias ? keep ? fwd_ring<T, VPT, VEC, true, true>(a, th, s) : fwd_ring<T, VPT, VEC, true, false>(a, th, s)
-              : keep ? fwd_ring<T, VPT, VEC, false, true>(a, th, s) : fwd_ring<T, VPT, VEC, false, false>(a, th, s);
+  const bool bias = a.pb || a.nb;
+  if (!a.fq && !a.nq) return bias ? fwd_ring<T, VPT, VEC, true, -1>(a, th, s) : fwd_ring<T, VPT, VEC, false, -1>(a, th, s);
+  if (a.fmt == ZL_ACT8_E4M3)
+    return bias ? fwd_ring<T, VPT, VEC, true, ZL_ACT8_E4M3>(a, th, s) : fwd_ring<T, VPT, VEC, false, ZL_ACT8_E4M3>(a, th, s);
+  return bias ? fwd_ring<T, VPT, VEC, true, ZL_ACT8_INT8>(a, th, s) : fwd_ring<T, VPT, VEC, false, ZL_ACT8_INT8>(a, th, s);
 }
 
 template <typename T, bool VEC>
@@ -884,10 +898,14 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = t; i < (LN ? 256 : 128); i += nt) (&sh[0][0][0])[i] = 0.f;
-  for (int k = 0; k < 4 * g.stages; ++k)   // columns past d, and tensors that are not given, read 0
-    for (int c = ((k & 3) == 0 && a.dn) || ((k & 3) == 1 && a.dho) || ((k & 3) == 2 && a.pre) || ((k & 3) == 3 && !a.fq) ? a.d + t : t;
-         c < ((k & 3) == 3 && a.fq ? 0 : a.D); c += nt)
-      reinterpret_cast<T*>(ring + (k >> 2) * g.stage + (k & 3) * g.pitch)[c] = from_f<T>(0.f);
+  if (a.d != a.D || !a.dho) {   // columns past d, and a tensor that is not given, read 0
+    for (int k = 0; k < 4 * g.stages; ++k) {
+      const int which = k & 3;
+      if (which == 3 && a.fq) continue;
+      for (int c = (which == 1 && !a.dho ? 0 : a.d) + t; c < a.D; c += nt)
+        reinterpret_cast<T*>(ring + (k >> 2) * g.stage + which * g.pitch)[c] = from_f<T>(0.f);
+    }
+  }
   __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -1027,7 +1045,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         row8<VEC>(a.pw, c, a.d, 1.f, p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) A[i] = mul2(mul2(A[i], f2(a.beta, a.beta)), p[i]);
-        cut(A, c, a.d);
+        cut<VEC>(A, c, a.d);
         if (c < a.D) put_pairs(prm + a.D, c, a.D, A);
       }
       new_gate = false;
@@ -1123,7 +1141,6 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         const int c = (t + j * nt) * 8;
         if (c >= a.d) continue;
         uint64_t v[4], A[4];
-        float y[8];
         get_pairs(prm + a.D, c, a.D, A);
         if (a.pre) {
 #pragma unroll
@@ -1131,7 +1148,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
             G[j][i] = fma2(xh[j][i], c2, G[j][i]);
             if (LN) G[j][i] = add2(G[j][i], c1);
           }
-          cut(G[j], c, a.d);
+          cut<VEC>(G[j], c, a.d);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1140,8 +1157,9 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
           v[i] = mul2(G[j][i], alpha);
         }
         if (a.dh) {
-          unpair(v, y);
-          store8<mode_of(VEC)>((T*)a.dh + o, c, a.d, y);
+          Raw8<T> out;
+          pack8(v, out);
+          store_raw<mode_of(VEC)>((T*)a.dh + o, c, a.d, out);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1149,8 +1167,9 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
           if (LN) v[i] = add2(v[i], d1);
           v[i] = mul2(v[i], prr);
         }
-        unpair(v, y);
-        store8<mode_of(VEC)>((T*)a.df + o, c, a.d, y);
+        Raw8<T> out;
+        pack8(v, out);
+        store_raw<mode_of(VEC)>((T*)a.df + o, c, a.d, out);
       }
     }
     if (--gate_left == 0 || k + 1 == rows) {
@@ -1230,7 +1249,7 @@ int bwd_threads(int nvec, bool ln) { return ln && nvec <= 512 ? (nvec + 31) / 32
 // (written once and read once, 8 bytes a column and sum) weigh as much as the rows.
 int ring_rows(int N, int d, bool ln) {
   const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
-  return std::max(4, (N + 152 * per_sm - 1) / (152 * per_sm));
+  return std::max(1, (N + 152 * per_sm - 1) / (152 * per_sm));
 }
 void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
   plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d, p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER) : kAnyRows, rows, per_group, chunks);
