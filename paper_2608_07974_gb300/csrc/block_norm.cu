@@ -602,15 +602,19 @@ struct Bwd {
   const void *dn, *dho;
   void *dh, *df;
   float* s12;                // [2, N]: mean(u), mean(u xh)
-  float* part;               // [chunks, 5, d] partial sums: dw_pre, db_pre, dw_post, db_post, dgate
-  float* out[5];
+  float* part;               // [chunks, slots, D] partial sums, see kDw .. (NULL: no gradient of a parameter is asked for)
+  float *dpw, *dpb, *dgate, *dnw, *dnb;
   int N, d, D;
   int post, pre, gate_rows;
   float alpha, beta;
   int fmt, accumulate;
   bool vec, wvec;
   int rows, per_group, chunks;   // the chunks of rows that partial sums are of
+  int slots;
 };
+// Slots of a chunk's partial sums: sum dn xh, s, and with a LayerNorm sum dn, z. s = sum G fh and z = sum G where a chunk lies
+// in one gate group (per_group > 0), else both already times beta gate.
+enum { kDw = 0, kS = 1, kDb = 2, kZ = 3 };
 
 // Rows [r0, r1) of chunk k. Gate groups longer than a chunk are cut into per_group chunks each; shorter ones lie whole in
 // a chunk (per_group 0), which then knows their dgate alone.
@@ -709,16 +713,15 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (blockIdx.y * 32 + tx) * 8;
   int r0, r1;
   chunk_rows(blockIdx.x, a.N, a.gate_rows ? a.gate_rows : a.N, a.rows, a.per_group, r0, r1);
-  float acc[5][8];
+  // sums dn xh, G fh, dn, G; and the last two of the post norm times beta gate, of gate groups within the chunk
+  float acc[4][8], post[2][8];
 #pragma unroll
-  for (int k = 0; k < 5; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[k][i] = 0.f;
-  // the sum over the row lanes of acc[k] at this thread's column blockIdx.y * 256 + threadIdx.x
-  auto join = [&](int k) {
+  for (int i = 0; i < 8; ++i) acc[0][i] = acc[1][i] = acc[2][i] = acc[3][i] = post[0][i] = post[1][i] = 0.f;
+  // the sum over the row lanes of v at this thread's column blockIdx.y * 256 + threadIdx.x
+  auto join = [&](const float* v) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sh[ty][tx * 8 + i] = acc[k][i];
+    for (int i = 0; i < 8; ++i) sh[ty][tx * 8 + i] = v[i];
     __syncthreads();
     float s = 0.f;
 #pragma unroll
@@ -737,41 +740,43 @@ __global__ void __launch_bounds__(256) bwd_cols_k(const Bwd a) {
         load8<mode_of(VEC)>((const T*)a.ho + (size_t)n * a.d, c, a.d, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          acc[0][i] += w[i] * ((x[i] - m) * r);
-          acc[1][i] += w[i];
+          acc[kDw][i] += w[i] * ((x[i] - m) * r);
+          acc[kDb][i] += w[i];
         }
       }
       f8<T, VEC>(a, n, c, x);
       const float pm = a.stats[n], pr = a.stats[(size_t)a.N + n];
-      float gt[8], b[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { gt[i] = 1.f; w[i] = 1.f; b[i] = 0.f; }
-      if (a.gate) load8<mode_of(VEC)>(a.gate + gate_row(n, a.gate_rows) * a.d, c, a.d, gt);
-      if (a.pw) load8<mode_of(VEC)>(a.pw, c, a.d, w);
-      if (a.pb) load8<mode_of(VEC)>(a.pb, c, a.d, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float fh = a.post ? (x[i] - pm) * pr : x[i], q = a.beta * G[i];
-        acc[2][i] += gt[i] * q * fh;
-        acc[3][i] += gt[i] * q;
-        acc[4][i] += q * (fh * w[i] + b[i]);
+        acc[kS][i] += G[i] * (a.post ? (x[i] - pm) * pr : x[i]);
+        acc[kZ][i] += G[i];
       }
     }
-    if (a.out[4] && !a.per_group) {
-      const float s = join(4);
-      if (col < a.d) {
-        float* p = a.out[4] + gate_row(g0, a.gate_rows) * a.d + col;
-        *p = a.accumulate ? *p + s : s;
-      }
+    if (a.per_group) continue;
+    float gt[8];
+    const size_t grow = gate_row(g0, a.gate_rows);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[4][i] = 0.f;
+    for (int i = 0; i < 8; ++i) gt[i] = 1.f;
+    if (a.gate) load8<mode_of(VEC)>(a.gate + grow * a.d, c, a.d, gt);
+    const float sv = join(acc[kS]), zv = join(acc[kZ]);
+    if (a.dgate && col < a.d) {
+      const float v = a.beta * ((a.pw ? a.pw[col] : 1.f) * sv + (a.pb ? a.pb[col] : 0.f) * zv);
+      float* p = a.dgate + grow * a.d + col;
+      *p = a.accumulate ? *p + v : v;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      post[0][i] += a.beta * gt[i] * acc[kS][i];
+      post[1][i] += a.beta * gt[i] * acc[kZ][i];
+      acc[kS][i] = acc[kZ][i] = 0.f;
     }
   }
+  float* const part = a.part + (size_t)blockIdx.x * a.slots * a.D;
 #pragma unroll
-  for (int k = 0; k < 5; ++k) {
-    if (!a.out[k] || (k == 4 && !a.per_group)) continue;
-    const float s = join(k);
-    if (col < a.d) a.part[((size_t)blockIdx.x * 5 + k) * a.d + col] = s;
+  for (int k = 0; k < 4; ++k) {
+    if (k >= a.slots) continue;
+    const float s = join(k == kS && !a.per_group ? post[0] : k == kZ && !a.per_group ? post[1] : acc[k]);
+    if (col < a.D) part[k * (size_t)a.D + col] = col < a.d ? s : 0.f;
   }
 }
 
@@ -939,7 +944,8 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   };
   if (VEC && t == 0)
     for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
-  // w_pre and A = beta gate w_post of the block's columns, behind the ring (every thread reads what it wrote)
+  // w_pre and A = beta gate w_post of the block's columns, behind the ring, and where gate groups end within the chunk the
+  // post norm's sums over them (every thread reads what it wrote)
   float* const prm = reinterpret_cast<float*>(ring + g.stages * g.stage);
   uint64_t s[VPT][4], z[LN ? VPT : 1][4];                // sums G fh, G of the gate row at hand
   uint64_t dw[VPT][4], db[LN ? VPT : 1][4];              // sums dn xh, dn
@@ -948,32 +954,34 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
     const int c = (t + j * nt) * 8;
     uint64_t w[4];
     row8<VEC>(a.nw, c, a.d, 1.f, w);
-    if (c < a.D) put_pairs(prm, c, a.D, w);
+    if (c < a.D) {
+      put_pairs(prm, c, a.D, w);
+      const uint64_t none[4] = {0, 0, 0, 0};
+      if (!a.per_group) put_pairs(prm + 2 * a.D, c, a.D, none);
+      if (LN && !a.per_group) put_pairs(prm + 3 * a.D, c, a.D, none);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       s[j][i] = dw[j][i] = 0;
       if (LN) z[j][i] = db[j][i] = 0;
     }
   }
-  // the sums over a gate row's rows [.., n] go to where their gradients are formed: dgate itself where the chunk knows all of
-  // its rows, else the chunk's part; and the post norm's sums, of gate rows one after another, to the chunk's part
-  float* const part = a.part + (size_t)blockIdx.x * 5 * a.d;
-  bool fresh = true;
+  float* const part = a.part ? a.part + (size_t)blockIdx.x * a.slots * a.D : nullptr;
+  // gate groups within the chunk: at the end of one its dgate, and its part of the post norm's gradients
   auto flush = [&](int n) {
     const float* gr = a.gate ? a.gate + gate_row(n, a.gate_rows) * a.d : nullptr;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
-      if (c >= a.d) continue;
+      if (c >= a.D) continue;
       uint64_t p[4], v[4], gt[4], pb[4];
       float x[8], y[8];
       row8<VEC>(a.pw, c, a.d, 1.f, p);   // every load first
       row8<VEC>(gr, c, a.d, 1.f, gt);
       if (LN) row8<VEC>(a.pb, c, a.d, 0.f, pb);
-      if (a.out[4]) {
-        float* q = a.per_group ? part + 4 * (size_t)a.d : a.out[4] + gate_row(n, a.gate_rows) * a.d;
-        const bool add = !a.per_group && a.accumulate;
-        if (add) load8<mode_of(VEC)>((const float*)q, c, a.d, y);
+      if (a.dgate) {
+        float* q = a.dgate + gate_row(n, a.gate_rows) * a.d;
+        if (a.accumulate) load8<mode_of(VEC)>((const float*)q, c, a.d, y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[i] = mul2(p[i], s[j][i]);
@@ -981,7 +989,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
           v[i] = mul2(v[i], f2(a.beta, a.beta));
         }
         unpair(v, x);
-        if (add) {
+        if (a.accumulate) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] += y[i];
         }
@@ -989,17 +997,11 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       }
 #pragma unroll
       for (int k = 0; k < (LN ? 2 : 1); ++k) {
-        if (!a.out[2 + k]) continue;
-        float* q = part + (2 + k) * (size_t)a.d;
+        float* q = prm + (2 + k) * a.D;
+        get_pairs(q, c, a.D, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = mul2(mul2(gt[i], f2(a.beta, a.beta)), k ? z[j][i] : s[j][i]);
-        unpair(v, x);
-        if (!fresh) {
-          load8<mode_of(VEC)>((const float*)q, c, a.d, y);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] += y[i];
-        }
-        store8<mode_of(VEC)>(q, c, a.d, x);
+        for (int i = 0; i < 4; ++i) v[i] = fma2(mul2(gt[i], f2(a.beta, a.beta)), k ? z[j][i] : s[j][i], v[i]);
+        put_pairs(q, c, a.D, v);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -1007,7 +1009,6 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         if (LN) z[j][i] = 0;
       }
     }
-    fresh = false;
   };
   int turn = 0;
   const float inv_d = 1.f / a.d;
@@ -1028,7 +1029,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   };
   if (rows > 0) ahead(r0);
   bool new_gate = true;
-  int gate_left = a.per_group ? rows : gate_rows - r0 % gate_rows;   // rows of the gate row at hand to come, this one among them
+  int gate_left = min(gate_rows, rows);   // rows of the gate group at hand to come, this one among them
   Turn at;
   int k = 0;
   for (; k < rows; ++k, at.next(g.stages)) {
@@ -1172,67 +1173,142 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         store_raw<mode_of(VEC)>((T*)a.df + o, c, a.d, out);
       }
     }
-    if (--gate_left == 0 || k + 1 == rows) {
-      flush(n);
+    if (--gate_left == 0 && !a.per_group) {
+      if (part) flush(n);
       new_gate = true;
-      gate_left = gate_rows;
+      gate_left = min(gate_rows, rows - 1 - k);
     }
   }
-  if (k == rows) {
+  if (k == rows && part) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
-      if (c >= a.d) continue;
-      float x[8];
-      unpair(dw[j], x);
-      if (a.out[0]) store8<mode_of(VEC)>(part, c, a.d, x);
-      if (LN && a.out[1]) {
-        unpair(db[j], x);
-        store8<mode_of(VEC)>(part + a.d, c, a.d, x);
-      }
-      if (rows == 0) {   // a chunk past its gate group's end
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        for (int i = 2; i < 5; ++i)
-          if (a.out[i]) store8<mode_of(VEC)>(part + i * (size_t)a.d, c, a.d, x);
+      if (c >= a.D) continue;
+      auto put = [&](int slot, const uint64_t* v) {
+        float x[8];
+        unpair(v, x);
+        Vec8<float>::store(part + slot * (size_t)a.D + c, x);
+      };
+      put(kDw, dw[j]);
+      if (!a.per_group) get_pairs(prm + 2 * a.D, c, a.D, s[j]);
+      put(kS, s[j]);
+      if (LN) {
+        if (!a.per_group) get_pairs(prm + 3 * a.D, c, a.D, z[j]);
+        put(kDb, db[j]);
+        put(kZ, z[j]);
       }
     }
   }
   if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
 }
 
-// The chunks' partial sums: a block takes 32 columns of one gradient (blockIdx.y 0..3 the parameters, 4 + g gate row g), 32
-// lanes of rows each adding every 32nd chunk, the lanes' sums then in order.
-__global__ void __launch_bounds__(1024) bwd_join_k(const Bwd a) {
+// The gradients from the chunks' partial sums: a block takes 32 columns (8 lanes of four), 32 lanes of chunks each adding every
+// 32nd one, eight of them under way together, then the lanes' sums in a fixed tree. blockIdx.y 0: the post norm's gradients,
+// and dgate where there is one gate group (or none); 1, 2: the pre norm's; 3 + g: dgate of group g where there are several.
+// Bound by latency (launch, one round of loads from L2, stores: 5 us at 128 x 4096): one wave of small blocks, what the last
+// step reads besides is read first.
+template <bool LN>
+__global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float sh[32][33];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
-  for (int y = blockIdx.y; y < 4 + (a.per_group ? a.chunks / a.per_group : 0); y += gridDim.y) {
-    const int k = min(y, 4);
-    if (!a.out[k]) continue;
-    const int b0 = k < 4 ? 0 : (y - 4) * a.per_group, b1 = k < 4 ? a.chunks : b0 + a.per_group;
-    float s = 0.f;
-    if (c < a.d) {
-#pragma unroll 8
-      for (int b = b0 + ty; b < b1; b += 32) s += a.part[((size_t)b * 5 + k) * a.d + c];
+  __shared__ float4 sh[LN ? 2 : 1][32][9];
+  constexpr int U = 8;
+  const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, c = blockIdx.x * 32 + tx * 4;
+  const int col = blockIdx.x * 32 + ty;   // of the last step, eight threads to a column
+  const int groups = a.per_group ? a.chunks / a.per_group : 1;
+  const bool gvec = a.wvec && a.d % 4 == 0 && c < a.d, one = a.per_group && groups == 1;
+  float pw = 1.f, pb = 0.f, gt = 1.f;
+  if (tx == 0 && col < a.d) {
+    if (a.pw) pw = a.pw[col];
+    if (LN && a.pb) pb = a.pb[col];
+    if (one && a.gate) gt = a.gate[col];
+  }
+  for (int y = blockIdx.y; y < 3 + (a.dgate && groups > 1 ? groups : 0); y += gridDim.y) {
+    const bool two = LN && (y == 0 || y > 2);
+    if (y == 0 ? !a.dpw && !a.dpb && !(a.dgate && one) : y == 1 ? !a.dnw : y == 2 && !a.dnb) continue;
+    const int b0 = y > 2 ? (y - 3) * a.per_group : 0, b1 = y > 2 ? b0 + a.per_group : a.chunks;
+    const int slot = y == 1 ? kDw : y == 2 ? kDb : kS;
+    const bool weigh = y == 0 && a.per_group && groups > 1 && a.gate;   // every chunk's sums times its gate row
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f), z = s;
+    for (int b = b0 + ty; b < b1; b += 32 * U) {
+      float4 v[U], w[LN ? U : 1];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (LN) w[u] = v[u];
+        if (b + 32 * u < b1) {
+          const float* p = a.part + ((size_t)(b + 32 * u) * a.slots + slot) * a.D + c;
+          v[u] = *reinterpret_cast<const float4*>(p);
+          if (two) w[u] = *reinterpret_cast<const float4*>(p + (kZ - kS) * (size_t)a.D);
+        }
+      }
+      if (weigh) {
+        float4 g[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float* gr = a.gate + (size_t)((b + 32 * u) / a.per_group) * a.d + c;
+          g[u] = make_float4(1.f, 1.f, 1.f, 1.f);
+          if (b + 32 * u >= b1) continue;
+          if (gvec) g[u] = *reinterpret_cast<const float4*>(gr);
+          else {
+            if (c < a.d) g[u].x = gr[0];
+            if (c + 1 < a.d) g[u].y = gr[1];
+            if (c + 2 < a.d) g[u].z = gr[2];
+            if (c + 3 < a.d) g[u].w = gr[3];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          v[u].x *= g[u].x; v[u].y *= g[u].y; v[u].z *= g[u].z; v[u].w *= g[u].w;
+          if (LN) { w[u].x *= g[u].x; w[u].y *= g[u].y; w[u].z *= g[u].z; w[u].w *= g[u].w; }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w;
+        if (LN) { z.x += w[u].x; z.y += w[u].y; z.z += w[u].z; z.w += w[u].w; }
+      }
     }
     __syncthreads();
-    sh[ty][tx] = s;
+    sh[0][ty][tx] = s;
+    if (LN) sh[LN ? 1 : 0][ty][tx] = z;
     __syncthreads();
-    s = warp_sum(sh[tx][ty]);   // column blockIdx.x * 32 + ty
-    const int col = blockIdx.x * 32 + ty;
-    if (tx == 0 && col < a.d) {
-      float* p = a.out[k] + (k < 4 ? 0 : (size_t)(y - 4) * a.d) + col;
-      *p = a.accumulate ? *p + s : s;
+    // column ty of the block's 32: thread tx of eight takes lanes 4 tx .. 4 tx + 3
+    float sv = 0.f, zv = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sv += reinterpret_cast<const float*>(&sh[0][4 * tx + i][0])[ty];
+      if (LN) zv += reinterpret_cast<const float*>(&sh[LN ? 1 : 0][4 * tx + i][0])[ty];
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      sv += __shfl_xor_sync(0xffffffffu, sv, o);
+      if (LN) zv += __shfl_xor_sync(0xffffffffu, zv, o);
+    }
+    if (tx != 0 || col >= a.d) continue;
+    auto put = [&](float* o, float v) {
+      if (o) o[col] = a.accumulate ? o[col] + v : v;
+    };
+    if (y == 1) put(a.dnw, sv);
+    else if (y == 2) put(a.dnb, sv);
+    else {
+      const float dg = a.beta * (pw * sv + pb * zv);
+      if (y > 2) put(a.dgate + (size_t)(y - 3) * a.d, dg);
+      else {
+        if (one) put(a.dgate, dg);
+        const float f = a.per_group ? a.beta * gt : 1.f;
+        put(a.dpw, f * sv);
+        put(a.dpb, f * zv);
+      }
     }
   }
 }
 
-// Chunks of rows for the partial sums, `rows` long where gate groups are longer, else of whole groups.
+// Chunks of rows for the partial sums, of about `target` rows: parts of gate groups that are as long or longer, else whole
+// groups together.
 void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, int& chunks) {
   const int gr = gate_rows && gate_rows < N ? gate_rows : std::max(N, 1);
-  if (gr > target) {
+  if (gr >= target || gr >= N) {
     per_group = (gr + target - 1) / target;
     rows = (gr + per_group - 1) / per_group;
     chunks = (N + gr - 1) / gr * per_group;
@@ -1248,7 +1324,7 @@ int bwd_threads(int nvec, bool ln) { return ln && nvec <= 512 ? (nvec + 31) / 32
 // Rows of a chunk of bwd_ring_k: enough chunks for the blocks that fit on 152 SMs, but not so short that their partial sums
 // (written once and read once, 8 bytes a column and sum) weigh as much as the rows.
 int ring_rows(int N, int d, bool ln) {
-  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
+  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(4, 512 / th));
   return std::max(1, (N + 152 * per_sm - 1) / (152 * per_sm));
 }
 void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
@@ -1260,7 +1336,7 @@ bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
   static const Occupancy occ(bwd_ring_k<T, VPT, VEC, LN>);
   if (!occ.ok) return false;
   Ring g = {};
-  const size_t prm = (size_t)a.D * 8;   // the parameters behind the ring
+  const size_t prm = (size_t)a.D * 4 * (2 + (a.per_group ? 0 : LN ? 2 : 1));   // behind the ring
   g.pitch = (uint32_t)a.D * sizeof(T);
   g.stage = 3 * g.pitch + (a.fq ? (uint32_t)a.D : g.pitch);
   const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), (a.chunks + sm_count() - 1) / sm_count()}));
@@ -1275,33 +1351,29 @@ bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
 template <typename T, bool VEC>
 bool backward_as(const Bwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
-  bool sums = false, parts = false;
-  for (int k = 0; k < 5; ++k) {
-    sums |= a.out[k] != nullptr;
-    parts |= a.out[k] && (k < 4 || a.per_group);
-  }
-  const int ys = 4 + (a.per_group ? a.chunks / a.per_group : 0);
-  const dim3 join((a.d + 31) / 32, std::min(ys, 65535));
+  const bool ln = a.slots > 2;
+  const int groups = a.per_group ? a.chunks / a.per_group : 1;
+  const dim3 join((a.D + 31) / 32, 3 + (a.dgate && groups > 1 ? std::min(groups, 60000) : 0));
+  const bool sums = a.dpw || a.dpb || a.dnw || a.dnb || (a.dgate && a.per_group);   // (dgate of short groups is done by then)
   if (a.d <= kRingCols) {
-    const bool ln = a.pre == ZL_NORM_LAYER || a.post == ZL_NORM_LAYER;
-    note_launch(parts ? 2 : 1);
+    note_launch(sums ? 2 : 1);
     const int th = bwd_threads(nvec, ln);
     if (th >= nvec) {
       if (!(ln ? bwd_ring<T, 1, VEC, true>(a, th, s) : bwd_ring<T, 1, VEC, false>(a, th, s))) return false;
     } else {
       if (!(ln ? bwd_ring<T, 2, VEC, true>(a, th, s) : bwd_ring<T, 2, VEC, false>(a, th, s))) return false;
     }
-    if (parts) launch_pdl(bwd_join_k, join, 1024, 0, s, a);
+    if (sums) launch_pdl(ln ? bwd_join_k<true> : bwd_join_k<false>, join, 256, 0, s, a);
     return true;
   }
   if (a.pre) {
     note_launch(1);
     launch_pdl(bwd_sums_k<T, VEC>, a.N, 256, 0, s, a);
   }
-  if (sums) {   // before dh, which may overwrite dh_out
+  if (sums || a.dgate) {   // before dh, which may overwrite dh_out
     note_launch(2);
-    launch_pdl(bwd_cols_k<T, VEC>, dim3(a.chunks, (a.d + 255) / 256), 256, 0, s, a);
-    launch_pdl(bwd_join_k, join, 1024, 0, s, a);
+    launch_pdl(bwd_cols_k<T, VEC>, dim3(a.chunks, (a.D + 255) / 256), 256, 0, s, a);
+    launch_pdl(ln ? bwd_join_k<true> : bwd_join_k<false>, join, 256, 0, s, a);
   }
   note_launch(1);
   launch_pdl(bwd_rows_k<T, VEC>, a.N, 256, 0, s, a);
@@ -1312,6 +1384,7 @@ bool backward(const Bwd& a, cudaStream_t s) {
   return a.vec && a.wvec ? backward_as<T, true>(a, s) : backward_as<T, false>(a, s);
 }
 
+int part_slots(const zl_block_norm& p) { return p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER ? 4 : 2; }
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 bool dims_ok(const zl_block_norm* p) {
@@ -1369,7 +1442,7 @@ zl_status zl_op_block_norm_bwd_bytes(const zl_block_norm* p, size_t* bytes) {
     if (!dims_ok(p) || !bytes) return act8::fail(ZL_ERR_ARG, kDimsMsg);
     int rows, per_group, chunks;
     plan_chunks(*p, rows, per_group, chunks);
-    *bytes = p->N ? up256((size_t)p->N * 8) + up256((size_t)chunks * 5 * p->d * 4) : 0;
+    *bytes = p->N ? up256((size_t)p->N * 8) + up256((size_t)chunks * part_slots(*p) * act8::pitch(p->d) * 4) : 0;
     return ZL_OK;
   });
 }
@@ -1404,8 +1477,9 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     a.ho = h_out; a.f = f; a.fq = f_q; a.fe = f_e; a.pw = post_w; a.pb = post_b; a.gate = gate; a.nw = pre_w; a.stats = stats;
     a.dn = dn; a.dho = dh_out; a.dh = dh; a.df = df;
     a.s12 = (float*)ws;
-    a.part = (float*)((char*)ws + up256((size_t)p->N * 8));
-    a.out[0] = dpre_w; a.out[1] = dpre_b; a.out[2] = dpost_w; a.out[3] = dpost_b; a.out[4] = dgate;
+    if (dpre_w || dpre_b || dpost_w || dpost_b || dgate) a.part = (float*)((char*)ws + up256((size_t)p->N * 8));
+    a.dnw = dpre_w; a.dnb = dpre_b; a.dpw = dpost_w; a.dpb = dpost_b; a.dgate = dgate;
+    a.slots = part_slots(*p);
     a.N = p->N; a.d = p->d; a.D = act8::pitch(p->d); a.post = p->post_norm; a.pre = p->pre_norm;
     a.gate_rows = p->gate_rows < p->N ? p->gate_rows : 0;   // one group holds every row
     a.alpha = p->res_scale; a.beta = p->branch_scale; a.fmt = p->fmt; a.accumulate = p->accumulate;
