@@ -368,63 +368,87 @@ def zl_op_qkv_rope(dtype: int, M: int, N: int, K: int, A, B, Cm, cs, S: int, hd:
                                S, hd, rot_cols, stream))
 
 
-def _operands(dtype: int, act, f32=(), codes=()) -> List[Optional[int]]:
-    """Checks the tensors of a call and gives their pointers in order. act, f32, codes: (tensor, elements, name) of the
-    compute dtype, fp32 and uint8; all dense (given with a row stride: (tensor, elements, name, rows, columns)) and on
-    one device, the current one."""
-    import torch
-    at = torch.bfloat16 if dtype == ZL_DTYPE_BF16 else torch.float32
-    cur, out = None, []
-    for group, want in ((act, at), (f32, torch.float32), (codes, torch.uint8)):
-        for t, n, name, *strided in group:
-            if t is None or isinstance(t, int):
-                out.append(t)
-                continue
-            if t.dtype != want:
-                raise TypeError(f"{name}: dtype {t.dtype}, expected {want}")
-            if cur is None:
-                cur = torch.cuda.current_device() if t.is_cuda else -1
-            if not t.is_cuda or t.get_device() != cur:
-                raise ZLError(ZL_ERR_ARG, f"{name}: on {t.device}, expected the current CUDA device")
-            if strided:   # rows of `columns` values, n apart
-                rows, cols = strided
-                if t.dim() != 2 or t.size(0) < rows or t.size(1) < cols or (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != n):
-                    raise ZLError(ZL_ERR_ARG, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, the call takes {rows} rows of {cols}, {n} apart")
-            elif not t.is_contiguous():
-                raise ZLError(ZL_ERR_ARG, f"{name}: not contiguous")
-            elif t.numel() < n:
-                raise ZLError(ZL_ERR_ARG, f"{name}: {t.numel()} elements, the call reads or writes {n}")
-            out.append(t.data_ptr())
-    return out
+# Tensors of the zl_op_act8_* and zl_op_block_norm* calls: checked (type, device, layout, size) and passed as pointers. Small
+# calls are bound by the host, so the check of a good tensor is one short expression; _refuse() then says what is wrong.
+_types = None   # (torch, fp32, bf16, uint8)
 
 
-def _codes(q, e, rows: int, d: int, what: str = ""):
-    g = (d + 31) // 32
-    return (q, rows * g * 32, what + "q"), (e, rows * g, what + "e")
+def _torch():
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch, torch.float32, torch.bfloat16, torch.uint8)
+    return _types
+
+
+def _here(torch) -> int:
+    """The current CUDA device (-2 without one: no tensor is on it)."""
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):
+        return -2
+
+
+def _refuse(t, want, n: int, cur: int, name: str):
+    if t.dtype != want:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {want}")
+    if t.get_device() != cur:
+        raise ZLError(ZL_ERR_ARG, f"{name}: on {t.device}, expected the current CUDA device")
+    if not t.is_contiguous():
+        raise ZLError(ZL_ERR_ARG, f"{name}: not contiguous")
+    raise ZLError(ZL_ERR_ARG, f"{name}: {t.numel()} elements, the call reads or writes {n}")
+
+
+def _ptr(t, want, n: int, cur: int, name: str):
+    """Pointer of a dense tensor of at least n elements on device cur (None and addresses as they are)."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is want and t.get_device() == cur and t.is_contiguous() and t.numel() >= n:
+        return t.data_ptr()
+    return _refuse(t, want, n, cur, name)
+
+
+def _rows_ptr(t, want, rows: int, cols: int, ld: int, cur: int, name: str):
+    """Pointer of a 2-D tensor with at least rows x cols elements, its rows ld apart."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not want or t.get_device() != cur:
+        return _refuse(t, want, 0, cur, name)
+    if t.dim() != 2 or t.size(0) < rows or t.size(1) < cols or (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld):
+        raise ZLError(ZL_ERR_ARG, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, the call takes {rows} rows of {cols}, {ld} apart")
+    return t.data_ptr()
 
 
 def zl_op_act8_store(dtype: int, fmt: int, x, N: int, d: int, ldx: int, q, e, stream: int = 0) -> None:
     """x: 2-D, rows of d values ldx apart."""
-    px, pq, pe = _operands(dtype, [(x, ldx, "x", N, d)], codes=_codes(q, e, N, d))
-    _check(_lib.zl_op_act8_store(dtype, fmt, px, N, d, ldx, pq, pe, stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, g = _here(torch), (d + 31) // 32
+    _check(_lib.zl_op_act8_store(dtype, fmt, _rows_ptr(x, bf16 if dtype == ZL_DTYPE_BF16 else f32, N, d, ldx, cur, "x"), N, d, ldx,
+                                 _ptr(q, u8, N * g * 32, cur, "q"), _ptr(e, u8, N * g, cur, "e"), stream))
 
 
 def zl_op_act8_load(dtype: int, fmt: int, q, e, N: int, d: int, ldx: int, x, stream: int = 0) -> None:
-    px, pq, pe = _operands(dtype, [(x, ldx, "x", N, d)], codes=_codes(q, e, N, d))
-    _check(_lib.zl_op_act8_load(dtype, fmt, pq, pe, N, d, ldx, px, stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, g = _here(torch), (d + 31) // 32
+    _check(_lib.zl_op_act8_load(dtype, fmt, _ptr(q, u8, N * g * 32, cur, "q"), _ptr(e, u8, N * g, cur, "e"), N, d, ldx,
+                                _rows_ptr(x, bf16 if dtype == ZL_DTYPE_BF16 else f32, N, d, ldx, cur, "x"), stream))
 
 
 def zl_op_act8_act(dtype: int, act: int, fmt: int, x, N: int, f: int, y, q, e, stream: int = 0) -> None:
-    w = 2 if act == ZL_ACT_SWIGLU else 1
-    px, py, pq, pe = _operands(dtype, [(x, w * N * f, "x"), (y, N * f, "y")], codes=_codes(q, e, w * N, f))
-    _check(_lib.zl_op_act8_act(dtype, act, fmt, px, N, f, py, pq, pe, stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, at = _here(torch), bf16 if dtype == ZL_DTYPE_BF16 else f32
+    rows, g = 2 * N if act == ZL_ACT_SWIGLU else N, (f + 31) // 32
+    _check(_lib.zl_op_act8_act(dtype, act, fmt, _ptr(x, at, rows * f, cur, "x"), N, f, _ptr(y, at, N * f, cur, "y"),
+                               _ptr(q, u8, rows * g * 32, cur, "q"), _ptr(e, u8, rows * g, cur, "e"), stream))
 
 
 def zl_op_act8_act_bwd(dtype: int, act: int, fmt: int, q, e, dy, N: int, f: int, dx, y=None, stream: int = 0) -> None:
-    w = 2 if act == ZL_ACT_SWIGLU else 1
-    pdy, pdx, py, pq, pe = _operands(dtype, [(dy, N * f, "dy"), (dx, w * N * f, "dx"), (y, N * f, "y")],
-                                     codes=_codes(q, e, w * N, f))
-    _check(_lib.zl_op_act8_act_bwd(dtype, act, fmt, pq, pe, pdy, N, f, pdx, py, stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, at = _here(torch), bf16 if dtype == ZL_DTYPE_BF16 else f32
+    rows, g = 2 * N if act == ZL_ACT_SWIGLU else N, (f + 31) // 32
+    _check(_lib.zl_op_act8_act_bwd(dtype, act, fmt, _ptr(q, u8, rows * g * 32, cur, "q"), _ptr(e, u8, rows * g, cur, "e"),
+                                   _ptr(dy, at, N * f, cur, "dy"), N, f, _ptr(dx, at, rows * f, cur, "dx"),
+                                   _ptr(y, at, N * f, cur, "y"), stream))
 
 
 def zl_op_act8_dw_bytes(dtype: int, M: int, N: int, K: int) -> int:
@@ -435,23 +459,24 @@ def zl_op_act8_dw_bytes(dtype: int, M: int, N: int, K: int) -> int:
 
 def zl_op_act8_dw(dtype: int, fmt: int, M: int, N: int, K: int, A, q, e, Cm, accumulate: int, ws, stream: int = 0) -> None:
     """ws: a uint8 tensor of at least zl_op_act8_dw_bytes(dtype, M, N, K) elements."""
-    pa, pc, pq, pe, pw = _operands(dtype, [(A, K * M, "A")], [(Cm, M * N, "C")], [*_codes(q, e, K, N), (ws, 0, "ws")])
-    _check(_lib.zl_op_act8_dw(dtype, fmt, M, N, K, pa, pq, pe, pc, accumulate, pw, 0 if ws is None else ws.numel(), stream))
-
-
-def _gate_numel(p: zl_block_norm) -> int:
-    return (-(-p.N // p.gate_rows) if p.gate_rows > 0 else 1) * p.d
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, g = _here(torch), (N + 31) // 32
+    _check(_lib.zl_op_act8_dw(dtype, fmt, M, N, K, _ptr(A, bf16 if dtype == ZL_DTYPE_BF16 else f32, K * M, cur, "A"),
+                              _ptr(q, u8, K * g * 32, cur, "q"), _ptr(e, u8, K * g, cur, "e"), _ptr(Cm, f32, M * N, cur, "C"),
+                              accumulate, _ptr(ws, u8, 0, cur, "ws"), 0 if ws is None else ws.numel(), stream))
 
 
 def zl_op_block_norm(p: zl_block_norm, h, f, post_w, post_b, gate, pre_w, pre_b, h_out, n_out, stats, f_q=None, f_e=None,
                      n_q=None, n_e=None, stream: int = 0) -> None:
-    n, d = p.N * p.d, p.d
-    ph, pf, po, pn, *w = _operands(
-        p.dtype, [(h, n, "h"), (f, n, "f"), (h_out, n, "h_out"), (n_out, n, "n_out")],
-        [(post_w, d, "post_w"), (post_b, d, "post_b"), (gate, _gate_numel(p), "gate"), (pre_w, d, "pre_w"), (pre_b, d, "pre_b"),
-         (stats, 4 * p.N, "stats")],
-        [*_codes(f_q, f_e, p.N, d, "f_"), *_codes(n_q, n_e, p.N, d, "n_")])
-    _check(_lib.zl_op_block_norm(C.byref(p), ph, pf, *w[:5], po, pn, *w[5:], stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, N, d, rows = _here(torch), p.N, p.d, p.gate_rows
+    at, n, g = bf16 if p.dtype == ZL_DTYPE_BF16 else f32, N * d, (d + 31) // 32
+    _check(_lib.zl_op_block_norm(
+        C.byref(p), _ptr(h, at, n, cur, "h"), _ptr(f, at, n, cur, "f"), _ptr(post_w, f32, d, cur, "post_w"),
+        _ptr(post_b, f32, d, cur, "post_b"), _ptr(gate, f32, -(-N // rows) * d if rows > 0 else d, cur, "gate"),
+        _ptr(pre_w, f32, d, cur, "pre_w"), _ptr(pre_b, f32, d, cur, "pre_b"), _ptr(h_out, at, n, cur, "h_out"),
+        _ptr(n_out, at, n, cur, "n_out"), _ptr(stats, f32, 4 * N, cur, "stats"), _ptr(f_q, u8, N * g * 32, cur, "f_q"),
+        _ptr(f_e, u8, N * g, cur, "f_e"), _ptr(n_q, u8, N * g * 32, cur, "n_q"), _ptr(n_e, u8, N * g, cur, "n_e"), stream))
 
 
 def zl_op_block_norm_bwd_bytes(p: zl_block_norm) -> int:
@@ -463,15 +488,18 @@ def zl_op_block_norm_bwd_bytes(p: zl_block_norm) -> int:
 def zl_op_block_norm_bwd(p: zl_block_norm, h_out, f, f_q, f_e, post_w, post_b, gate, pre_w, stats, dn, dh_out, dh, df,
                          dpost_w, dpost_b, dgate, dpre_w, dpre_b, ws, stream: int = 0) -> None:
     """ws: a uint8 tensor of at least zl_op_block_norm_bwd_bytes(p) elements."""
-    n, d = p.N * p.d, p.d
-    pho, pf, pdn, pdho, pdh, pdf, *w = _operands(
-        p.dtype, [(h_out, n, "h_out"), (f, n, "f"), (dn, n, "dn"), (dh_out, n, "dh_out"), (dh, n, "dh"), (df, n, "df")],
-        [(post_w, d, "post_w"), (post_b, d, "post_b"), (gate, _gate_numel(p), "gate"), (pre_w, d, "pre_w"), (stats, 4 * p.N, "stats"),
-         (dpost_w, d, "dpost_w"), (dpost_b, d, "dpost_b"), (dgate, _gate_numel(p), "dgate"), (dpre_w, d, "dpre_w"),
-         (dpre_b, d, "dpre_b")],
-        [*_codes(f_q, f_e, p.N, d, "f_"), (ws, 0, "ws")])
-    _check(_lib.zl_op_block_norm_bwd(C.byref(p), pho, pf, *w[10:12], *w[:5], pdn, pdho, pdh, pdf, *w[5:10], w[12],
-                                     0 if ws is None else ws.numel(), stream))
+    torch, f32, bf16, u8 = _types or _torch()
+    cur, N, d, rows = _here(torch), p.N, p.d, p.gate_rows
+    at, n, g = bf16 if p.dtype == ZL_DTYPE_BF16 else f32, N * d, (d + 31) // 32
+    ng = -(-N // rows) * d if rows > 0 else d
+    _check(_lib.zl_op_block_norm_bwd(
+        C.byref(p), _ptr(h_out, at, n, cur, "h_out"), _ptr(f, at, n, cur, "f"), _ptr(f_q, u8, N * g * 32, cur, "f_q"),
+        _ptr(f_e, u8, N * g, cur, "f_e"), _ptr(post_w, f32, d, cur, "post_w"), _ptr(post_b, f32, d, cur, "post_b"),
+        _ptr(gate, f32, ng, cur, "gate"), _ptr(pre_w, f32, d, cur, "pre_w"), _ptr(stats, f32, 4 * N, cur, "stats"),
+        _ptr(dn, at, n, cur, "dn"), _ptr(dh_out, at, n, cur, "dh_out"), _ptr(dh, at, n, cur, "dh"), _ptr(df, at, n, cur, "df"),
+        _ptr(dpost_w, f32, d, cur, "dpost_w"), _ptr(dpost_b, f32, d, cur, "dpost_b"), _ptr(dgate, f32, ng, cur, "dgate"),
+        _ptr(dpre_w, f32, d, cur, "dpre_w"), _ptr(dpre_b, f32, d, cur, "dpre_b"), _ptr(ws, u8, 0, cur, "ws"),
+        0 if ws is None else ws.numel(), stream))
 
 
 def zl_profile(ctx, on: bool) -> None:
