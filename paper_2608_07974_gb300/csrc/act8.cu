@@ -14,46 +14,86 @@ using namespace act8;
 constexpr int kThreads = 256;
 
 // Items of a kernel over the 8-column pieces of N rows in whole groups, four neighbouring lanes to a group: every lane of
-// a warp runs the loop, `in` says whether its item exists.
+// a warp runs the code, `in` says whether its item exists. Rows that do not start on 16 bytes (MODE kSingle) are written
+// through shared memory, a tile of a row to a block (2048 x 22001 from integer codes 111 -> 44 us); they are read value by
+// value, which L1 makes up for (29 us to write such rows as codes; through shared memory 54).
 struct Items {
   uint32_t n;      // N * D / 8, below 2^31
   FastDiv row;     // D / 8 pieces to a row
+  uint32_t tiles;  // kSingle: blocks to a row
 };
+struct Item {
+  uint32_t r, c8, at;   // row, piece of it, r * (D / 8) + c8
+  bool in;
+  int c0, cols;         // kSingle: first column of the block's tile, columns of the row in it
+  __device__ __forceinline__ int c() const { return (int)c8 * 8; }
+};
+template <int MODE>
+__device__ __forceinline__ Item item(const Items& it, int d) {
+  Item x;
+  if (MODE != kSingle) {
+    x.at = blockIdx.x * kThreads + threadIdx.x;
+    x.in = x.at < it.n;
+    x.r = x.in ? it.row.quot(x.at) : 0;
+    x.c8 = x.at - x.r * it.row.d;
+    x.c0 = x.cols = 0;
+    return x;
+  }
+  x.r = blockIdx.x / it.tiles;
+  const uint32_t tile = blockIdx.x - x.r * it.tiles;
+  x.c8 = tile * blockDim.x + threadIdx.x;
+  x.in = x.c8 < it.row.d;
+  x.at = x.r * it.row.d + x.c8;
+  x.c0 = (int)(tile * blockDim.x * 8);
+  x.cols = max(0, min(d - x.c0, (int)blockDim.x * 8));
+  return x;
+}
+// One tile of a row in shared memory (nothing where rows start on 16 bytes).
+template <typename T, int MODE>
+struct Tile {
+  static constexpr int N = MODE == kSingle ? kThreads * 8 : 8;
+};
+template <int MODE, typename T>
+__device__ __forceinline__ void tile_out(T* sm, T* p, const Item& x, int d, const float* f) {
+  if (MODE != kSingle) {
+    if (x.in) store8<MODE>(p, x.c(), d, f);
+    return;
+  }
+  store8<kTail>(sm, x.c() - x.c0, x.cols, f);
+  __syncthreads();
+  row_out(p + x.c0, sm, x.cols, (int)threadIdx.x, (int)blockDim.x);
+  __syncthreads();
+}
 
 // ------------------------------------------------------------------------------------------------
 // Rows to 8 bits and back. HBM-bound: 3.03 bytes a value in bf16, 5.03 in fp32.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int FMT, int MODE>
-__global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it,
-                                                    uint2* __restrict__ q, uint8_t* __restrict__ e) {
+__global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it, uint2* __restrict__ q,
+                                                    uint8_t* __restrict__ e) {
   pdl_wait();
   pdl_trigger();
-  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  const bool in = i < it.n;
-  float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (in) {
-    const uint32_t r = it.row.quot(i);
-    load8<MODE>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
-  }
+  const Item i = item<MODE>(it, d);
+  float f[8];
+  floats(load_raw<MODE>(x + i.r * ldx, i.c(), i.in ? d : 0), f);
   uint2 w;
   const uint32_t b = encode_quarter<FMT>(f, w);
-  if (in) {
-    q[i] = w;
-    if ((i & 3u) == 0) e[i >> 2] = (uint8_t)b;
+  if (i.in) {
+    q[i.at] = w;
+    if ((i.at & 3u) == 0) e[i.at >> 2] = (uint8_t)b;
   }
 }
 
 template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e, Items it,
                                                    T* __restrict__ x, size_t ldx, int d) {
+  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= it.n) return;
-  const uint32_t r = it.row.quot(i);
-  float f[8];
-  decode8<FMT>(q[i], e[i >> 2], f);
-  store8<MODE>(x + r * ldx, (int)(i - r * it.row.d) * 8, d, f);
+  const Item i = item<MODE>(it, d);
+  float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (i.in) decode8<FMT>(q[i.at], e[i.at >> 2], f);
+  tile_out<MODE>(sm, x + i.r * ldx, i, d, f);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -74,41 +114,38 @@ template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, Items it, T* __restrict__ y,
                                                   uint2* __restrict__ q, uint8_t* __restrict__ e) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
+  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  const bool in = i < it.n;
-  const uint32_t r = in ? it.row.quot(i) : 0, c8 = i - r * it.row.d;
-  const int c = (int)c8 * 8;
-  const T* xr = x + (size_t)r * W * f;
-  const Raw8<T> rg = load_raw<MODE>(xr, c, in ? f : 0);
+  const Item i = item<MODE>(it, f);
+  const T* xr = x + (size_t)i.r * W * f;
+  const Raw8<T> rg = load_raw<MODE>(xr, i.c(), i.in ? f : 0);
   Raw8<T> ru;
-  if (W == 2) ru = load_raw<MODE>(xr + f, c, in ? f : 0);
+  if (W == 2) ru = load_raw<MODE>(xr + f, i.c(), i.in ? f : 0);
   float g[8], u[8];
   floats(rg, g);
   if (W == 2) floats(ru, u);
   uint2 w;
   uint32_t b = encode_quarter<FMT>(g, w);
-  size_t at = (size_t)r * W * it.row.d + c8;
-  if (in) {
+  size_t at = (size_t)i.r * W * it.row.d + i.c8;
+  if (i.in) {
     q[at] = w;
-    if ((c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
+    if ((i.c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
   }
   if (W == 2) {
     b = encode_quarter<FMT>(u, w);
     at += it.row.d;
-    if (in) {
+    if (i.in) {
       q[at] = w;
-      if ((c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
+      if ((i.c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
     }
   }
-  if (!in) return;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
     else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
   }
-  store8<MODE>(y + (size_t)r * f, c, f, g);
+  tile_out<MODE>(sm, y + (size_t)i.r * f, i, f, g);
 }
 
 template <typename T, int FMT, int ACT, int MODE>
@@ -116,16 +153,13 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
                                                       const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
+  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= it.n) return;
-  const uint32_t r = it.row.quot(i), c8 = i - r * it.row.d;
-  const int c = (int)c8 * 8;
-  const size_t at = (size_t)r * W * it.row.d + c8;
+  const Item i = item<MODE>(it, f);
+  const size_t at = i.in ? (size_t)i.r * W * it.row.d + i.c8 : 0, at2 = i.in && W == 2 ? at + it.row.d : at;
   float g[8], u[8], t[8], a[8];
-  const size_t at2 = W == 2 ? at + it.row.d : at;
-  const Raw8<T> rt = load_raw<MODE>(dy + (size_t)r * f, c, f);
+  const Raw8<T> rt = load_raw<MODE>(dy + (size_t)i.r * f, i.c(), i.in ? f : 0);
   const uint2 qg = q[at], qu = q[at2];
   const uint32_t eg = e[at >> 2], eu = e[at2 >> 2];
   floats(rt, t);
@@ -144,10 +178,10 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
       g[k] = t[k] * (s + 2.f * x * s * (1.f - s) * kGeluK * (1.f + 3.f * kGeluC * x * x));
     }
   }
-  T* dr = dx + (size_t)r * W * f;
-  store8<MODE>(dr, c, f, g);
-  if (W == 2) store8<MODE>(dr + f, c, f, u);
-  if (y) store8<MODE>(y + (size_t)r * f, c, f, a);
+  T* dr = dx + (size_t)i.r * W * f;
+  tile_out<MODE>(sm, dr, i, f, g);
+  if (W == 2) tile_out<MODE>(sm, dr + f, i, f, u);
+  if (y) tile_out<MODE>(sm, y + (size_t)i.r * f, i, f, a);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -267,28 +301,39 @@ const char* const kShapeMsg =
 bool codes_ok(const void* q, const void* e) { return q && e && ((uintptr_t)q & 15u) == 0; }
 const char* const kPtrMsg = "NULL pointer, or codes that are not 16-byte aligned";
 
-Items items(int N, int d) { return Items{(uint32_t)((size_t)N * (pitch(d) / 8)), FastDiv((uint32_t)(pitch(d) / 8))}; }
-unsigned blocks_of(const Items& it) { return (it.n + kThreads - 1) / kThreads; }
+// Items of N rows and the blocks and threads that take them.
+struct Shape {
+  Items it;
+  unsigned blocks, threads;
+  Shape(int N, int d, int mode) {
+    const uint32_t pieces = (uint32_t)(pitch(d) / 8);
+    it.n = (uint32_t)((size_t)N * pieces);
+    it.row = FastDiv(pieces);
+    threads = mode == kSingle ? std::min<unsigned>(kThreads, (pieces + 31) / 32 * 32) : kThreads;
+    it.tiles = (pieces + threads - 1) / threads;
+    blocks = mode == kSingle ? (unsigned)N * it.tiles : (it.n + kThreads - 1) / kThreads;
+  }
+};
 
 template <typename T, int FMT>
 void store_t(const void* x, size_t ldx, int N, int d, int mode, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Items it = items(N, d);
-  launch_pdl(mode == kWhole ? store_k<T, FMT, kWhole> : mode == kTail ? store_k<T, FMT, kTail> : store_k<T, FMT, kSingle>, blocks_of(it), kThreads, 0, s, (const T*)x, ldx, d, it, (uint2*)q, e);
+  const Shape h(N, d, mode);
+  launch_pdl(mode == kWhole ? store_k<T, FMT, kWhole> : mode == kTail ? store_k<T, FMT, kTail> : store_k<T, FMT, kSingle>, h.blocks, h.threads, 0, s, (const T*)x, ldx, d, h.it, (uint2*)q, e);
 }
 template <typename T, int FMT>
 void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, int mode, cudaStream_t s) {
-  const Items it = items(N, d);
-  launch_pdl(mode == kWhole ? load_k<T, FMT, kWhole> : mode == kTail ? load_k<T, FMT, kTail> : load_k<T, FMT, kSingle>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, it, (T*)x, ldx, d);
+  const Shape h(N, d, mode);
+  launch_pdl(mode == kWhole ? load_k<T, FMT, kWhole> : mode == kTail ? load_k<T, FMT, kTail> : load_k<T, FMT, kSingle>, h.blocks, h.threads, 0, s, (const uint2*)q, e, h.it, (T*)x, ldx, d);
 }
 template <typename T, int FMT, int ACT>
 void act_t(const void* x, int N, int f, int mode, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Items it = items(N, f);
-  launch_pdl(mode == kWhole ? act_k<T, FMT, ACT, kWhole> : mode == kTail ? act_k<T, FMT, ACT, kTail> : act_k<T, FMT, ACT, kSingle>, blocks_of(it), kThreads, 0, s, (const T*)x, f, it, (T*)y, (uint2*)q, e);
+  const Shape h(N, f, mode);
+  launch_pdl(mode == kWhole ? act_k<T, FMT, ACT, kWhole> : mode == kTail ? act_k<T, FMT, ACT, kTail> : act_k<T, FMT, ACT, kSingle>, h.blocks, h.threads, 0, s, (const T*)x, f, h.it, (T*)y, (uint2*)q, e);
 }
 template <typename T, int FMT, int ACT>
 void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, int mode, void* dx, void* y, cudaStream_t s) {
-  const Items it = items(N, f);
-  launch_pdl(mode == kWhole ? act_bwd_k<T, FMT, ACT, kWhole> : mode == kTail ? act_bwd_k<T, FMT, ACT, kTail> : act_bwd_k<T, FMT, ACT, kSingle>, blocks_of(it), kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, it, (T*)dx,
+  const Shape h(N, f, mode);
+  launch_pdl(mode == kWhole ? act_bwd_k<T, FMT, ACT, kWhole> : mode == kTail ? act_bwd_k<T, FMT, ACT, kTail> : act_bwd_k<T, FMT, ACT, kSingle>, h.blocks, h.threads, 0, s, (const uint2*)q, e, (const T*)dy, f, h.it, (T*)dx,
              (T*)y);
 }
 

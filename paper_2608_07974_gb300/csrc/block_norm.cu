@@ -259,10 +259,8 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
       bulk_row(p, (const T*)a.f + o, bytes, bar);
       bulk_row(p + g.pitch, (const T*)a.h + o, bytes, bar);
     } else {
-      for (int c = t; c < a.d; c += nt) {
-        reinterpret_cast<T*>(p)[c] = ((const T*)a.f)[o + c];
-        reinterpret_cast<T*>(p + g.pitch)[c] = ((const T*)a.h)[o + c];
-      }
+      row_in(reinterpret_cast<T*>(p), (const T*)a.f + o, a.d, t, nt);
+      row_in(reinterpret_cast<T*>(p + g.pitch), (const T*)a.h + o, a.d, t, nt);
     }
   };
   if (VEC && t == 0)
@@ -384,7 +382,8 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
         cut<VEC>(h[j], c, a.d);
         Raw8<T> out;
         pack8(h[j], out);
-        store_raw<mode_of(VEC)>((T*)a.ho + o, c, a.d, out);
+        if (VEC) store_raw<kWhole>((T*)a.ho + o, c, a.d, out);
+        else if (c < a.D) out.set(ring + c * sizeof(T));   // in f's place, which everyone has read
       }
     }
     stat(a.pre, [&](int j, uint64_t* x) {
@@ -394,6 +393,10 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
     if (t == 0) {
       a.stats[2 * (size_t)a.N + row] = mean;
       a.stats[3 * (size_t)a.N + row] = rstd;
+    }
+    if (!VEC) {
+      if (!a.pre) __syncthreads();
+      row_out((T*)a.ho + o, reinterpret_cast<const T*>(ring), a.d, t, nt);
     }
     if (!a.pre) continue;
     const uint64_t mm = f2(mean, mean), rr = f2(rstd, rstd);
@@ -409,12 +412,17 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
       cut<VEC>(h[j], c, a.d);
       Raw8<T> out;
       pack8(h[j], out);
-      store_raw<mode_of(VEC)>((T*)a.no + o, c, a.d, out);
+      if (VEC) store_raw<kWhole>((T*)a.no + o, c, a.d, out);
+      else if (c < a.D) out.set(ring + g.pitch + c * sizeof(T));
       if (KEEP >= 0 && a.nq) {   // of n as it is stored
         float n[8];
         floats(out, n);
         put_codes<KEEP < 0 ? 0 : KEEP>(n, a.nq + (size_t)row * a.D, a.ne + (size_t)row * (a.D >> 5), c, a.D);
       }
+    }
+    if (!VEC) {
+      __syncthreads();
+      row_out((T*)a.no + o, reinterpret_cast<const T*>(ring + g.pitch), a.d, t, nt);
     }
   }
   if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
@@ -929,14 +937,14 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       if (a.fq) bulk_row(p + 3 * g.pitch, a.fq + (size_t)n * a.D, (uint32_t)a.D, bar);
       else bulk_row(p + 3 * g.pitch, (const T*)a.f + o, bytes, bar);
     } else {
-      for (int c = t; c < a.d; c += nt) {
-        if (a.pre) {
-          reinterpret_cast<T*>(p)[c] = ((const T*)a.dn)[o + c];
-          reinterpret_cast<T*>(p + 2 * g.pitch)[c] = ((const T*)a.ho)[o + c];
-        }
-        if (a.dho) reinterpret_cast<T*>(p + g.pitch)[c] = ((const T*)a.dho)[o + c];
-        if (!a.fq) reinterpret_cast<T*>(p + 3 * g.pitch)[c] = ((const T*)a.f)[o + c];
+      if (a.pre) {
+        row_in(reinterpret_cast<T*>(p), (const T*)a.dn + o, a.d, t, nt);
+        row_in(reinterpret_cast<T*>(p + 2 * g.pitch), (const T*)a.ho + o, a.d, t, nt);
       }
+      if (a.dho) row_in(reinterpret_cast<T*>(p + g.pitch), (const T*)a.dho + o, a.d, t, nt);
+      else
+        for (int c = t; c < a.d; c += nt) reinterpret_cast<T*>(p + g.pitch)[c] = from_f<T>(0.f);   // (dh was formed there)
+      if (!a.fq) row_in(reinterpret_cast<T*>(p + 3 * g.pitch), (const T*)a.f + o, a.d, t, nt);
       if (a.fq)
         for (int c = t; c < a.D / 16; c += nt)
           reinterpret_cast<uint4*>(p + 3 * g.pitch)[c] = reinterpret_cast<const uint4*>(a.fq + (size_t)n * a.D)[c];
@@ -1160,7 +1168,8 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         if (a.dh) {
           Raw8<T> out;
           pack8(v, out);
-          store_raw<mode_of(VEC)>((T*)a.dh + o, c, a.d, out);
+          if (VEC) store_raw<kWhole>((T*)a.dh + o, c, a.d, out);
+          else out.set(ring + g.pitch + c * sizeof(T));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1170,7 +1179,13 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         }
         Raw8<T> out;
         pack8(v, out);
-        store_raw<mode_of(VEC)>((T*)a.df + o, c, a.d, out);
+        if (VEC) store_raw<kWhole>((T*)a.df + o, c, a.d, out);
+        else out.set(ring + c * sizeof(T));
+      }
+      if (!VEC) {
+        __syncthreads();
+        if (a.dh) row_out((T*)a.dh + o, reinterpret_cast<const T*>(ring + g.pitch), a.d, t, nt);
+        row_out((T*)a.df + o, reinterpret_cast<const T*>(ring), a.d, t, nt);
       }
     }
     if (--gate_left == 0 && !a.per_group) {
