@@ -154,7 +154,8 @@ __device__ __forceinline__ void drain(uint64_t* full, Turn at, int stages, int n
 
 // What a launch of a ring kernel is given besides its operands.
 struct Ring {
-  int stages, rows;   // rows: of a block, one after another
+  int stages;
+  int rows, more;     // forward: neighbouring rows of a block, one more of the first `more` blocks
   uint32_t pitch;     // bytes of a row of T in shared memory (whole groups)
   uint32_t stage;     // bytes of a stage
 };
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
   const int t = threadIdx.x, nt = blockDim.x;
-  const int r0 = (int)blockIdx.x * g.rows, rows = min(g.rows, a.N - r0);
+  const int r0 = (int)blockIdx.x * g.rows + min((int)blockIdx.x, g.more), rows = g.rows + ((int)blockIdx.x < g.more ? 1 : 0);
   const uint32_t bytes = (uint32_t)a.d * sizeof(T);
   if (t == 0) {
     for (int i = 0; i < g.stages; ++i) tc::mbar_init(&full[i], 1);
@@ -569,8 +570,10 @@ bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
   const size_t smem = (size_t)g.stages * g.stage;
   if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
   const int slots = sm_count() * occ.blocks(th, smem);
-  g.rows = (a.N + slots - 1) / slots;
-  return launch_pdl(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>, (a.N + g.rows - 1) / g.rows, th, smem, s, a, g) == cudaSuccess;
+  const int grid = std::min(a.N, slots);
+  g.rows = a.N / grid;
+  g.more = a.N % grid;
+  return launch_pdl(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>, grid, th, smem, s, a, g) == cudaSuccess;
 }
 template <typename T, int VPT, bool VEC>
 bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
