@@ -460,3 +460,34 @@ def test_on_another_stream_and_in_a_graph(B):
         torch.cuda.synchronize()
         for a, b in zip(got, (y, dx, again, C)):
             assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,d", [(1, 1), (5, 31), (37, 1001), (130, 264), (3, 5000)])
+def test_outputs_stay_in_bounds(B, dtype, N, d):
+    """Every output between two bands of a bit pattern, which stay as they are."""
+    T, dt, bufs = R.DT[dtype], code(B, dtype), {}
+
+    def out(name, n, t):
+        size = torch.empty(0, dtype=t).element_size()
+        bufs[name] = (torch.full((n * size + 8192,), 0xA5, dtype=torch.uint8, device="cuda"), n * size)
+        return bufs[name][0][4096:4096 + n * size].view(t)
+
+    D = R.width(d)
+    x, dy, A = (torch.randn(*s, device="cuda").to(T) for s in ((N, 2 * d), (N, d), (N, 24)))
+    q, e = out("q", 2 * N * D, torch.uint8), out("e", 2 * N * D // 32, torch.uint8)
+    y, again, dx, back = out("y", N * d, T), out("again", N * d, T), out("dx", 2 * N * d, T), out("back", 2 * N * d, T)
+    B.zl_op_act8_act(dt, R.SWIGLU, R.INT8, x, N, d, y, q, e)
+    B.zl_op_act8_act_bwd(dt, R.SWIGLU, R.INT8, q, e, dy, N, d, dx, again)
+    B.zl_op_act8_load(dt, R.INT8, q, e, 2 * N, d, d, back.view(2 * N, d))
+    q2, e2 = out("q2", N * D, torch.uint8), out("e2", N * D // 32, torch.uint8)
+    B.zl_op_act8_store(dt, R.E4M3, y.view(N, d), N, d, d, q2, e2)
+    C = out("C", 24 * d, torch.float32)
+    nws = B.zl_op_act8_dw_bytes(dt, 24, d, N)
+    ws = torch.full((nws + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    B.zl_op_act8_dw(dt, R.E4M3, 24, d, N, A, q2, e2, C, 0, ws[:nws])
+    torch.cuda.synchronize()
+    for name, (b, m) in bufs.items():
+        assert bool((b[:4096] == 0xA5).all()) and bool((b[4096 + m:] == 0xA5).all()), name
+    assert bool((ws[nws:] == 0xA5).all())

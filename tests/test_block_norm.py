@@ -405,3 +405,119 @@ def test_feed_forward_block_with_checkpoints(B, dtype, fmt):
     for k, (a, b) in want.items():
         a = a.cpu().double()
         assert float((a - b).norm() / b.norm()) <= tol, (k, float((a - b).norm() / b.norm()))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,d,rows", [(37, 1000, 5), (130, 72, 0), (9, 4097, 2), (3, 8192, 0), (2, 9000, 1), (301, 264, 100)])
+def test_outputs_stay_in_bounds(B, dtype, N, d, rows):
+    """Every output between two bands of a bit pattern, which stay as they are; and nothing but the outputs is written."""
+    T, c = R.DT[dtype], setting(R.LAYER, R.LAYER, rows=rows)
+    g = torch.Generator().manual_seed(N)
+    p = cuda(params(c, N, d, g))
+    D, G = R.width(d), p["gate"].shape[0]
+    bufs = {}
+
+    def out(name, n, dt):
+        size = torch.empty(0, dtype=dt).element_size()
+        bufs[name] = (torch.full((n * size + 8192,), 0xA5, dtype=torch.uint8, device="cuda"), n * size)
+        return bufs[name][0][4096:4096 + n * size].view(dt)
+
+    h, f = acts(N, d, dtype, g).cuda(), acts(N, d, dtype, g).cuda()
+    pr = dims(B, dtype, c, N, d, R.INT8)
+    keep = [t.clone() for t in (h, f)]
+    ho, n, st = out("ho", N * d, T), out("n", N * d, T), out("stats", 4 * N, torch.float32)
+    fq, fe, nq, ne = out("fq", N * D, torch.uint8), out("fe", N * D // 32, torch.uint8), out("nq", N * D, torch.uint8), out("ne", N * D // 32, torch.uint8)
+    B.zl_op_block_norm(pr, h, f, p["post_w"], p["post_b"], p["gate"], p["pre_w"], p["pre_b"], ho, n, st, fq, fe, nq, ne)
+    nws = B.zl_op_block_norm_bwd_bytes(pr)
+    ws = torch.full((nws + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    dh, df = out("dh", N * d, T), out("df", N * d, T)
+    gr = [out(k, m, torch.float32) for k, m in (("dpost_w", d), ("dpost_b", d), ("dgate", G * d), ("dpre_w", d), ("dpre_b", d))]
+    dn, dho = acts(N, d, dtype, g).cuda(), acts(N, d, dtype, g).cuda()
+    B.zl_op_block_norm_bwd(pr, ho, None, fq, fe, p["post_w"], p["post_b"], p["gate"], p["pre_w"], st, dn, dho, dh, df, *gr, ws[:nws])
+    torch.cuda.synchronize()
+    for name, (b, m) in bufs.items():
+        assert bool((b[:4096] == 0xA5).all()) and bool((b[4096 + m:] == 0xA5).all()), name
+    assert bool((ws[nws:] == 0xA5).all())
+    assert torch.equal(h, keep[0]) and torch.equal(f, keep[1])
+
+
+@gpu
+def test_calls_on_two_streams_at_once(B):
+    """The same work on two streams, each with its own workspace, gives what it gives alone."""
+    N, d, T = 517, 2048, torch.bfloat16
+    c, g = setting(R.RMS, R.RMS), torch.Generator().manual_seed(2)
+    p = cuda(params(c, N, d, g))
+    pr = dims(B, "bf16", c, N, d)
+    nws = B.zl_op_block_norm_bwd_bytes(pr)
+    ins = [[acts(N, d, "bf16", g).cuda() for _ in range(4)] for _ in range(2)]
+
+    def work(k, s):
+        h, f, dn, dho = ins[k]
+        e = lambda *a, dt=T: torch.empty(*a, dtype=dt, device="cuda")  # noqa: E731
+        o = [e(N, d), e(N, d), e(4, N, dt=torch.float32), *codes(N, d), e(N, d), e(N, d), e(d, dt=torch.float32), e(1, d, dt=torch.float32), e(d, dt=torch.float32),
+             e(nws, dt=torch.uint8)]
+        torch.cuda.synchronize()
+
+        def go():
+            for _ in range(10):
+                B.zl_op_block_norm(pr, h, f, p["post_w"], None, p["gate"], p["pre_w"], None, *o[:3], o[3], o[4], None, None, s)
+                B.zl_op_block_norm_bwd(pr, o[0], None, o[3], o[4], p["post_w"], None, p["gate"], p["pre_w"], o[2], dn, dho, o[5], o[6], o[7], None, o[8], o[9], None,
+                                       o[10], s)
+        return o[:-1], go
+
+    alone = []
+    for k in range(2):
+        o, go = work(k, 0)
+        go()
+        torch.cuda.synchronize()
+        alone.append(o)
+    st = [torch.cuda.Stream(), torch.cuda.Stream()]
+    both = [work(k, st[k].cuda_stream) for k in range(2)]
+    for _, go in both:
+        go()
+    torch.cuda.synchronize()
+    for k in range(2):
+        for a, b in zip(alone[k], both[k][0]):
+            assert torch.equal(a, b)
+
+
+FIRST_CALL = """
+import sys, torch
+sys.path.insert(0, %r)
+from paper_2608_07974_gb300 import binding as B
+T, N, d = torch.bfloat16, 64, 512
+x = torch.randn(N, d, device="cuda").to(T)
+e = lambda *a, dt=T: torch.empty(*a, dtype=dt, device="cuda")
+q, s = e(N, d, dt=torch.uint8), e(N, d // 32, dt=torch.uint8)
+p = B.zl_block_norm(dtype=1, post_norm=1, pre_norm=1, N=N, d=d, gate_rows=0, eps=1e-5, res_scale=1, branch_scale=1, fmt=0, accumulate=0)
+w, C = e(d, dt=torch.float32).fill_(1), e(d, d, dt=torch.float32)
+ho, n, st, dh, df = e(N, d), e(N, d), e(4, N, dt=torch.float32), e(N, d), e(N, d)
+gr, ws, ws2 = e(d, dt=torch.float32), e(B.zl_op_block_norm_bwd_bytes(p), dt=torch.uint8), e(B.zl_op_act8_dw_bytes(1, d, d, N), dt=torch.uint8)
+torch.cuda.synchronize()
+def step(s_):
+    B.zl_op_block_norm(p, x, x, w, None, None, w, None, ho, n, st, q, s, None, None, s_)
+    B.zl_op_block_norm_bwd(p, ho, None, q, s, w, None, None, w, st, n, x, dh, df, gr, None, None, None, None, ws, s_)
+    B.zl_op_act8_dw(1, 0, d, d, N, df, q, s, C, 0, ws2, s_)
+g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+with torch.cuda.graph(g, stream=side):
+    step(side.cuda_stream)
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (ho, n, st, dh, df, gr, C)]
+step(0)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (ho, n, st, dh, df, gr, C)))
+print("captured")
+"""
+
+
+@gpu
+def test_first_call_may_be_captured(B):
+    """A process whose first calls are those of a capture: nothing has to run before it."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL % root], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
