@@ -205,33 +205,36 @@ __device__ __forceinline__ void cut(uint64_t* v, int c, int d) {
   }
 }
 
-// The parameters of a thread's columns: a = beta gate w_post, b = beta gate b_post, w = w_pre, v = b_pre. They stay in
-// registers from row to row (a and b until the gate's row changes): read for every row they were 48 KB more a row than its
-// 32 KB of traffic (d = 4096, bf16), and their latency the longest part of it. BIAS: b and v exist.
-template <int VPT, bool VEC, bool BIAS>
+// The parameters of a thread's columns: a = beta gate w_post, b = beta gate b_post, w = w_pre, v = b_pre, all 0 past d (so is
+// then what they multiply). They stay in registers from row to row (a and b until the gate's row changes): read for every row
+// they were 48 KB more a row than its 32 KB of traffic (d = 4096, bf16), and their latency the longest part of it.
+template <int VPT, bool VEC, bool LN>
 struct Params {
-  uint64_t a[VPT][4], b[BIAS ? VPT : 1][4], w[VPT][4], v[BIAS ? VPT : 1][4];
+  uint64_t a[VPT][4], b[LN ? VPT : 1][4], w[VPT][4], v[LN ? VPT : 1][4];
   __device__ __forceinline__ void post(int j, int c, int d, const float* pw, const float* pb, const float* gate, float beta) {
     uint64_t g[4];
     row8<VEC>(gate, c, d, 1.f, g);
     row8<VEC>(pw, c, d, 1.f, a[j]);
-    if (BIAS) row8<VEC>(pb, c, d, 0.f, b[j]);
+    if (LN) row8<VEC>(pb, c, d, 0.f, b[j]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       g[i] = mul2(g[i], f2(beta, beta));
       a[j][i] = mul2(a[j][i], g[i]);
-      if (BIAS) b[j][i] = mul2(b[j][i], g[i]);
+      if (LN) b[j][i] = mul2(b[j][i], g[i]);
     }
+    cut<VEC>(a[j], c, d);
   }
   __device__ __forceinline__ void pre(int j, int c, int d, const float* nw, const float* nb) {
     row8<VEC>(nw, c, d, 1.f, w[j]);
-    if (BIAS) row8<VEC>(nb, c, d, 0.f, v[j]);
+    if (LN) row8<VEC>(nb, c, d, 0.f, v[j]);
+    cut<VEC>(w[j], c, d);
   }
 };
 
 // VEC: rows start on 16 bytes; they come by bulk copies. KEEP: the format that f or n are written in, -1: neither is.
-template <typename T, int VPT, bool VEC, bool BIAS, int KEEP>
-__global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80) fwd_ring_k(const Fwd a, const Ring g) {
+// LN: one of the norms is a LayerNorm.
+template <typename T, int VPT, bool VEC, bool LN, int KEEP>
+__global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80) fwd_ring_k(const Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][2][16];
@@ -266,7 +269,7 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
   };
   if (VEC && t == 0)
     for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
-  Params<VPT, VEC, BIAS> pa;
+  Params<VPT, VEC, LN> pa;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) pa.pre(j, (t + j * nt) * 8, a.d, a.nw, a.nb);
   int gate_left = 0;   // rows of the gate row at hand that are still to come
@@ -303,18 +306,23 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
         rh[j].get(ring + st * g.stage + g.pitch + c * sizeof(T));
       }
     }
-    float mean = 0.f, rstd = 1.f;
-    uint64_t h[VPT][4];
-    // mean and 1 / deviation of the values val(j, x) of every vector; after the first barrier of a row everyone has it in
-    // registers, and its stage takes the row `stages` further on
-    auto stat = [&](int kind, auto&& val, bool first) {
+    // 1 / deviation of the values val(j, x) of every vector, and with a LayerNorm their mean; after the first barrier of a row
+    // everyone has it in registers, and its stage takes the row `stages` further on
+    auto stat = [&](int kind, auto&& val, bool first, float& mean, float& rstd) {
       mean = 0.f;
       rstd = 1.f;
       auto next = [&]() {
         if (VEC && first && t == 0 && k + g.stages < rows && !*abort_flag) fill(k + g.stages, st);
         first = false;
       };
-      if (kind == ZL_NORM_LAYER) {
+      if (kind == ZL_NORM_NONE) {
+        if (first) {
+          __syncthreads();
+          next();
+        }
+        return;
+      }
+      if (LN && kind == ZL_NORM_LAYER) {
         uint64_t s = 0;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
@@ -322,35 +330,32 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
           val(j, x);
           s = add2(s, add2(add2(x[0], x[1]), add2(x[2], x[3])));
         }
-        float m = fold(s);
-        red.sum(m);
+        mean = fold(s);
+        red.sum(mean);
         next();
-        mean = m * inv_d;
+        mean *= inv_d;
       }
-      if (kind != ZL_NORM_NONE) {
-        const uint64_t mm = f2(mean, mean);
-        uint64_t q2 = 0;
+      const uint64_t mm = f2(-mean, -mean);
+      uint64_t q2 = 0;
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-          const int c = (t + j * nt) * 8;
-          uint64_t x[4];
-          val(j, x);
-          if (kind == ZL_NORM_LAYER) {
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (t + j * nt) * 8;
+        uint64_t x[4];
+        val(j, x);
+        if (LN) {   // columns past d are not 0 any more
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = sub2(x[i], mm);
-            cut<VEC>(x, c, a.d);
-          }
+          for (int i = 0; i < 4; ++i) x[i] = add2(x[i], mm);
+          if (!VEC) cut<VEC>(x, c, a.d);
+        }
+        if (!LN || !VEC || c < a.d) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) q2 = fma2(x[i], x[i], q2);
         }
-        float q = fold(q2);
-        red.sum(q);
-        next();
-        rstd = 1.f / sqrtf(q * inv_d + a.eps);
-      } else if (first) {
-        __syncthreads();
-        next();
       }
+      float q = fold(q2);
+      red.sum(q);
+      next();
+      rstd = rsqrtf(q * inv_d + a.eps);
     };
     if (KEEP >= 0 && a.fq) {
 #pragma unroll
@@ -360,14 +365,12 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
         put_codes<KEEP < 0 ? 0 : KEEP>(x, a.fq + (size_t)row * a.D, a.fe + (size_t)row * (a.D >> 5), (t + j * nt) * 8, a.D);
       }
     }
-    stat(a.post, [&](int j, uint64_t* x) { rf[j].pairs(x); }, true);
+    float pm, pr, m, r;
+    stat(a.post, [&](int j, uint64_t* x) { rf[j].pairs(x); }, true, pm, pr);
     if (VEC && *abort_flag) break;
-    if (t == 0) {
-      a.stats[row] = mean;
-      a.stats[(size_t)a.N + row] = rstd;
-    }
+    uint64_t h[VPT][4];
     {
-      const uint64_t mm = f2(mean, mean), rr = f2(rstd, rstd);
+      const uint64_t mm = f2(-pm, -pm), rr = f2(pr, pr);
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (t + j * nt) * 8;
@@ -376,11 +379,10 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
         rh[j].pairs(h[j]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (a.post == ZL_NORM_LAYER) f[i] = sub2(f[i], mm);
+          if (LN) f[i] = add2(f[i], mm);
           h[j][i] = fma2(mul2(f[i], rr), pa.a[j][i], mul2(alpha, h[j][i]));
-          if (BIAS) h[j][i] = add2(h[j][i], pa.b[j][i]);
+          if (LN) h[j][i] = add2(h[j][i], pa.b[j][i]);
         }
-        cut<VEC>(h[j], c, a.d);
         Raw8<T> out;
         pack8(h[j], out);
         if (VEC) store_raw<kWhole>((T*)a.ho + o, c, a.d, out);
@@ -390,27 +392,29 @@ __global__ void __launch_bounds__(VPT == 1 ? 256 : 512) __maxnreg__(BIAS || (VPT
     stat(a.pre, [&](int j, uint64_t* x) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = h[j][i];
-    }, false);
+    }, false, m, r);
     if (t == 0) {
-      a.stats[2 * (size_t)a.N + row] = mean;
-      a.stats[3 * (size_t)a.N + row] = rstd;
+      float* q = a.stats + row;
+      q[0] = pm;
+      q[a.N] = pr;
+      q[2 * (size_t)a.N] = m;
+      q[3 * (size_t)a.N] = r;
     }
     if (!VEC) {
       if (!a.pre) __syncthreads();
       row_out((T*)a.ho + o, reinterpret_cast<const T*>(ring), a.d, t, nt);
     }
     if (!a.pre) continue;
-    const uint64_t mm = f2(mean, mean), rr = f2(rstd, rstd);
+    const uint64_t mm = f2(-m, -m), rr = f2(r, r);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (a.pre == ZL_NORM_LAYER) h[j][i] = sub2(h[j][i], mm);
+        if (LN) h[j][i] = add2(h[j][i], mm);
         h[j][i] = mul2(mul2(h[j][i], rr), pa.w[j][i]);
-        if (BIAS) h[j][i] = add2(h[j][i], pa.v[j][i]);
+        if (LN) h[j][i] = add2(h[j][i], pa.v[j][i]);
       }
-      cut<VEC>(h[j], c, a.d);
       Raw8<T> out;
       pack8(h[j], out);
       if (VEC) store_raw<kWhole>((T*)a.no + o, c, a.d, out);
@@ -556,9 +560,9 @@ constexpr int kRingCols = 8192;   // the widest row of the ring kernels
 // Threads of a block for a row of nvec vectors, one vector a thread or two.
 int ring_threads(int nvec) { return nvec <= 224 ? (nvec + 31) / 32 * 32 : (nvec + 63) / 64 * 32; }
 
-template <typename T, int VPT, bool VEC, bool BIAS, int KEEP>
+template <typename T, int VPT, bool VEC, bool LN, int KEEP>
 bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
-  static const Occupancy occ(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>);
+  static const Occupancy occ(fwd_ring_k<T, VPT, VEC, LN, KEEP>);
   if (!occ.ok) return false;
   Ring g;
   g.pitch = (uint32_t)a.D * sizeof(T);
@@ -573,24 +577,26 @@ bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
   const int grid = std::min(a.N, slots);
   g.rows = a.N / grid;
   g.more = a.N % grid;
-  return launch_pdl(fwd_ring_k<T, VPT, VEC, BIAS, KEEP>, grid, th, smem, s, a, g) == cudaSuccess;
+  return launch_pdl(fwd_ring_k<T, VPT, VEC, LN, KEEP>, grid, th, smem, s, a, g) == cudaSuccess;
 }
-template <typename T, int VPT, bool VEC>
+template <typename T, int VPT, bool VEC, bool LN>
 bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
-  const bool bias = a.pb || a.nb;
-  if (!a.fq && !a.nq) return bias ? fwd_ring<T, VPT, VEC, true, -1>(a, th, s) : fwd_ring<T, VPT, VEC, false, -1>(a, th, s);
-  if (a.fmt == ZL_ACT8_E4M3)
-    return bias ? fwd_ring<T, VPT, VEC, true, ZL_ACT8_E4M3>(a, th, s) : fwd_ring<T, VPT, VEC, false, ZL_ACT8_E4M3>(a, th, s);
-  return bias ? fwd_ring<T, VPT, VEC, true, ZL_ACT8_INT8>(a, th, s) : fwd_ring<T, VPT, VEC, false, ZL_ACT8_INT8>(a, th, s);
+  if (!a.fq && !a.nq) return fwd_ring<T, VPT, VEC, LN, -1>(a, th, s);
+  return a.fmt == ZL_ACT8_E4M3 ? fwd_ring<T, VPT, VEC, LN, ZL_ACT8_E4M3>(a, th, s) : fwd_ring<T, VPT, VEC, LN, ZL_ACT8_INT8>(a, th, s);
 }
 
+// One vector a thread up to 512 threads with RMS norms, up to 224 with a LayerNorm, whose parameters leave no second block of
+// 512 threads on an SM: 2048 x 4096 bf16 18.2 us (two vectors 19.1) and 23.4 us (one vector 30.7).
 template <typename T, bool VEC>
 void forward_as(const Fwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
+  const bool ln = a.post == ZL_NORM_LAYER || a.pre == ZL_NORM_LAYER;
   note_launch(1);
   if (a.d <= kRingCols) {
-    const int th = ring_threads(nvec);
-    if (th >= nvec ? fwd_ring_by<T, 1, VEC>(a, th, s) : fwd_ring_by<T, 2, VEC>(a, th, s)) return;
+    const int th = !ln && nvec <= 512 ? (nvec + 31) / 32 * 32 : ring_threads(nvec);
+    if (th >= nvec ? ln ? fwd_ring_by<T, 1, VEC, true>(a, th, s) : fwd_ring_by<T, 1, VEC, false>(a, th, s)
+                   : ln ? fwd_ring_by<T, 2, VEC, true>(a, th, s) : fwd_ring_by<T, 2, VEC, false>(a, th, s))
+      return;
   }
   launch_pdl(fwd_any_k<T, VEC>, a.N, 512, 0, s, a);
 }
