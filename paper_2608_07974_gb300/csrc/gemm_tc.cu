@@ -319,42 +319,42 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
         int kb0 = (unit / num_tiles) * g.kb_per_split;
         const int kbe = min(nk, kb0 + g.kb_per_split);
         do {   // once, but for DW's segments
-        const int kb1 = DW ? min(kbe, kb0 + g.kb_per_seg) : kbe;
-        const int acc = it & 1;
-        const uint32_t aph = (uint32_t)(it >> 1) & 1u;
-        if (!uwait(&tempty[acc], aph ^ 1u, abort_flag, g.err)) { ok = false; break; }
-        fence_after();
-        const uint32_t d = tmem + (uint32_t)(acc * BN);
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!uwait(&full[stage], phase, abort_flag, g.err)) { ok = false; break; }
+          const int kb1 = DW ? min(kbe, kb0 + g.kb_per_seg) : kbe;
+          const int acc = it & 1;
+          const uint32_t aph = (uint32_t)(it >> 1) & 1u;
+          if (!uwait(&tempty[acc], aph ^ 1u, abort_flag, g.err)) { ok = false; break; }
           fence_after();
-          if (leader) {
-            const uint32_t a0 = su32(smem + stage * C_::STAGE_BYTES), b0 = a0 + C_::A_BYTES;
-  #pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk) {
-              const bool b_mn = B_MN || (!A_MN && kb >= nk1);
-              const uint64_t ad = A_MN ? sdesc(a0 + kk * 2048, 8192, 1024) : sdesc(a0 + kk * 32, 16, 1024);
-              const uint64_t bd = b_mn ? sdesc(b0 + kk * 2048, 8192, 1024) : sdesc(b0 + kk * 32, 16, 1024);
-              const uint32_t idk = b_mn ? id_mn : id;
-              const uint32_t add = (kb > kb0 || kk > 0) ? 1u : 0u;
-              if (PAIR) mma_bf16_pair(d, ad, bd, idk, add);
-              else mma_bf16(d, ad, bd, idk, add);
+          const uint32_t d = tmem + (uint32_t)(acc * BN);
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!uwait(&full[stage], phase, abort_flag, g.err)) { ok = false; break; }
+            fence_after();
+            if (leader) {
+              const uint32_t a0 = su32(smem + stage * C_::STAGE_BYTES), b0 = a0 + C_::A_BYTES;
+    #pragma unroll
+              for (int kk = 0; kk < BK / 16; ++kk) {
+                const bool b_mn = B_MN || (!A_MN && kb >= nk1);
+                const uint64_t ad = A_MN ? sdesc(a0 + kk * 2048, 8192, 1024) : sdesc(a0 + kk * 32, 16, 1024);
+                const uint64_t bd = b_mn ? sdesc(b0 + kk * 2048, 8192, 1024) : sdesc(b0 + kk * 32, 16, 1024);
+                const uint32_t idk = b_mn ? id_mn : id;
+                const uint32_t add = (kb > kb0 || kk > 0) ? 1u : 0u;
+                if (PAIR) mma_bf16_pair(d, ad, bd, idk, add);
+                else mma_bf16(d, ad, bd, idk, add);
+              }
+              if (PAIR) mma_commit_pair(&empty[stage]);   // the stage is free in both CTAs
+              else mma_commit(&empty[stage]);
             }
-            if (PAIR) mma_commit_pair(&empty[stage]);   // the stage is free in both CTAs
-            else mma_commit(&empty[stage]);
+            __syncwarp();
+            if (++stage == C_::STAGES) { stage = 0; phase ^= 1u; }
+          }
+          if (ok && leader) {
+            if (PAIR) mma_commit_pair(&tfull[acc]);
+            else mma_commit(&tfull[acc]);
           }
           __syncwarp();
-          if (++stage == C_::STAGES) { stage = 0; phase ^= 1u; }
-        }
-        if (ok && leader) {
-          if (PAIR) mma_commit_pair(&tfull[acc]);
-          else mma_commit(&tfull[acc]);
-        }
-        __syncwarp();
-        if (DW) {
-          kb0 = kb1;
-          if (kb0 < kbe) ++it;
-        }
+          if (DW) {
+            kb0 = kb1;
+            if (kb0 < kbe) ++it;
+          }
         } while (DW && ok && kb0 < kbe);
       }
       // all MMAs issued by the leader complete before TMEM is released
@@ -471,58 +471,134 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
       int ok = 1, left = DW ? min(nk - split * g.kb_per_split, g.kb_per_split) : 0;   // k blocks of the unit's segments to come
       bool later = false;   // a later segment: added to what the first one wrote
       do {   // once, but for DW's segments
-      const int acc = it & 1;
-      const uint32_t aph = (uint32_t)(it >> 1) & 1u;
-      if (lane == 0) ok = mbar_wait(&tfull[acc], aph, abort_flag, g.err) ? 1 : 0;
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) break;
-      fence_after();
-      if (DW && later && lane == 0) bulk_wait_all();   // the segment before has reached C: the additions keep their order
-      const int row0 = tm * BM + q * 32;
-      const int m = row0 + lane;
-      const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
+        const int acc = it & 1;
+        const uint32_t aph = (uint32_t)(it >> 1) & 1u;
+        if (lane == 0) ok = mbar_wait(&tfull[acc], aph, abort_flag, g.err) ? 1 : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        fence_after();
+        if (DW && later && lane == 0) bulk_wait_all();   // the segment before has reached C: the additions keep their order
+        const int row0 = tm * BM + q * 32;
+        const int m = row0 + lane;
+        const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
 #pragma unroll 1
-      for (int c = 0; c < BN; c += ccols, ++nchunk) {
-        const int n0 = tn * BN + c;
-        if constexpr (BN >= 128 && !A_MN && !B_MN) {   // mode 0 kernels of 128- or 256-column tiles
-        if (g.rope_cs != nullptr && n0 < g.rope_cols) {
-          // one query / key head (rope_hd columns: one or two 64-column chunks, both staging buffers):
-          // pairs (i, i + hd/2) read from TMEM together, rounded to bf16, rotated, rounded again
-          const int hd = g.rope_hd, half = hd >> 1, nch = hd >> 6;
-          if (lane == 0) bulk_wait_read0();   // both buffers free
-          __syncwarp();
-          const float2* csr = g.rope_cs + (size_t)(m % g.rope_S) * half;
+        for (int c = 0; c < BN; c += ccols, ++nchunk) {
+          const int n0 = tn * BN + c;
+          if constexpr (BN >= 128 && !A_MN && !B_MN) {   // mode 0 kernels of 128- or 256-column tiles
+          if (g.rope_cs != nullptr && n0 < g.rope_cols) {
+            // one query / key head (rope_hd columns: one or two 64-column chunks, both staging buffers):
+            // pairs (i, i + hd/2) read from TMEM together, rounded to bf16, rotated, rounded again
+            const int hd = g.rope_hd, half = hd >> 1, nch = hd >> 6;
+            if (lane == 0) bulk_wait_read0();   // both buffers free
+            __syncwarp();
+            const float2* csr = g.rope_cs + (size_t)(m % g.rope_S) * half;
 #pragma unroll 1
-          for (int a = 0; a < half; a += 32) {
-            float4 cs4[16];   // (cos, sin) of pairs a .. a + 31 (16-byte loads, issued before the TMEM reads)
+            for (int a = 0; a < half; a += 32) {
+              float4 cs4[16];   // (cos, sin) of pairs a .. a + 31 (16-byte loads, issued before the TMEM reads)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) cs4[e] = reinterpret_cast<const float4*>(csr + a)[e];
-            float v1[32], v2[32];
-            tmem_ld32(trow + (uint32_t)(c + a), v1);
-            tmem_ld32(trow + (uint32_t)(c + a + half), v2);
+              for (int e = 0; e < 16; ++e) cs4[e] = reinterpret_cast<const float4*>(csr + a)[e];
+              float v1[32], v2[32];
+              tmem_ld32(trow + (uint32_t)(c + a), v1);
+              tmem_ld32(trow + (uint32_t)(c + a + half), v2);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float x1 = v1[e] * g.alpha, x2 = v2[e] * g.alpha;
-              if (g.bias) {
-                if (n0 + a + e < g.N) x1 += g.bias[n0 + a + e];
-                if (n0 + a + half + e < g.N) x2 += g.bias[n0 + a + half + e];
+              for (int e = 0; e < 32; ++e) {
+                float x1 = v1[e] * g.alpha, x2 = v2[e] * g.alpha;
+                if (g.bias) {
+                  if (n0 + a + e < g.N) x1 += g.bias[n0 + a + e];
+                  if (n0 + a + half + e < g.N) x2 += g.bias[n0 + a + half + e];
+                }
+                x1 = __bfloat162float(__float2bfloat16_rn(x1));
+                x2 = __bfloat162float(__float2bfloat16_rn(x2));
+                const float4 c4 = cs4[e >> 1];
+                rope_rot(x1, x2, (e & 1) ? c4.z : c4.x, (e & 1) ? c4.w : c4.y, v1[e], v2[e]);
               }
-              x1 = __bfloat162float(__float2bfloat16_rn(x1));
-              x2 = __bfloat162float(__float2bfloat16_rn(x2));
-              const float4 c4 = cs4[e >> 1];
-              rope_rot(x1, x2, (e & 1) ? c4.z : c4.x, (e & 1) ? c4.w : c4.y, v1[e], v2[e]);
-            }
 #pragma unroll
-            for (int side = 0; side < 2; ++side) {
-              const float* vv = side ? v2 : v1;
-              const int col = a + side * half;   // column within the head
-              uint8_t* srow = stage_out + (col >> 6) * (32 * 128) + lane * 128;
+              for (int side = 0; side < 2; ++side) {
+                const float* vv = side ? v2 : v1;
+                const int col = a + side * half;   // column within the head
+                uint8_t* srow = stage_out + (col >> 6) * (32 * 128) + lane * 128;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  __nv_bfloat162 hv[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) hv[e] = __floats2bfloat162_rn(vv[8 * k + 2 * e], vv[8 * k + 2 * e + 1]);
+                  const int piece = ((col & 63) >> 3) + k;
+                  *reinterpret_cast<uint4*>(srow + ((piece ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(hv);
+                }
+              }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              for (int j = 0; j < nch; ++j) {
+                if (row0 < g.M && n0 + 64 * j < g.N) tma_store2d(&tcm, stage_out + j * (32 * 128), n0 + 64 * j, row0);
+                bulk_commit();
+              }
+            }
+            drain = 1;
+            c += hd - ccols;
+            nchunk += nch - 1;
+            continue;
+          }
+          }
+          uint8_t* sbuf = stage_out + (nchunk & 1) * (32 * 128);
+          if (lane == 0) {   // the store that last used this buffer has read it
+            if (drain) bulk_wait_read0();
+            else bulk_wait_read1();
+          }
+          drain = 0;
+          __syncwarp();
+          uint8_t* srow = sbuf + lane * 128;
+          // 32 columns at a time: f32 chunks are one half, bf16 chunks two (16-byte pieces 4h .. 4h+3)
+#pragma unroll 1
+          for (int h = 0; h < ccols / 32; ++h) {
+            const int nh = n0 + 32 * h;
+            float v[32];
+            tmem_ld32(trow + (uint32_t)(c + 32 * h), v);
+            if (g.alpha != 1.f) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] *= g.alpha;
+            }
+            if (f32out) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const uint4 u = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]),
+                                           __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
+                *reinterpret_cast<uint4*>(srow + ((k ^ (lane & 7)) << 4)) = u;
+              }
+            } else {
+              if (g.bias) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  if (nh + 4 * j < g.N) {
+                    const float4 b4 = *reinterpret_cast<const float4*>(g.bias + nh + 4 * j);
+                    v[4 * j] += b4.x; v[4 * j + 1] += b4.y; v[4 * j + 2] += b4.z; v[4 * j + 3] += b4.w;
+                  }
+                }
+              }
+              if (g.R && m < g.M) {
+                const bf16* rr = g.R + (size_t)m * g.N + nh;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if (nh + 8 * j < g.N) {
+                    float r8[8];
+                    Vec8<bf16>::load(rr + 8 * j, r8);
+                    if (g.rmode) {
+#pragma unroll
+                      for (int e = 0; e < 8; ++e) v[8 * j + e] *= gelu_tanh_grad(r8[e], true);
+                    } else {
+#pragma unroll
+                      for (int e = 0; e < 8; ++e) v[8 * j + e] += r8[e];
+                    }
+                  }
+                }
+              }
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 __nv_bfloat162 hv[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) hv[e] = __floats2bfloat162_rn(vv[8 * k + 2 * e], vv[8 * k + 2 * e + 1]);
-                const int piece = ((col & 63) >> 3) + k;
+                for (int e = 0; e < 4; ++e) hv[e] = __floats2bfloat162_rn(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
+                const int piece = 4 * h + k;
                 *reinterpret_cast<uint4*>(srow + ((piece ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(hv);
               }
             }
@@ -530,102 +606,26 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
           fence_async_smem();
           __syncwarp();
           if (lane == 0) {
-            for (int j = 0; j < nch; ++j) {
-              if (row0 < g.M && n0 + 64 * j < g.N) tma_store2d(&tcm, stage_out + j * (32 * 128), n0 + 64 * j, row0);
-              bulk_commit();
+            if (row0 < g.M && n0 < g.N) {
+              if (g.mode == 2) tma_reduce_add2d(&tcm, sbuf, n0, row0);
+              else if (DW && later) tma_reduce_add3d(&tcm, sbuf, n0, row0, split);
+              else if (g.mode == 3) tma_store3d(&tcm, sbuf, n0, row0, split);
+              else tma_store2d(&tcm, sbuf, n0, row0);
             }
-          }
-          drain = 1;
-          c += hd - ccols;
-          nchunk += nch - 1;
-          continue;
-        }
-        }
-        uint8_t* sbuf = stage_out + (nchunk & 1) * (32 * 128);
-        if (lane == 0) {   // the store that last used this buffer has read it
-          if (drain) bulk_wait_read0();
-          else bulk_wait_read1();
-        }
-        drain = 0;
-        __syncwarp();
-        uint8_t* srow = sbuf + lane * 128;
-        // 32 columns at a time: f32 chunks are one half, bf16 chunks two (16-byte pieces 4h .. 4h+3)
-#pragma unroll 1
-        for (int h = 0; h < ccols / 32; ++h) {
-          const int nh = n0 + 32 * h;
-          float v[32];
-          tmem_ld32(trow + (uint32_t)(c + 32 * h), v);
-          if (g.alpha != 1.f) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] *= g.alpha;
-          }
-          if (f32out) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint4 u = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]),
-                                         __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
-              *reinterpret_cast<uint4*>(srow + ((k ^ (lane & 7)) << 4)) = u;
-            }
-          } else {
-            if (g.bias) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                if (nh + 4 * j < g.N) {
-                  const float4 b4 = *reinterpret_cast<const float4*>(g.bias + nh + 4 * j);
-                  v[4 * j] += b4.x; v[4 * j + 1] += b4.y; v[4 * j + 2] += b4.z; v[4 * j + 3] += b4.w;
-                }
-              }
-            }
-            if (g.R && m < g.M) {
-              const bf16* rr = g.R + (size_t)m * g.N + nh;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if (nh + 8 * j < g.N) {
-                  float r8[8];
-                  Vec8<bf16>::load(rr + 8 * j, r8);
-                  if (g.rmode) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[8 * j + e] *= gelu_tanh_grad(r8[e], true);
-                  } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[8 * j + e] += r8[e];
-                  }
-                }
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              __nv_bfloat162 hv[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) hv[e] = __floats2bfloat162_rn(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
-              const int piece = 4 * h + k;
-              *reinterpret_cast<uint4*>(srow + ((piece ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(hv);
-            }
+            bulk_commit();
           }
         }
-        fence_async_smem();
+        fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (row0 < g.M && n0 < g.N) {
-            if (g.mode == 2) tma_reduce_add2d(&tcm, sbuf, n0, row0);
-            else if (DW && later) tma_reduce_add3d(&tcm, sbuf, n0, row0, split);
-            else if (g.mode == 3) tma_store3d(&tcm, sbuf, n0, row0, split);
-            else tma_store2d(&tcm, sbuf, n0, row0);
-          }
-          bulk_commit();
+          if (PAIR) mbar_arrive_cluster(tempty_addr + 8u * (uint32_t)acc);
+          else mbar_arrive(&tempty[acc]);
         }
-      }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) mbar_arrive_cluster(tempty_addr + 8u * (uint32_t)acc);
-        else mbar_arrive(&tempty[acc]);
-      }
-      if (DW) {
-        left -= g.kb_per_seg;
-        later = true;
-        if (left > 0) ++it;
-      }
+        if (DW) {
+          left -= g.kb_per_seg;
+          later = true;
+          if (left > 0) ++it;
+        }
       } while (DW && left > 0);
       if (!ok) break;
     }
