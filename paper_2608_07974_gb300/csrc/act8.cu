@@ -28,11 +28,18 @@ struct Item {
   int c0, cols;         // kSingle: first column of the block's tile, columns of the row in it
   __device__ __forceinline__ int c() const { return (int)c8 * 8; }
 };
-template <int MODE>
-__device__ __forceinline__ Item item(const Items& it, int d) {
+// Items of a thread: their loads are under way together (2048 x 22016 bf16 to e4m3 24.7 / 21.2 / 22.5 us with one, two, four,
+// back 24.6 / 21.1 / 21.7; SwiGLU forward of 2048 x 11008 32.2 / 29.5 with one, two; the backward, with more streams an item
+// and more registers, gains nothing).
+constexpr int kStoreItems = 2, kLoadItems = 2, kActItems = 2, kActBwdItems = 1;
+template <int MODE, int U>
+constexpr int per_thread = MODE == kSingle ? 1 : U;
+// Item u of U.
+template <int MODE, int U>
+__device__ __forceinline__ Item item(const Items& it, int d, int u) {
   Item x;
   if (MODE != kSingle) {
-    x.at = blockIdx.x * kThreads + threadIdx.x;
+    x.at = (blockIdx.x * U + u) * kThreads + threadIdx.x;
     x.in = x.at < it.n;
     x.r = x.in ? it.row.quot(x.at) : 0;
     x.c8 = x.at - x.r * it.row.d;
@@ -71,29 +78,52 @@ __device__ __forceinline__ void tile_out(T* sm, T* p, const Item& x, int d, cons
 template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it, uint2* __restrict__ q,
                                                     uint8_t* __restrict__ e) {
+  constexpr int U = per_thread<MODE, kStoreItems>;
   pdl_wait();
   pdl_trigger();
-  const Item i = item<MODE>(it, d);
-  float f[8];
-  floats(load_raw<MODE>(x + i.r * ldx, i.c(), i.in ? d : 0), f);
-  uint2 w;
-  const uint32_t b = encode_quarter<FMT>(f, w);
-  if (i.in) {
-    q[i.at] = w;
-    if ((i.at & 3u) == 0) e[i.at >> 2] = (uint8_t)b;
+  Item i[U];
+  Raw8<T> r[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    i[u] = item<MODE, U>(it, d, u);
+    r[u] = load_raw<MODE>(x + i[u].r * ldx, i[u].c(), i[u].in ? d : 0);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float f[8];
+    floats(r[u], f);
+    uint2 w;
+    const uint32_t b = encode_quarter<FMT>(f, w);
+    if (i[u].in) {
+      q[i[u].at] = w;
+      if ((i[u].at & 3u) == 0) e[i[u].at >> 2] = (uint8_t)b;
+    }
   }
 }
 
 template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e, Items it,
                                                    T* __restrict__ x, size_t ldx, int d) {
+  constexpr int U = per_thread<MODE, kLoadItems>;
   __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const Item i = item<MODE>(it, d);
-  float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (i.in) decode8<FMT>(q[i.at], e[i.at >> 2], f);
-  tile_out<MODE>(sm, x + i.r * ldx, i, d, f);
+  Item i[U];
+  uint2 w[U];
+  uint32_t b[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    i[u] = item<MODE, U>(it, d, u);
+    const uint32_t at = i[u].in ? i[u].at : 0;
+    w[u] = q[at];
+    b[u] = e[at >> 2];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float f[8];
+    decode8<FMT>(w[u], b[u], f);
+    tile_out<MODE>(sm, x + i[u].r * ldx, i[u], d, f);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -113,75 +143,96 @@ constexpr float kGeluK = 0.7978845608028654f, kGeluC = 0.044715f;
 template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, Items it, T* __restrict__ y,
                                                   uint2* __restrict__ q, uint8_t* __restrict__ e) {
-  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
+  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = per_thread<MODE, kActItems>;
   __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const Item i = item<MODE>(it, f);
-  const T* xr = x + (size_t)i.r * W * f;
-  const Raw8<T> rg = load_raw<MODE>(xr, i.c(), i.in ? f : 0);
-  Raw8<T> ru;
-  if (W == 2) ru = load_raw<MODE>(xr + f, i.c(), i.in ? f : 0);
-  float g[8], u[8];
-  floats(rg, g);
-  if (W == 2) floats(ru, u);
-  uint2 w;
-  uint32_t b = encode_quarter<FMT>(g, w);
-  size_t at = (size_t)i.r * W * it.row.d + i.c8;
-  if (i.in) {
-    q[at] = w;
-    if ((i.c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
-  }
-  if (W == 2) {
-    b = encode_quarter<FMT>(u, w);
-    at += it.row.d;
-    if (i.in) {
-      q[at] = w;
-      if ((i.c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
-    }
+  Item i[U];
+  Raw8<T> rg[U], ru[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    i[u] = item<MODE, U>(it, f, u);
+    const T* xr = x + (size_t)i[u].r * W * f;
+    rg[u] = load_raw<MODE>(xr, i[u].c(), i[u].in ? f : 0);
+    if (W == 2) ru[u] = load_raw<MODE>(xr + f, i[u].c(), i[u].in ? f : 0);
   }
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
-    else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
+  for (int n = 0; n < U; ++n) {
+    float g[8], u[8];
+    floats(rg[n], g);
+    if (W == 2) floats(ru[n], u);
+    uint2 w;
+    uint32_t b = encode_quarter<FMT>(g, w);
+    size_t at = (size_t)i[n].r * W * it.row.d + i[n].c8;
+    if (i[n].in) {
+      q[at] = w;
+      if ((i[n].c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
+    }
+    if (W == 2) {
+      b = encode_quarter<FMT>(u, w);
+      at += it.row.d;
+      if (i[n].in) {
+        q[at] = w;
+        if ((i[n].c8 & 3u) == 0) e[at >> 2] = (uint8_t)b;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
+      else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
+    }
+    tile_out<MODE>(sm, y + (size_t)i[n].r * f, i[n], f, g);
   }
-  tile_out<MODE>(sm, y + (size_t)i.r * f, i, f, g);
 }
 
 template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
                                                       const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
-  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1;
+  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = per_thread<MODE, kActBwdItems>;
   __shared__ __align__(16) T sm[Tile<T, MODE>::N];
   pdl_wait();
   pdl_trigger();
-  const Item i = item<MODE>(it, f);
-  const size_t at = i.in ? (size_t)i.r * W * it.row.d + i.c8 : 0, at2 = i.in && W == 2 ? at + it.row.d : at;
-  float g[8], u[8], t[8], a[8];
-  const Raw8<T> rt = load_raw<MODE>(dy + (size_t)i.r * f, i.c(), i.in ? f : 0);
-  const uint2 qg = q[at], qu = q[at2];
-  const uint32_t eg = e[at >> 2], eu = e[at2 >> 2];
-  floats(rt, t);
-  decode8<FMT>(qg, eg, g);
-  if (W == 2) decode8<FMT>(qu, eu, u);
+  Item i[U];
+  Raw8<T> rt[U];
+  uint2 qg[U], qu[U];
+  uint32_t eg[U], eu[U];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int n = 0; n < U; ++n) {
+    i[n] = item<MODE, U>(it, f, n);
+    const size_t at = i[n].in ? (size_t)i[n].r * W * it.row.d + i[n].c8 : 0, at2 = i[n].in && W == 2 ? at + it.row.d : at;
+    rt[n] = load_raw<MODE>(dy + (size_t)i[n].r * f, i[n].c(), i[n].in ? f : 0);
+    qg[n] = q[at];
+    eg[n] = e[at >> 2];
     if (W == 2) {
-      const float s = sigm<T>(g[k]), gs = g[k] * s, uu = u[k];
-      a[k] = gs * uu;
-      u[k] = t[k] * gs;                                    // du
-      g[k] = t[k] * uu * s * (1.f + g[k] * (1.f - s));     // dg
-    } else {
-      const float x = g[k], s = sigm<T>(2.f * kGeluK * (x + kGeluC * x * x * x));
-      a[k] = x * s;
-      g[k] = t[k] * (s + 2.f * x * s * (1.f - s) * kGeluK * (1.f + 3.f * kGeluC * x * x));
+      qu[n] = q[at2];
+      eu[n] = e[at2 >> 2];
     }
   }
-  T* dr = dx + (size_t)i.r * W * f;
-  tile_out<MODE>(sm, dr, i, f, g);
-  if (W == 2) tile_out<MODE>(sm, dr + f, i, f, u);
-  if (y) tile_out<MODE>(sm, y + (size_t)i.r * f, i, f, a);
+#pragma unroll
+  for (int n = 0; n < U; ++n) {
+    float g[8], u[8], t[8], a[8];
+    floats(rt[n], t);
+    decode8<FMT>(qg[n], eg[n], g);
+    if (W == 2) decode8<FMT>(qu[n], eu[n], u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (W == 2) {
+        const float s = sigm<T>(g[k]), gs = g[k] * s, uu = u[k];
+        a[k] = gs * uu;
+        u[k] = t[k] * gs;                                    // du
+        g[k] = t[k] * uu * s * (1.f + g[k] * (1.f - s));     // dg
+      } else {
+        const float x = g[k], s = sigm<T>(2.f * kGeluK * (x + kGeluC * x * x * x));
+        a[k] = x * s;
+        g[k] = t[k] * (s + 2.f * x * s * (1.f - s) * kGeluK * (1.f + 3.f * kGeluC * x * x));
+      }
+    }
+    T* dr = dx + (size_t)i[n].r * W * f;
+    tile_out<MODE>(sm, dr, i[n], f, g);
+    if (W == 2) tile_out<MODE>(sm, dr + f, i[n], f, u);
+    if (y) tile_out<MODE>(sm, y + (size_t)i[n].r * f, i[n], f, a);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -234,12 +285,23 @@ __global__ void __launch_bounds__(kThreads) dw_prep_k(const DwPrep p) {
   pdl_trigger();
   float f[8];
   if (blockIdx.x < p.blocks_b) {
-    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= p.nb) return;
-    const uint32_t r = p.brow.quot(i);
-    const size_t at = (size_t)r * p.gpitch + (i - r * p.brow.d);
-    decode8<FMT>(p.q[at], p.e[at >> 2], f);
-    Vec8<bf16>::store(p.B + (size_t)i * 8, f);
+    constexpr int U = kLoadItems;
+    uint2 w[U];
+    uint32_t b[U];
+    const uint32_t i0 = blockIdx.x * U * kThreads + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = min(i0 + u * kThreads, p.nb - 1), r = p.brow.quot(i);
+      const size_t at = (size_t)r * p.gpitch + (i - r * p.brow.d);
+      w[u] = p.q[at];
+      b[u] = p.e[at >> 2];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u * kThreads >= p.nb) return;
+      decode8<FMT>(w[u], b[u], f);
+      Vec8<bf16>::store(p.B + (size_t)(i0 + u * kThreads) * 8, f);
+    }
     return;
   }
   const uint32_t i = (blockIdx.x - p.blocks_b) * kThreads + threadIdx.x;
@@ -305,34 +367,35 @@ const char* const kPtrMsg = "NULL pointer, or codes that are not 16-byte aligned
 struct Shape {
   Items it;
   unsigned blocks, threads;
-  Shape(int N, int d, int mode) {
+  Shape(int N, int d, int mode, unsigned items) {
     const uint32_t pieces = (uint32_t)(pitch(d) / 8);
     it.n = (uint32_t)((size_t)N * pieces);
     it.row = FastDiv(pieces);
     threads = mode == kSingle ? std::min<unsigned>(kThreads, (pieces + 31) / 32 * 32) : kThreads;
     it.tiles = (pieces + threads - 1) / threads;
-    blocks = mode == kSingle ? (unsigned)N * it.tiles : (it.n + kThreads - 1) / kThreads;
+    const unsigned per = kThreads * items;   // of a block
+    blocks = mode == kSingle ? (unsigned)N * it.tiles : (it.n + per - 1) / per;
   }
 };
 
 template <typename T, int FMT>
 void store_t(const void* x, size_t ldx, int N, int d, int mode, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Shape h(N, d, mode);
+  const Shape h(N, d, mode, kStoreItems);
   launch_pdl(mode == kWhole ? store_k<T, FMT, kWhole> : mode == kTail ? store_k<T, FMT, kTail> : store_k<T, FMT, kSingle>, h.blocks, h.threads, 0, s, (const T*)x, ldx, d, h.it, (uint2*)q, e);
 }
 template <typename T, int FMT>
 void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, int mode, cudaStream_t s) {
-  const Shape h(N, d, mode);
+  const Shape h(N, d, mode, kLoadItems);
   launch_pdl(mode == kWhole ? load_k<T, FMT, kWhole> : mode == kTail ? load_k<T, FMT, kTail> : load_k<T, FMT, kSingle>, h.blocks, h.threads, 0, s, (const uint2*)q, e, h.it, (T*)x, ldx, d);
 }
 template <typename T, int FMT, int ACT>
 void act_t(const void* x, int N, int f, int mode, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Shape h(N, f, mode);
+  const Shape h(N, f, mode, kActItems);
   launch_pdl(mode == kWhole ? act_k<T, FMT, ACT, kWhole> : mode == kTail ? act_k<T, FMT, ACT, kTail> : act_k<T, FMT, ACT, kSingle>, h.blocks, h.threads, 0, s, (const T*)x, f, h.it, (T*)y, (uint2*)q, e);
 }
 template <typename T, int FMT, int ACT>
 void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, int mode, void* dx, void* y, cudaStream_t s) {
-  const Shape h(N, f, mode);
+  const Shape h(N, f, mode, kActBwdItems);
   launch_pdl(mode == kWhole ? act_bwd_k<T, FMT, ACT, kWhole> : mode == kTail ? act_bwd_k<T, FMT, ACT, kTail> : act_bwd_k<T, FMT, ACT, kSingle>, h.blocks, h.threads, 0, s, (const uint2*)q, e, (const T*)dy, f, h.it, (T*)dx,
              (T*)y);
 }
@@ -449,7 +512,7 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
     DwPrep r = {};
     r.q = (const uint2*)q; r.e = e; r.B = (bf16*)w; r.brow = FastDiv((uint32_t)p.Np / 8); r.gpitch = pitch(N) / 8;
     r.nb = (uint32_t)((size_t)K * (p.Np / 8));
-    r.blocks_b = (r.nb + kThreads - 1) / kThreads;
+    r.blocks_b = (r.nb + kLoadItems * kThreads - 1) / (kLoadItems * kThreads);
     r.A = A; r.Aw = (bf16*)(w + p.b); r.arow = FastDiv((uint32_t)p.Mp / 8); r.M = M; r.K = K;
     r.vec = row_mode(A, M, M, dtype) != kSingle;
     r.na = p.copy_a ? (uint32_t)((size_t)p.Kp * (p.Mp / 8)) : 0;
