@@ -98,8 +98,9 @@ __device__ __forceinline__ void codes4(uint32_t w, float* x) {
 }
 
 // 8 values of a row at column c of d. MODE kWhole: rows start on 16 bytes and d is a multiple of 8; kTail: rows start on 16
-// bytes, and all but a row's last few values are read 16 bytes at a time; kSingle: one value at a time. Columns from d on read 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread
-// are all under way before the first of them is waited for.
+// bytes, and all but a row's last few values are read 16 bytes at a time; kSingle: one value at a time. Columns from d on read
+// 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread are all under way before
+// the first of them is waited for.
 enum { kSingle = 0, kTail = 1, kWhole = 2 };
 template <typename T>
 struct Raw8;
@@ -130,7 +131,9 @@ struct Raw8<float> {
     reinterpret_cast<float4*>(p)[0] = u;
     reinterpret_cast<float4*>(p)[1] = v;
   }
-  __device__ __forceinline__ void pairs(uint64_t* f) const { f[0] = f2(u.x, u.y); f[1] = f2(u.z, u.w); f[2] = f2(v.x, v.y); f[3] = f2(v.z, v.w); }
+  __device__ __forceinline__ void pairs(uint64_t* f) const {
+    f[0] = f2(u.x, u.y); f[1] = f2(u.z, u.w); f[2] = f2(v.x, v.y); f[3] = f2(v.z, v.w);
+  }
   __device__ __forceinline__ void put(int i, float x) {
     (i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : i == 3 ? u.w : i == 4 ? v.x : i == 5 ? v.y : i == 6 ? v.z : v.w) = x;
   }

@@ -44,11 +44,11 @@ __device__ __forceinline__ void put_codes(const float* x, uint8_t* q, uint8_t* e
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows through a ring in shared memory, shared by forward and backward: a block (of as many threads as a row has 8-column
-// vectors, or half or a quarter of them) works through its rows one after another while the next rows' tensors are
-// copied in (bulk copies of whole rows on an mbarrier). What such a row costs a block is two block-wide sums, one after the
-// other, and no wait for memory; what bounds the kernel is then HBM.
-// BULK: rows start on 16 bytes; else the block copies a row itself, value by value and without running ahead.
+// Rows through a ring in shared memory, shared by forward and backward (rows of at most 8192 columns): a block, of as many
+// threads as a row has 8-column vectors or half as many, works through neighbouring rows one after another while the next
+// rows' tensors are copied in (bulk copies of whole rows on an mbarrier). What a row costs is then its block-wide sums, two
+// in turn forward and one backward, and the issue slots of its arithmetic, not the wait for memory. Rows that do not start on
+// 16 bytes, or not of whole vectors, are copied in and out by the block itself, without running ahead.
 // ------------------------------------------------------------------------------------------------
 constexpr int kStages = 4;
 
@@ -231,10 +231,14 @@ struct Params {
   }
 };
 
-// VEC: rows start on 16 bytes; they come by bulk copies. KEEP: the format that f or n are written in, -1: neither is.
-// LN: one of the norms is a LayerNorm.
+// Forward. VEC: rows come by bulk copies. KEEP: the format that f or n are written in, -1: neither is. LN: one of the norms
+// is a LayerNorm. HBM-bound on large batches, 8 bytes a value in bf16 (10.06 with both checkpoints): 4096 x 8192 with RMS
+// norms 45 us (6.0 TB/s, 88% of the measured copy rate; with checkpoints 66 us); on 2048 x 4096, where a block has six or seven
+// rows, the launch, the first rows' copies and the sums' latency show: 15.7 us (20.4 with checkpoints), LayerNorms, with four
+// sums a row, 21.1. A block for each row, which waits for it and reads the parameters anew, took 35 and 43 us.
 template <typename T, int VPT, bool VEC, bool LN, int KEEP>
-__global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80) fwd_ring_k(const Fwd a, const Ring g) {
+__global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80)
+    fwd_ring_k(const Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][2][16];
@@ -438,7 +442,7 @@ __device__ __forceinline__ void put_any(int fmt, const float* x, uint8_t* q, uin
   else put_codes<ZL_ACT8_INT8>(x, q + row * D, e + row * (D >> 5), c, D);
 }
 
-// Rows of any width: a block per row that reads it again for every sum.
+// Rows of any width (the ring kernels take up to 8192 columns): a block per row that reads it again for every sum.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   pdl_wait();
@@ -582,7 +586,8 @@ bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
 template <typename T, int VPT, bool VEC, bool LN>
 bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
   if (!a.fq && !a.nq) return fwd_ring<T, VPT, VEC, LN, -1>(a, th, s);
-  return a.fmt == ZL_ACT8_E4M3 ? fwd_ring<T, VPT, VEC, LN, ZL_ACT8_E4M3>(a, th, s) : fwd_ring<T, VPT, VEC, LN, ZL_ACT8_INT8>(a, th, s);
+  return a.fmt == ZL_ACT8_E4M3 ? fwd_ring<T, VPT, VEC, LN, ZL_ACT8_E4M3>(a, th, s)
+                               : fwd_ring<T, VPT, VEC, LN, ZL_ACT8_INT8>(a, th, s);
 }
 
 // One vector a thread up to 512 threads with RMS norms, up to 224 with a LayerNorm, whose parameters leave no second block of
@@ -866,6 +871,10 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
 // and of v fh. These are linear in m1 and m2: with g = dh' + r u,
 //   sum v fh = sum A fh g - r m1 sum A fh - r m2 sum A fh xh,   sum v = sum A g - r m1 sum A - r m2 sum A xh
 // so one barrier a row yields every mean: three sums with RMS norms, eight at most.
+// HBM-bound on large batches, 11.03 bytes a value in bf16 with f from its checkpoint: 4096 x 8192 73 us (5.1 TB/s, 75% of the
+// measured copy rate; without gradients of parameters 65 us); 2048 x 4096 27.5 us, of which the partial sums and their
+// joining kernel take 6, launch and the first rows 4; LayerNorms 33.8. Three kernels that each read the rows took 91 us, two
+// barriers a row in one kernel 38.6.
 // ------------------------------------------------------------------------------------------------
 // The normalised f, (f - pm) pr, at column c of a row in shared memory (a row of T, or of codes whose group byte is e).
 template <typename T, bool LN>
@@ -1346,14 +1355,15 @@ void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, in
 constexpr int kAnyRows = 64;      // rows of a chunk of bwd_cols_k
 // (LayerNorm's sums leave no room for two vectors a thread up to 512 threads)
 int bwd_threads(int nvec, bool ln) { return ln && nvec <= 512 ? (nvec + 31) / 32 * 32 : ring_threads(nvec); }
-// Rows of a chunk of bwd_ring_k: enough chunks for the blocks that fit on 152 SMs, but not so short that their partial sums
-// (written once and read once, 8 bytes a column and sum) weigh as much as the rows.
+// Rows of a chunk of bwd_ring_k: as many chunks as blocks fit on 152 SMs at once (4096 x 768, LayerNorms: five an SM 20.8 us,
+// four 21.5).
 int ring_rows(int N, int d, bool ln) {
-  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(4, 512 / th));
+  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
   return std::max(1, (N + 152 * per_sm - 1) / (152 * per_sm));
 }
 void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
-  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d, p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER) : kAnyRows, rows, per_group, chunks);
+  const bool ln = p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER;
+  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d, ln) : kAnyRows, rows, per_group, chunks);
 }
 
 template <typename T, int VPT, bool VEC, bool LN>
@@ -1480,7 +1490,8 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     if (!dims_ok(p)) return act8::fail(ZL_ERR_ARG, kDimsMsg);
     if ((p->post_norm != ZL_NORM_LAYER && (post_b || dpost_b)) || (p->pre_norm != ZL_NORM_LAYER && dpre_b) ||
         (!p->post_norm && (post_w || dpost_w)) || (!p->pre_norm && (pre_w || dpre_w)) || (dgate && !gate))
-      return act8::fail(ZL_ERR_ARG, "a weight or its gradient without its norm, a bias gradient without a LayerNorm, or dgate without gate");
+      return act8::fail(ZL_ERR_ARG,
+                        "a weight or its gradient without its norm, a bias gradient without a LayerNorm, or dgate without gate");
     cudaStream_t s = (cudaStream_t)stream;
     const size_t d = (size_t)p->d;
     if (p->N == 0) {
@@ -1510,7 +1521,8 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     a.alpha = p->res_scale; a.beta = p->branch_scale; a.fmt = p->fmt; a.accumulate = p->accumulate;
     plan_chunks(*p, a.rows, a.per_group, a.chunks);
     a.vec = true;
-    for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df}) a.vec &= !t || row_mode(t, d, d, p->dtype) == kWhole;
+    for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df})
+      a.vec &= !t || row_mode(t, d, d, p->dtype) == kWhole;
     a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(dgate) && al16(gate);
     const bool done = p->dtype == ZL_DTYPE_BF16 ? backward<bf16>(a, s) : backward<float>(a, s);
     const zl_status st = launched("zl_op_block_norm_bwd");

@@ -875,9 +875,11 @@ bool launch_upd(int bn, bool pair, const Args& a, const void* A, const void* B, 
 // The weight gradient from checkpoints (DW kernels).
 bool launch_dw(int bn, bool pair, const Args& a, const void* A, const void* B, cudaStream_t s) {
   if (bn == 256)
-    return pair ? launch<256, true, true, false, true, true>(a, A, B, s, 1) : launch<256, true, true, false, false, true>(a, A, B, s, 1);
+    return pair ? launch<256, true, true, false, true, true>(a, A, B, s, 1)
+                : launch<256, true, true, false, false, true>(a, A, B, s, 1);
   if (bn == 128)
-    return pair ? launch<128, true, true, false, true, true>(a, A, B, s, 1) : launch<128, true, true, false, false, true>(a, A, B, s, 1);
+    return pair ? launch<128, true, true, false, true, true>(a, A, B, s, 1)
+                : launch<128, true, true, false, false, true>(a, A, B, s, 1);
   return launch<64, true, true, false, false, true>(a, A, B, s, 2);
 }
 
@@ -1049,8 +1051,8 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
       note_launch(1);
       const size_t n8 = (size_t)M * N / 8;
       const int blocks = (int)std::min<size_t>((n8 + 255) / 256, (size_t)tc::g_sms * 8);
-      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, dw && dw->overwrite ? 3 : mode, C, bias, (const bf16*)R, alpha,
-                 rmode, a.u);
+      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, dw && dw->overwrite ? 3 : mode, C, bias,
+                 (const bf16*)R, alpha, rmode, a.u);
     }
     if (!dw) cudaFreeAsync(ws, s);
   }
