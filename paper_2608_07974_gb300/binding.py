@@ -414,8 +414,9 @@ def _rows_ptr(t, want, rows: int, cols: int, ld: int, cur: int, name: str):
         return t
     if t.dtype is not want or t.get_device() != cur:
         return _refuse(t, want, 0, cur, name)
-    if t.dim() != 2 or t.size(0) < rows or t.size(1) < cols or (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld):
-        raise ZLError(ZL_ERR_ARG, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, the call takes {rows} rows of {cols}, {ld} apart")
+    sh, st = t.shape, t.stride()
+    if len(sh) != 2 or sh[0] < rows or sh[1] < cols or (st[1] != 1 and cols > 1) or (st[0] != ld and rows > 1):
+        raise ZLError(ZL_ERR_ARG, f"{name}: shape {tuple(sh)} with strides {st}, the call takes {rows} rows of {cols}, {ld} apart")
     return t.data_ptr()
 
 

@@ -251,23 +251,20 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
 // ------------------------------------------------------------------------------------------------
 struct DwPlan {
   int Mp, Np, Kp, parts;
-  bool copy_a, pad_c;        // A through the workspace; C through a padded one
-  size_t b, a, c, splits;    // bytes of the workspace's pieces
+  bool copy_a;               // A through the workspace: cut into terms, or its rows onto 16 bytes
+  size_t b, a, splits;       // bytes of the workspace's pieces
 };
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 DwPlan dw_plan(int dtype, int M, int N, int K) {
   DwPlan p;
-  auto pad = [](int n) { return std::max(16, (n + 7) / 8 * 8); };
-  p.Mp = pad(M);
-  p.Np = pad(N);
+  p.Mp = (M + 7) / 8 * 8;
+  p.Np = (N + 7) / 8 * 8;
   p.Kp = (K + 63) / 64 * 64;
   p.parts = dtype == ZL_DTYPE_F32 ? 3 : 1;
   p.copy_a = p.parts > 1 || p.Mp != M;
-  p.pad_c = p.Mp != M || p.Np != N;
   p.b = up256((size_t)K * p.Np * 2);
   p.a = p.copy_a ? up256((size_t)p.parts * p.Kp * p.Mp * 2) : 0;
-  p.c = p.pad_c ? up256((size_t)p.Mp * p.Np * 4) : 0;
-  p.splits = up256(gemm_tc_dw_bytes(p.Mp, p.Np, K, p.parts));
+  p.splits = up256(gemm_tc_dw_bytes(M, N, K, p.parts));
   return p;
 }
 
@@ -342,26 +339,10 @@ __global__ void __launch_bounds__(kThreads) dw_prep_k(const DwPrep p) {
   }
 }
 
-// C [M, N] = or += W [., Np] (a product whose rows or columns are no multiples of 8, or fewer than 16): 4098 x 4099 over 2048
-// tokens, A copied in, C copied out, 107 us (the CUDA-core GEMM 2308).
-__global__ void __launch_bounds__(kThreads) dw_out_k(const float* __restrict__ W, int Np, float* __restrict__ C, int N,
-                                                     uint32_t n, FastDiv row, int accumulate) {
-  pdl_wait();
-  pdl_trigger();
-  const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const uint32_t r = row.quot(i);   // a thread takes every row.d-th column of a row, neighbours neighbouring ones
-  const int c = (int)(i - r * row.d);
-  float* p = C + (size_t)r * N;
-  const float* w = W + (size_t)r * Np;
-  for (int k = c; k < N; k += (int)row.d) p[k] = accumulate ? p[k] + w[k] : w[k];
-}
-
 bool act_shape(int dtype, int fmt, int N, long long d) {
   return (dtype == ZL_DTYPE_F32 || dtype == ZL_DTYPE_BF16) && (fmt == ZL_ACT8_E4M3 || fmt == ZL_ACT8_INT8) && N >= 0 &&
          N <= ZL_ACT8_MAX_ROWS && d >= 1 && d <= ZL_ACT8_MAX_COLS && (long long)N * pitch((int)d) / 8 < (1ll << 31);
 }
-// (the product's C is indexed as rows of pieces, too)
 bool dw_shape(int dtype, int fmt, int M, int N, int K) {
   return act_shape(dtype, fmt, K, N) && act_shape(dtype, fmt, K, M) && act_shape(dtype, fmt, M, N);
 }
@@ -369,7 +350,7 @@ const char* const kShapeMsg =
     "bad dtype, code format, activation or size (0 <= rows <= 2^24, 1 <= columns <= 2^20, rows x columns in whole groups "
     "below 2^34, row strides >= columns, accumulate 0 or 1)";
 bool codes_ok(const void* q, const void* e) { return q && e && ((uintptr_t)q & 15u) == 0; }
-const char* const kPtrMsg = "NULL pointer, or codes that are not 16-byte aligned";
+const char* const kPtrMsg = "NULL pointer, or codes (or A) that are not 16-byte aligned";
 
 // Items of N rows and the blocks and threads that take them.
 struct Shape {
@@ -500,7 +481,7 @@ zl_status zl_op_act8_dw_bytes(int dtype, int M, int N, int K, size_t* bytes) {
   return entry([&]() -> zl_status {
     if (!bytes || !dw_shape(dtype, ZL_ACT8_E4M3, M, N, K)) return fail(ZL_ERR_ARG, kShapeMsg);
     const DwPlan p = dw_plan(dtype, M, N, K);
-    *bytes = K ? p.b + p.a + p.c + p.splits : 0;
+    *bytes = K ? p.b + p.a + p.splits : 0;
     return ZL_OK;
   });
 }
@@ -515,10 +496,9 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
       if (!accumulate) cudaMemsetAsync(C, 0, (size_t)M * N * 4, s);
       return launched("zl_op_act8_dw");
     }
-    if (!A || !C || !codes_ok(q, e) || ((uintptr_t)A & 15u) || ((uintptr_t)C & 15u))
-      return fail(ZL_ERR_ARG, "NULL pointer, or A, C or codes that are not 16-byte aligned");
+    if (!A || !C || !codes_ok(q, e) || ((uintptr_t)A & 15u)) return fail(ZL_ERR_ARG, kPtrMsg);
     const DwPlan p = dw_plan(dtype, M, N, K);
-    if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < p.b + p.a + p.c + p.splits)
+    if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < p.b + p.a + p.splits)
       return fail(ZL_ERR_ARG, "the workspace must be 256-byte aligned and hold zl_op_act8_dw_bytes() bytes");
     uint8_t* w = (uint8_t*)ws;
     DwPrep r = {};
@@ -530,18 +510,10 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
     r.na = p.copy_a ? (uint32_t)((size_t)p.Kp * (p.Mp / 8)) : 0;
     note_launch(1);
     ZL_BY_TYPE(prep_t, dtype, fmt, r, r.blocks_b + (r.na + kThreads - 1) / kThreads, s);
-    float* out = p.pad_c ? (float*)(w + p.b + p.a) : C;
-    const GemmDw dw{p.parts, p.pad_c || !accumulate, w + p.b + p.a + p.c, p.splits};
-    if (!gemm_tc_dw(p.Mp, p.Np, K, p.copy_a ? (const void*)r.Aw : A, r.B, out, dw, s)) {
+    const GemmDw dw{p.parts, !accumulate, w + p.b + p.a, p.splits};
+    if (!gemm_tc_dw(M, N, K, p.copy_a ? (const void*)r.Aw : A, p.copy_a ? p.Mp : M, r.B, p.Np, C, dw, s)) {
       const zl_status st = launched("zl_op_act8_dw");
       return st != ZL_OK ? st : fail(ZL_ERR_CUDA, "zl_op_act8_dw: the tensor-core product could not be launched on this device");
-    }
-    if (p.pad_c) {
-      const uint32_t per_row = (uint32_t)(N + 7) / 8;
-      const uint32_t n = (uint32_t)((size_t)M * per_row);
-      note_launch(1);
-      launch_pdl(dw_out_k, (n + kThreads - 1) / kThreads, kThreads, 0, s, (const float*)out, p.Np, C, N, n, FastDiv(per_row),
-                 accumulate);
     }
     return launched("zl_op_act8_dw");
   });

@@ -634,6 +634,7 @@ struct Bwd {
   bool vec, wvec;
   int rows, per_group, chunks;   // the chunks of rows that partial sums are of
   int slots;
+  bool ring;                 // by bwd_ring_k
 };
 // Slots of a chunk's partial sums: sum dn xh, s, and with a LayerNorm sum dn, z. s = sum G fh and z = sum G where a chunk lies
 // in one gate group (per_group > 0), else both already times beta gate.
@@ -1338,17 +1339,19 @@ __global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
   }
 }
 
-// Chunks of rows for the partial sums, of about `target` rows: parts of gate groups that are as long or longer, else whole
-// groups together.
+// Chunks of rows for the partial sums, of about `target` rows: whole gate groups together, whose dgate a chunk then writes
+// itself; a group of more than twice the target is cut into chunks, and its dgate joined from theirs. (Cut from the target
+// on, many short groups each had a block of the joining kernel for every 32 columns: 140 x 7576, a gate row for each row,
+// 174 us against 31.)
 void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, int& chunks) {
   const int gr = gate_rows && gate_rows < N ? gate_rows : std::max(N, 1);
-  if (gr >= target || gr >= N) {
+  if (gr > 2 * target) {
     per_group = (gr + target - 1) / target;
     rows = (gr + per_group - 1) / per_group;
     chunks = (N + gr - 1) / gr * per_group;
   } else {
     per_group = 0;
-    rows = target / gr * gr;
+    rows = std::max(1, target / gr) * gr;
     chunks = (N + rows - 1) / rows;
   }
 }
@@ -1361,9 +1364,19 @@ int ring_rows(int N, int d, bool ln) {
   const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
   return std::max(1, (N + 152 * per_sm - 1) / (152 * per_sm));
 }
-void plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
+// What the ring kernel needs behind the ring: w_pre, A, and with gate groups within a chunk the post norm's sums.
+size_t bwd_prm(int D, bool ln, int per_group) { return (size_t)D * 4 * (2 + (per_group ? 0 : ln ? 2 : 1)); }
+// The chunks, and whether the ring kernel takes the rows: up to 8192 columns, and what does not fit in shared memory (fp32
+// LayerNorms beyond 7100 columns with several gate groups to a chunk) not.
+bool plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
   const bool ln = p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER;
-  plan_chunks(p.N, p.gate_rows, p.d <= kRingCols ? ring_rows(p.N, p.d, ln) : kAnyRows, rows, per_group, chunks);
+  if (p.d <= kRingCols) {
+    const int D = pitch(p.d);
+    plan_chunks(p.N, p.gate_rows, ring_rows(p.N, p.d, ln), rows, per_group, chunks);
+    if (4 * (size_t)D * dt_size(p.dtype) + bwd_prm(D, ln, per_group) + 4096 <= (size_t)Occupancy::kMaxSmem) return true;
+  }
+  plan_chunks(p.N, p.gate_rows, kAnyRows, rows, per_group, chunks);
+  return false;
 }
 
 template <typename T, int VPT, bool VEC, bool LN>
@@ -1371,7 +1384,7 @@ bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
   static const Occupancy occ(bwd_ring_k<T, VPT, VEC, LN>);
   if (!occ.ok) return false;
   Ring g = {};
-  const size_t prm = (size_t)a.D * 4 * (2 + (a.per_group ? 0 : LN ? 2 : 1));   // behind the ring
+  const size_t prm = bwd_prm(a.D, LN, a.per_group);
   g.pitch = (uint32_t)a.D * sizeof(T);
   g.stage = 3 * g.pitch + (a.fq ? (uint32_t)a.D : g.pitch);
   const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), (a.chunks + sm_count() - 1) / sm_count()}));
@@ -1390,7 +1403,7 @@ bool backward_as(const Bwd& a, cudaStream_t s) {
   const int groups = a.per_group ? a.chunks / a.per_group : 1;
   const dim3 join((a.D + 31) / 32, 3 + (a.dgate && groups > 1 ? std::min(groups, 60000) : 0));
   const bool sums = a.dpw || a.dpb || a.dnw || a.dnb || (a.dgate && a.per_group);   // (dgate of short groups is done by then)
-  if (a.d <= kRingCols) {
+  if (a.ring) {
     note_launch(sums ? 2 : 1);
     const int th = bwd_threads(nvec, ln);
     if (th >= nvec) {
@@ -1519,7 +1532,7 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
     a.N = p->N; a.d = p->d; a.D = act8::pitch(p->d); a.post = p->post_norm; a.pre = p->pre_norm;
     a.gate_rows = p->gate_rows < p->N ? p->gate_rows : 0;   // one group holds every row
     a.alpha = p->res_scale; a.beta = p->branch_scale; a.fmt = p->fmt; a.accumulate = p->accumulate;
-    plan_chunks(*p, a.rows, a.per_group, a.chunks);
+    a.ring = plan_chunks(*p, a.rows, a.per_group, a.chunks);
     a.vec = true;
     for (const void* t : {h_out, f, dn, dh_out, (const void*)dh, (const void*)df})
       a.vec &= !t || row_mode(t, d, d, p->dtype) == kWhole;

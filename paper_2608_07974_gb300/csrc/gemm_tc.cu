@@ -106,7 +106,8 @@ __device__ __forceinline__ void upd_apply(const GemmUpdate& u, const AdamHP& h, 
 
 struct Args {
   int M, N, K, mode;       // mode 0/1: bf16 C (+bias, +R); 2: fp32 C += acc; 3: fp32 store into split slice;
-                           // 4: the AdamW step of the tensor in `u` with this tile as (the last part of) its gradient
+                           // 4: the AdamW step of the tensor in `u` with this tile as (the last part of) its gradient;
+                           // 5 (DW): fp32 C = or += acc by plain stores, for rows that do not start on 16 bytes
   void* C;
   const float* bias;
   const bf16* R;
@@ -119,8 +120,9 @@ struct Args {
   GemmUpdate u;               // mode 4
   const float2* rope_cs;      // mode 0: rotate-half RoPE of columns < rope_cols (heads of rope_hd = 64 or 128),
   int rope_S, rope_hd, rope_cols;   // row n by position n % rope_S (NULL: none)
-  int kB, kwrap;              // DW kernels: rows and k blocks of B; A holds several such ranges one after another, all against B
-  int kb_per_seg;             // DW kernels: k blocks that one accumulation in TMEM spans; a tile's segments meet in fp32 in C
+  // DW kernels: rows and k blocks of B (A holds several such ranges one after another, all against B); the row pitches of A,
+  // B and C; k blocks that one accumulation in TMEM spans (a tile's segments meet in fp32 in C); whether mode 5 adds to C
+  int kB, kwrap, lda, ldb, ldc, kb_per_seg, add;
   int nk2;                    // modes 0/1: further k blocks, of a second product A2 B2 into the same accumulator
                               // (A2 [M, K2] K-major, B2 [K2, N] MN-major; a map's rows past K2 are zeros)
 };
@@ -605,7 +607,22 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
           }
           fence_async_smem();
           __syncwarp();
-          if (lane == 0) {
+          if (DW && g.mode == 5) {   // row by row, neighbouring lanes neighbouring columns
+            float* cp = (float*)g.C + (size_t)row0 * g.ldc + n0 + lane;
+            const int nr = n0 + lane < g.N ? min(32, g.M - row0) : 0;
+            const bool add = g.add || later;
+#pragma unroll 1
+            for (int r0 = 0; r0 < nr; r0 += 8) {
+              float o[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) o[r] = add && r0 + r < nr ? cp[(size_t)(r0 + r) * g.ldc] : 0.f;
+#pragma unroll
+              for (int r = 0; r < 8; ++r) {
+                const float v = *reinterpret_cast<const float*>(sbuf + (r0 + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4);
+                if (r0 + r < nr) cp[(size_t)(r0 + r) * g.ldc] = o[r] + v;
+              }
+            }
+          } else if (lane == 0) {
             if (row0 < g.M && n0 < g.N) {
               if (g.mode == 2) tma_reduce_add2d(&tcm, sbuf, n0, row0);
               else if (DW && later) tma_reduce_add3d(&tcm, sbuf, n0, row0, split);
@@ -658,7 +675,7 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
 }
 
 // Sums the split-K partials in split order (deterministic) and applies the epilogue (mode 4: the fused
-// optimizer step of `u`, as the fused epilogue does it; mode 3: the sum itself, fp32).
+// optimizer step of `u`, as the fused epilogue does it).
 __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M, int N, int mode, void* C,
                                 const float* __restrict__ bias, const bf16* R, float alpha, int rmode,
                                 const GemmUpdate u) {
@@ -699,8 +716,6 @@ __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M,
         const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         Vec8<float>::store(u.g + e, z);
       }
-    } else if (mode == 3) {
-      Vec8<float>::store((float*)C + e, acc);
     } else if (mode == 2) {
       float c[8];
       Vec8<float>::load((float*)C + e, c);
@@ -726,6 +741,38 @@ __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M,
       }
       Vec8<bf16>::store((bf16*)C + e, acc);
     }
+  }
+}
+
+// C [M, N] = or += the sum of `splits` partials [M, Np] in order (DW products; Np a multiple of 8, C's rows wherever they start).
+__global__ void __launch_bounds__(256) dw_reduce_k(const float* __restrict__ ws, int splits, int M, int Np, float* C, int N, int add) {
+  pdl_wait();
+  pdl_trigger();
+  const size_t MN = (size_t)M * Np;
+  const bool whole = N == Np && ((uintptr_t)C & 15u) == 0;
+  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < MN / 4; i += (size_t)gridDim.x * blockDim.x) {
+    const size_t e = 4 * i;
+    float4 s = *reinterpret_cast<const float4*>(ws + e);
+    for (int k = 1; k < splits; ++k) {
+      const float4 t = *reinterpret_cast<const float4*>(ws + k * MN + e);
+      s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+    }
+    if (whole) {
+      float4* p = reinterpret_cast<float4*>(C + e);
+      if (add) {
+        const float4 c = *p;
+        s.x += c.x; s.y += c.y; s.z += c.z; s.w += c.w;
+      }
+      *p = s;
+      continue;
+    }
+    const size_t r = e / Np;
+    const int c = (int)(e - r * Np);
+    float* p = C + r * N + c;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c + k < N) p[k] = add ? p[k] + v[k] : v[k];
   }
 }
 
@@ -755,10 +802,11 @@ bool init() {
   return true;
 }
 
-// 2-D bf16 tensor [outer, inner] (inner contiguous), box [box_outer, box_inner], 128-byte swizzle.
-bool make_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t outer, uint32_t box_inner, uint32_t box_outer) {
+// 2-D bf16 tensor [outer, inner] (inner contiguous, rows `pitch` apart: 0, inner), box [box_outer, box_inner], 128-byte swizzle.
+bool make_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t outer, uint32_t box_inner, uint32_t box_outer,
+              uint64_t pitch = 0) {
   cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {inner * 2};
+  cuuint64_t strides[1] = {(pitch ? pitch : inner) * 2};
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t es[2] = {1, 1};
   return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, es,
@@ -773,7 +821,8 @@ bool make_map_c(CUtensorMap* m, const Args& a) {
   const bool f32 = a.mode >= 2;
   const uint64_t esz = f32 ? 4 : 2;
   cuuint64_t dims[3] = {(cuuint64_t)a.N, (cuuint64_t)a.M, (cuuint64_t)a.splits};
-  cuuint64_t strides[2] = {(cuuint64_t)a.N * esz, (cuuint64_t)a.M * a.N * esz};
+  const cuuint64_t ldc = a.ldc ? a.ldc : a.N;
+  cuuint64_t strides[2] = {ldc * esz, (cuuint64_t)a.M * ldc * esz};
   cuuint32_t box[3] = {f32 ? 32u : 64u, 32u, 1u};
   cuuint32_t es[3] = {1, 1, 1};
   return g_encode(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.mode == 3 ? 3 : 2,
@@ -817,14 +866,16 @@ bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int cta
     attr = true;
   }
   CUtensorMap ta, tb;
-  const bool okA = A_MN ? make_map(&ta, A, (uint64_t)a.M, (uint64_t)a.K, 64, 64)
+  const bool okA = A_MN ? make_map(&ta, A, (uint64_t)a.M, (uint64_t)a.K, 64, 64, DW ? a.lda : 0)
                         : make_map(&ta, A, (uint64_t)a.K, (uint64_t)a.M, 64, BM);
   // a pair's CTA loads half of a K-major B tile (BN / 2 rows); MN-major B tiles are 64-column boxes
   const uint64_t kB = DW ? (uint64_t)a.kB : (uint64_t)a.K;
-  const bool okB = B_MN ? make_map(&tb, B, (uint64_t)a.N, kB, 64, 64)
+  const bool okB = B_MN ? make_map(&tb, B, (uint64_t)a.N, kB, 64, 64, DW ? a.ldb : 0)
                         : make_map(&tb, B, (uint64_t)a.K, (uint64_t)a.N, 64, PAIR ? BN / 2 : BN);
   CUtensorMap tcm;
-  if (!okA || !okB || !make_map_c(&tcm, a)) return false;
+  if (DW && a.mode == 5) tcm = ta;   // (not used)
+  else if (!make_map_c(&tcm, a)) return false;
+  if (!okA || !okB) return false;
   CUtensorMap ta2 = ta, tb2 = tb;
   if (ext && (A_MN || !make_map(&ta2, ext->A2, (uint64_t)ext->K2, (uint64_t)a.M, 64, BM) ||
               !make_map(&tb2, ext->B2, (uint64_t)a.N, (uint64_t)ext->K2, 64, 64)))
@@ -954,13 +1005,26 @@ bool gemm_tc_available() { return tc::init(); }
 
 namespace {
 
+// Test hook: ZL_GEMM_TILE = "BN:SPLITS[:PAIR]" forces the plan.
+void force_plan(tc::Plan& p, int mode, int M, int K) {
+  const char* force = std::getenv("ZL_GEMM_TILE");
+  if (!force) return;
+  int fb = 0, fs = 0, fp = -1;
+  const int nf = std::sscanf(force, "%d:%d:%d", &fb, &fs, &fp);
+  if (nf < 2 || (fb != 64 && fb != 128 && fb != 256) || fs < 1 || fs > 16) return;
+  p.bn = mode == 4 && fb == 64 ? 128 : fb;
+  p.splits = std::max(1, std::min(fs, (K + tc::BK - 1) / tc::BK));
+  p.pair = p.bn >= 128 && M > tc::BM ? 1 : 0;
+  if (nf == 3 && (fp == 0 || fp == 1)) p.pair = fp && p.bn >= 128 ? 1 : 0;
+}
+
 // Plans and launches one tensor-core GEMM (modes 0-2, or 4 with `u`); false if the shape or alignment
 // is outside the kernel's rules.
 bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C, const float* bias, const void* R,
             unsigned* err, cudaStream_t s, cudaMemPool_t pool, float alpha, int rmode, const GemmUpdate* u,
-            const GemmRope* rope = nullptr, const GemmExt* ext = nullptr, const GemmDw* dw = nullptr) {
+            const GemmRope* rope = nullptr, const GemmExt* ext = nullptr) {
   if (!tc::init()) return false;
-  if (M < 16 || N < 16 || (K < 16 && !dw)) return false;
+  if (M < 16 || N < 16 || K < 16) return false;
   auto al16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
   if (!al16(A) || !al16(B) || !al16(C) || (R && !al16(R)) || (bias && !al16(bias))) return false;   // all read 16 bytes at a time
   // the fused update: 16-byte aligned state rows, a compute copy, no accumulated gradient
@@ -976,25 +1040,14 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
   if (mode >= 2 && M % 8 != 0) return false;
   if (ext && (mode > 1 || ext->K2 < 16 || ext->K2 % 8 != 0 || !ext->A2 || !ext->B2 || !al16(ext->A2) || !al16(ext->B2)))
     return false;
-  const int kB = K, kblocks = (K + tc::BK - 1) / tc::BK;
-  if (dw && dw->parts > 1) K = dw->parts * kblocks * tc::BK;   // A's ranges, each of whole k blocks
-  const tc::Plan plan = tc::choose(mode, M, N, K, rope != nullptr);
+  tc::Plan plan = tc::choose(mode, M, N, K, rope != nullptr);
+  force_plan(plan, mode, M, K);
   int bn = plan.bn, splits = plan.splits, pair = plan.pair;
-  if (const char* force = std::getenv("ZL_GEMM_TILE")) {   // test hook "BN:SPLITS[:PAIR]": forces the plan
-    int fb = 0, fs = 0, fp = -1;
-    const int nf = std::sscanf(force, "%d:%d:%d", &fb, &fs, &fp);
-    if (nf >= 2 && (fb == 64 || fb == 128 || fb == 256) && fs >= 1 && fs <= 16) {
-      bn = mode == 4 && fb == 64 ? 128 : fb;
-      splits = std::max(1, std::min(fs, (K + tc::BK - 1) / tc::BK));
-      pair = bn >= 128 && M > tc::BM ? 1 : 0;
-      if (nf == 3 && (fp == 0 || fp == 1)) pair = fp && bn >= 128 ? 1 : 0;
-    }
-  }
   if (rope) {   // also of a forced plan: one split (the reduction does not rotate), tiles of 128 or 256 columns (heads never straddle)
     splits = 1;
     if (bn < 128) bn = 128;
   }
-  tc::Args a;
+  tc::Args a = {};
   a.M = M; a.N = N; a.K = K; a.mode = mode;
   a.rope_cs = rope ? reinterpret_cast<const float2*>(rope->cs) : nullptr;
   a.rope_S = rope ? rope->S : 1;
@@ -1010,19 +1063,13 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
   a.group_m = (a_bytes <= 48e6 || a_bytes <= b_bytes) ? a.tiles_m : std::min(8, a.tiles_m);
   if (pair) a.group_m = (a.group_m + 1) / 2;   // in pairs of tile rows
   a.nk2 = ext ? (ext->K2 + tc::BK - 1) / tc::BK : 0;
-  a.kwrap = kblocks;
-  a.kB = kB;
   const int nk = (K + tc::BK - 1) / tc::BK + a.nk2;
   a.kb_per_split = (nk + splits - 1) / splits;
   a.splits = (nk + a.kb_per_split - 1) / a.kb_per_split;   // no empty split (its slice would never be formed)
   float* ws = nullptr;
   if (a.splits > 1) {
     const size_t bytes = (size_t)a.splits * M * N * 4;
-    cudaError_t e;
-    if (dw) {   // the caller's workspace
-      ws = (float*)dw->ws;
-      e = bytes <= dw->ws_bytes ? cudaSuccess : cudaErrorMemoryAllocation;
-    } else e = pool ? cudaMallocFromPoolAsync((void**)&ws, bytes, pool, s) : cudaMallocAsync((void**)&ws, bytes, s);
+    cudaError_t e = pool ? cudaMallocFromPoolAsync((void**)&ws, bytes, pool, s) : cudaMallocAsync((void**)&ws, bytes, s);
     if (e != cudaSuccess) {   // no room for the partials: one split
       cudaGetLastError();
       ws = nullptr;
@@ -1036,14 +1083,10 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
       a.alpha = 1.f;   // applied by the reduction
     }
   }
-  const int segs = (a.kb_per_split + tc::kSegBlocks - 1) / tc::kSegBlocks;   // of equal length
-  a.kb_per_seg = (a.kb_per_split + segs - 1) / segs;
-  if (dw && dw->overwrite && !ws) a.mode = 3;   // the tiles stored where the sums would be added (one slice)
   note_launch(1);
   bool ok;
   if (mode == 0) ok = tc::launch_bn<false, false>(bn, pair, a, A, B, s, ext);
   else if (mode == 1) ok = tc::launch_bn<false, true>(bn, pair, a, A, B, s, ext);
-  else if (dw) ok = tc::launch_dw(bn, pair, a, A, B, s);
   else if (a.mode == 4) ok = tc::launch_upd(bn, pair, a, A, B, s);
   else ok = tc::launch_bn<true, true>(bn, pair, a, A, B, s);
   if (ws) {
@@ -1051,10 +1094,10 @@ bool run_tc(int mode, int M, int N, int K, const void* A, const void* B, void* C
       note_launch(1);
       const size_t n8 = (size_t)M * N / 8;
       const int blocks = (int)std::min<size_t>((n8 + 255) / 256, (size_t)tc::g_sms * 8);
-      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, dw && dw->overwrite ? 3 : mode, C, bias,
-                 (const bf16*)R, alpha, rmode, a.u);
+      launch_pdl(tc::splitk_reduce_k, blocks, 256, 0, s, ws, a.splits, M, N, mode, C, bias, (const bf16*)R, alpha,
+                 rmode, a.u);
     }
-    if (!dw) cudaFreeAsync(ws, s);
+    cudaFreeAsync(ws, s);
   }
   return ok;
 }
@@ -1067,14 +1110,63 @@ bool gemm_tc(int mode, int M, int N, int K, const void* A, const void* B, void* 
   return run_tc(mode, M, N, K, A, B, C, bias, R, err, s, pool, alpha, rmode, nullptr);
 }
 
-bool gemm_tc_dw(int M, int N, int K, const void* A, const void* B, float* C, const GemmDw& dw, cudaStream_t s) {
-  return run_tc(2, M, N, K, A, B, C, nullptr, nullptr, nullptr, s, nullptr, 1.f, 0, nullptr, nullptr, nullptr, &dw);
-}
+namespace {
+int dw_depth(int K, int parts) { return parts > 1 ? parts * ((K + tc::BK - 1) / tc::BK * tc::BK) : K; }
+}  // namespace
 
 size_t gemm_tc_dw_bytes(int M, int N, int K, int parts) {
-  if (M < 16 || N < 16 || K < 1) return 0;
-  const int sp = tc::choose(2, M, N, parts > 1 ? parts * ((K + tc::BK - 1) / tc::BK * tc::BK) : K).splits;
-  return sp > 1 ? (size_t)sp * M * N * 4 : 0;
+  const int Np = (N + 7) / 8 * 8, sp = tc::choose(2, M, Np, dw_depth(K, parts)).splits;
+  return sp > 1 ? (size_t)sp * M * Np * 4 : 0;
+}
+
+bool gemm_tc_dw(int M, int N, int K, const void* A, int lda, const void* B, int ldb, float* C, const GemmDw& dw, cudaStream_t s) {
+  auto al16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
+  if (!tc::init() || M < 1 || N < 1 || K < 1 || !al16(A) || !al16(B) || lda % 8 != 0 || ldb % 8 != 0) return false;
+  const int Np = (N + 7) / 8 * 8;
+  tc::Args a = {};
+  a.M = M; a.N = N; a.K = dw_depth(K, dw.parts);
+  a.alpha = 1.f;
+  a.rope_S = 1;
+  tc::Plan plan = tc::choose(2, M, Np, a.K);
+  force_plan(plan, 2, M, a.K);
+  const double a_bytes = (double)M * a.K * 2.0, b_bytes = (double)N * K * 2.0;   // (tile order as in run_tc)
+  a.tiles_m = (M + tc::BM - 1) / tc::BM;
+  a.tiles_n = (N + plan.bn - 1) / plan.bn;
+  a.group_m = (a_bytes <= 48e6 || a_bytes <= b_bytes) ? a.tiles_m : std::min(8, a.tiles_m);
+  if (plan.pair) a.group_m = (a.group_m + 1) / 2;
+  a.kB = K;
+  a.kwrap = (K + tc::BK - 1) / tc::BK;
+  a.lda = lda;
+  a.ldb = ldb;
+  const int nk = (a.K + tc::BK - 1) / tc::BK;
+  auto split = [&](int n) {
+    a.kb_per_split = (nk + n - 1) / n;
+    a.splits = (nk + a.kb_per_split - 1) / a.kb_per_split;
+  };
+  split(plan.splits);
+  if (a.splits > 1 && (size_t)a.splits * M * Np * 4 > dw.ws_bytes) split(1);   // (a forced plan) no room for the partials
+  const int segs = (a.kb_per_split + tc::kSegBlocks - 1) / tc::kSegBlocks;     // of equal length
+  a.kb_per_seg = (a.kb_per_split + segs - 1) / segs;
+  a.ldc = N;
+  a.C = C;
+  if (a.splits > 1) {   // partials of whole vectors, summed below
+    a.mode = 3;
+    a.C = dw.ws;
+    a.N = a.ldc = Np;
+  } else if (al16(C) && N % 4 == 0) {
+    a.mode = dw.overwrite ? 3 : 2;
+  } else {
+    a.mode = 5;
+    a.add = !dw.overwrite;
+  }
+  note_launch(1);
+  if (!tc::launch_dw(plan.bn, plan.pair, a, A, B, s)) return false;
+  if (a.splits > 1) {
+    note_launch(1);
+    const int blocks = (int)std::min<size_t>(((size_t)M * Np / 4 + 255) / 256, (size_t)tc::g_sms * 8);
+    return launch_pdl(tc::dw_reduce_k, blocks, 256, 0, s, (const float*)dw.ws, a.splits, M, Np, C, N, (int)!dw.overwrite) == cudaSuccess;
+  }
+  return true;
 }
 
 bool gemm_tc_update(int M, int N, int K, const void* A, const void* B, const GemmUpdate& u, unsigned* err,

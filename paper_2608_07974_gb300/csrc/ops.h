@@ -141,16 +141,16 @@ struct GemmExt {
 };
 bool gemm_tc_ext(int mode, int M, int N, int K, const void* A, const void* B, void* C, const float* bias, const void* R,
                  const GemmExt& e, const GemmRope* rope, unsigned* err, cudaStream_t s, cudaMemPool_t pool);
-// The weight gradient C [M, N] (fp32) = or += A^T B, bf16, on the tensor cores alone: A [parts][Kp][M], Kp = K in whole blocks
-// of 64 rows, its parts (an fp32 matrix cut into bf16 terms) summed against the same B [K, N]; parts 1: A [K, M]. Splits
-// of K use the caller's workspace (gemm_tc_dw_bytes; with less of it there is one split). M, N >= 16 and multiples of 8,
-// A, B and C 16-byte aligned; else false.
+// The weight gradient C [M, N] (fp32) = or += A^T B, bf16, on the tensor cores at any size: A [parts][Kp] rows of M values lda
+// apart, Kp = K in whole blocks of 64, its parts (an fp32 matrix cut into bf16 terms) summed against the same B [K] rows of N
+// values ldb apart; parts 1: A [K]. A and B 16-byte aligned, lda and ldb multiples of 8 (else false); C anywhere. Splits of K
+// use the caller's workspace (gemm_tc_dw_bytes; with less of it there is one split).
 struct GemmDw {
   int parts, overwrite;
   void* ws;
   size_t ws_bytes;
 };
-bool gemm_tc_dw(int M, int N, int K, const void* A, const void* B, float* C, const GemmDw& dw, cudaStream_t s);
+bool gemm_tc_dw(int M, int N, int K, const void* A, int lda, const void* B, int ldb, float* C, const GemmDw& dw, cudaStream_t s);
 size_t gemm_tc_dw_bytes(int M, int N, int K, int parts);
 // The rank-16 products of LoRA, bf16: U [N, 16] = scale * X [N, K] W [16, K]^T, and G [16, C] += U [N, 16]^T Y [N, C]
 // (fp32). False, with nothing launched, unless the row lengths are multiples of 8 and the operands 16-byte aligned.

@@ -101,7 +101,7 @@ def test_activations_refuse(B, bad):
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=-1), dict(fmt=2), dict(M=0), dict(N=0), dict(K=-1), dict(A=None), dict(q=None), dict(C=None),
-                                 dict(acc=2), dict(ws=None), dict(ws="small"), dict(A=P + 8), dict(C=P + 4)])
+                                 dict(acc=2), dict(ws=None), dict(ws="small"), dict(A=P + 8)])
 def test_weight_gradient_refuses(B, bad):
     a = dict(dtype=1, fmt=0, M=32, N=64, K=16, A=P, q=P, e=P, C=P, acc=0, ws="ok") | bad
     n = B.zl_op_act8_dw_bytes(1, 32, 64, 16)
