@@ -610,17 +610,19 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
           if (DW && g.mode == 5) {   // row by row, neighbouring lanes neighbouring columns
             float* cp = (float*)g.C + (size_t)row0 * g.ldc + n0 + lane;
             const int nr = n0 + lane < g.N ? min(32, g.M - row0) : 0;
-            const bool add = g.add || later;
-#pragma unroll 1
-            for (int r0 = 0; r0 < nr; r0 += 8) {
-              float o[8];
+            if (g.add || later) {   // every load first
+              float o[32];
 #pragma unroll
-              for (int r = 0; r < 8; ++r) o[r] = add && r0 + r < nr ? cp[(size_t)(r0 + r) * g.ldc] : 0.f;
+              for (int r = 0; r < 32; ++r) o[r] = r < nr ? cp[(size_t)r * g.ldc] : 0.f;
 #pragma unroll
-              for (int r = 0; r < 8; ++r) {
-                const float v = *reinterpret_cast<const float*>(sbuf + (r0 + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4);
-                if (r0 + r < nr) cp[(size_t)(r0 + r) * g.ldc] = o[r] + v;
-              }
+              for (int r = 0; r < 32; ++r)
+                if (r < nr)
+                  cp[(size_t)r * g.ldc] = o[r] + *reinterpret_cast<const float*>(sbuf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+            } else {
+#pragma unroll
+              for (int r = 0; r < 32; ++r)
+                if (r < nr)
+                  cp[(size_t)r * g.ldc] = *reinterpret_cast<const float*>(sbuf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
             }
           } else if (lane == 0) {
             if (row0 < g.M && n0 < g.N) {
