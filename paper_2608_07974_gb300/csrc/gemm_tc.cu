@@ -610,19 +610,20 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
           if (DW && g.mode == 5) {   // row by row, neighbouring lanes neighbouring columns
             float* cp = (float*)g.C + (size_t)row0 * g.ldc + n0 + lane;
             const int nr = n0 + lane < g.N ? min(32, g.M - row0) : 0;
+            auto staged = [&](int r) {
+              return *reinterpret_cast<const float*>(sbuf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+            };
             if (g.add || later) {   // every load first
               float o[32];
 #pragma unroll
               for (int r = 0; r < 32; ++r) o[r] = r < nr ? cp[(size_t)r * g.ldc] : 0.f;
 #pragma unroll
               for (int r = 0; r < 32; ++r)
-                if (r < nr)
-                  cp[(size_t)r * g.ldc] = o[r] + *reinterpret_cast<const float*>(sbuf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                if (r < nr) cp[(size_t)r * g.ldc] = o[r] + staged(r);
             } else {
 #pragma unroll
               for (int r = 0; r < 32; ++r)
-                if (r < nr)
-                  cp[(size_t)r * g.ldc] = *reinterpret_cast<const float*>(sbuf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                if (r < nr) cp[(size_t)r * g.ldc] = staged(r);
             }
           } else if (lane == 0) {
             if (row0 < g.M && n0 < g.N) {
@@ -747,7 +748,8 @@ __global__ void splitk_reduce_k(const float* __restrict__ ws, int splits, int M,
 }
 
 // C [M, N] = or += the sum of `splits` partials [M, Np] in order (DW products; Np a multiple of 8, C's rows wherever they start).
-__global__ void __launch_bounds__(256) dw_reduce_k(const float* __restrict__ ws, int splits, int M, int Np, float* C, int N, int add) {
+__global__ void __launch_bounds__(256) dw_reduce_k(const float* __restrict__ ws, int splits, int M, int Np, float* C, int N,
+                                                   int add) {
   pdl_wait();
   pdl_trigger();
   const size_t MN = (size_t)M * Np;
@@ -1166,7 +1168,8 @@ bool gemm_tc_dw(int M, int N, int K, const void* A, int lda, const void* B, int 
   if (a.splits > 1) {
     note_launch(1);
     const int blocks = (int)std::min<size_t>(((size_t)M * Np / 4 + 255) / 256, (size_t)tc::g_sms * 8);
-    return launch_pdl(tc::dw_reduce_k, blocks, 256, 0, s, (const float*)dw.ws, a.splits, M, Np, C, N, (int)!dw.overwrite) == cudaSuccess;
+    return launch_pdl(tc::dw_reduce_k, blocks, 256, 0, s, (const float*)dw.ws, a.splits, M, Np, C, N, (int)!dw.overwrite) ==
+           cudaSuccess;
   }
   return true;
 }
