@@ -243,8 +243,9 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
 // Weight gradient C = A^T X, X from its checkpoint, on the tensor cores in bf16. X is exactly a bf16 matrix, so it is read
 // from its codes once into a workspace (2 bytes a value, which stay in L2 for the product) and the tcgen05 GEMM does the
 // rest. An fp32 A is cut into three bf16 terms a = hi + mid + lo, each the leading 8 bits of what is left (truncated, so
-// that nothing overflows and 24 bits are covered exactly); X being exact, the three products in one fp32 accumulation are
-// the fp32 product, at a third of the bf16 rate instead of the fp32 units' (about 1/27 of it). The small terms go first.
+// that nothing overflows and 24 bits are covered exactly, down to 2^-133); X being exact, the three products in one fp32
+// accumulation are the fp32 product, at a third of the bf16 rate instead of the fp32 units' (about 1/27 of it). The small
+// terms go first.
 // Tensor-core bound: 22016 x 4096 over 2048 tokens 209 us (1.77 PFLOP/s, 92% of the measured cuBLAS burst; the workspace
 // about 5 us of it), 4096 x 4096 over 8192 tokens 190 us (the GEMM on a bf16 X 161; the workspace 16, the segments of its
 // sums the rest); fp32 2048 x 2048 over 1021 tokens 26 us (the CUDA-core GEMM 213), 8192 x 8192 over 2048 478 us;

@@ -51,7 +51,7 @@ __device__ __forceinline__ void put_codes(const float* x, uint8_t* q, uint8_t* e
 // in turn forward and one backward, and the issue slots of its arithmetic, not the wait for memory.
 // Rows that do not start on 16 bytes, or not of whole vectors, are copied in and out by the block's threads: where they are of
 // whole 4-byte words the next row is under way meanwhile (cp.async), else a row is read as it is needed. RMSNorm, 2048 rows,
-// bf16, forward and backward: 4096 columns 16 and 27 us, 4094 28 and 45 us (36 and 67 without running ahead), 4095 36 and 69.
+// bf16, forward and backward: 4096 columns 16 and 28 us, 4094 29 and 46 us (36 and 67 without running ahead), 4095 39 and 72.
 // ------------------------------------------------------------------------------------------------
 constexpr int kStages = 4;
 
@@ -408,6 +408,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
           h[j][i] = fma2(mul2(f[i], rr), pa.a[j][i], mul2(alpha, h[j][i]));
           if (LN) h[j][i] = add2(h[j][i], pa.b[j][i]);
         }
+        if (!VEC) cut<VEC>(h[j], c, a.d);   // (0 past d is NaN times 0 in a row with a NaN; the stage's next row is read with it)
         Raw8<T> out;
         pack8(h[j], out);
         if (VEC) store_raw<kWhole>((T*)a.ho + o, c, a.d, out);
@@ -440,6 +441,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
         h[j][i] = mul2(mul2(h[j][i], rr), pa.w[j][i]);
         if (LN) h[j][i] = add2(h[j][i], pa.v[j][i]);
       }
+      if (!VEC || KEEP >= 0) cut<VEC>(h[j], c, a.d);
       Raw8<T> out;
       pack8(h[j], out);
       if (VEC) store_raw<kWhole>((T*)a.no + o, c, a.d, out);
@@ -1226,6 +1228,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         }
         if (a.dh) {
           Raw8<T> out;
+          if (!VEC) cut<VEC>(v, c, a.d);   // (as in the forward)
           pack8(v, out);
           if (VEC) store_raw<kWhole>((T*)a.dh + o, c, a.d, out);
           else out.set(ring + st * g.stage + g.pitch + c * sizeof(T));
@@ -1237,6 +1240,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
           v[i] = mul2(v[i], prr);
         }
         Raw8<T> out;
+        if (!VEC) cut<VEC>(v, c, a.d);
         pack8(v, out);
         if (VEC) store_raw<kWhole>((T*)a.df + o, c, a.d, out);
         else out.set(ring + st * g.stage + c * sizeof(T));

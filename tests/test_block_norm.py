@@ -345,6 +345,43 @@ def test_rows_of_zeros_and_nan(B, dtype):
     assert torch.equal(torch.isfinite(df).all(1), ok)
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("post,pre", [(R.RMS, R.RMS), (R.LAYER, R.LAYER), (R.NONE, R.RMS)])
+@pytest.mark.parametrize("d", [35, 38, 40, 64])
+def test_nan_rows_among_many(B, dtype, post, pre, d):
+    """Rows with a NaN or an infinity among many (a block takes several): every other row keeps its bits, in shapes whose rows
+    end inside a vector, a word or a group of the codes; columns past d of the codes stay 0."""
+    c, N, T = setting(post, pre), 20000, R.DT[dtype]
+    g = torch.Generator().manual_seed(d)
+    h, f, dn, dho = (acts(N, d, dtype, g).cuda() for _ in range(4))
+    bad = torch.zeros(N, dtype=torch.bool, device="cuda")
+    bad[3::7] = True
+    p = dims(B, dtype, c, N, d)
+    D = (d + 31) // 32 * 32
+    ws = torch.empty(B.zl_op_block_norm_bwd_bytes(p), dtype=torch.uint8, device="cuda")
+
+    def run(f, h):
+        ho, n, dh, df = (torch.empty(N, d, dtype=T, device="cuda") for _ in range(4))
+        st, (fq, fe), (nq, ne) = torch.empty(4, N, device="cuda"), codes(N, d), codes(N, d)
+        B.zl_op_block_norm(p, h, f, None, None, None, None, None, ho, n, st, fq, fe, nq, ne)
+        B.zl_op_block_norm_bwd(p, ho, f, None, None, None, None, None, None, st, dn, dho, dh, df, None, None, None, None, None, ws)
+        torch.cuda.synchronize()
+        return ho, n, dh, df, fq, fe, nq, ne, st.t().contiguous()
+
+    clean = run(f, h)
+    f2, h2 = f.clone(), h.clone()
+    f2[3::14, d // 2] = float("nan")
+    h2[10::14, d - 1] = float("inf")
+    spoilt = run(f2, h2)
+    for a, b in zip(clean, spoilt):
+        a, b = a.view(N, -1), b.view(N, -1)
+        assert torch.equal(a[~bad], b[~bad])
+    for k in (4, 6):
+        assert not bool(spoilt[k].view(N, D)[:, d:].any())
+    assert not bool(torch.isfinite(spoilt[1][bad]).all(1).any()) and not bool(torch.isfinite(spoilt[3][3::14]).all(1).any())
+
+
 # ---- together --------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
