@@ -229,7 +229,8 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
       } else {
         const float x = g[k], s = sigm<T>(2.f * kGeluK * (x + kGeluC * x * x * x));
         a[k] = x * s;
-        g[k] = t[k] * (s + 2.f * x * s * (1.f - s) * kGeluK * (1.f + 3.f * kGeluC * x * x));
+        // (s (1 - s) is 0 long before 2 x or x^2 overflows: with finite factors their product is 0, not NaN)
+        g[k] = t[k] * (s + 2.f * kGeluK * (s * (1.f - s) * x) * (1.f + 3.f * kGeluC * fminf(x * x, 1e30f)));
       }
     }
     T* dr = dx + (size_t)i[n].r * W * f;

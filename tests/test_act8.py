@@ -333,6 +333,35 @@ def test_activation_keeps_nan(B):
     assert int(bad.sum()) == 5
 
 
+@gpu
+@pytest.mark.parametrize("dtype,fmt", [("f32", R.E4M3), ("bf16", R.INT8)])
+@pytest.mark.parametrize("kind", [R.SWIGLU, R.GELU])
+def test_activation_of_large_values(B, dtype, fmt, kind):
+    """Values whose square and cube overflow, a group of 32 columns for each: an activation is 0 or its input (times up) and
+    its derivative 0 or 1 (times up). Sigmoids above are 1 in fp32; below, that of -64 is e^-64 = 1.6e-28 (SwiGLU; GELU's
+    argument is the cube), times at most 64 below 1.1e-26, and the others are 0."""
+    T = R.DT[dtype]
+    mags = torch.tensor([2.0 ** k for k in (6, 20, 43, 64, 90, 127)])
+    v = torch.cat([mags, -mags])
+    x = v.repeat_interleave(32).view(1, -1).to(T)
+    f, w = x.shape[1], 2 if kind == R.SWIGLU else 1
+    full = torch.cat([x, torch.full_like(x, 0.5)], 1) if w == 2 else x
+    y, dx, again = (torch.full((1, n), 7.0, dtype=T, device="cuda") for n in (f, w * f, f))
+    q, e = empty_codes(w, f)
+    B.zl_op_act8_act(code(B, dtype), kind, fmt, full.cuda(), 1, f, y, q, e)
+    B.zl_op_act8_act_bwd(code(B, dtype), kind, fmt, q, e, torch.full((1, f), 0.25, dtype=T, device="cuda"), 1, f, dx, again)
+    up = 0.5 if w == 2 else 1.0
+    want = torch.where(x > 0, x * up, torch.zeros_like(x))
+
+    def same(got, want):
+        return bool(((got.cpu().double() - want.double()).abs() <= 1.1e-26).all())
+
+    assert same(y, want) and same(again, want)
+    assert same(dx[:, :f], torch.where(x > 0, 0.25 * up, 0.0))
+    if w == 2:
+        assert same(dx[:, f:], 0.25 * torch.where(x > 0, x, torch.zeros_like(x)))
+
+
 # ---- weight gradient ----------------------------------------------------------------------------
 DWS = [(1, 1, 1), (16, 16, 16), (24, 40, 1), (8, 32, 5), (130, 72, 50), (256, 128, 203), (33, 65, 77), (384, 1000, 129), (257, 96, 1021), (768, 768, 4096),
        (130, 770, 300)]
