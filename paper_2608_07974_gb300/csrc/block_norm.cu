@@ -1282,130 +1282,177 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
 
 // The gradients from the chunks' partial sums: a block takes 32 columns (8 lanes of four), 32 lanes of chunks each adding every
 // 32nd one, eight of them under way together, then the lanes' sums in a fixed tree. blockIdx.y 0: the post norm's gradients,
-// and dgate where there is one gate group (or none); 1, 2: the pre norm's; 3 + g: dgate of group g where there are several.
+// and dgate where there is one gate group (or none); 1, 2: the pre norm's; 3 + g: dgate of group g where there are a few. Where
+// there are more, of fewer chunks each, the lanes of y = 0 take whole groups and write their dgate on the way: 2048 x 4096, 8
+// groups of 38 chunks, 28.4 us against 32.5 with blocks for each group (32 groups of 8 chunks 27.4, 54 with blocks and more
+// chunks than run at once); 4096 x 768, 8 groups of 95 chunks, 24.4 against 21.4, and 4 of 76 (2048 x 4096) 31.0 against 30.2.
 // Bound by latency (launch, one round of loads from L2, stores: 5 us at 128 x 4096): one wave of small blocks, what the last
 // step reads besides is read first.
+__host__ __device__ __forceinline__ bool many_groups(int groups, int per_group) { return groups > 1 && per_group <= 6 * groups; }
 template <bool LN>
 __global__ void __launch_bounds__(256) bwd_join_k(const Bwd a) {
   pdl_wait();
   pdl_trigger();
   __shared__ float4 sh[LN ? 2 : 1][32][9];
   constexpr int U = 8;
-  const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, c = blockIdx.x * 32 + tx * 4;
+  const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, y = blockIdx.y, c = blockIdx.x * 32 + tx * 4;
   const int col = blockIdx.x * 32 + ty;   // of the last step, eight threads to a column
   const int groups = a.per_group ? a.chunks / a.per_group : 1;
-  const bool gvec = a.wvec && a.d % 4 == 0 && c < a.d, one = a.per_group && groups == 1;
+  const bool gvec = a.wvec && a.d % 4 == 0 && c < a.d, one = a.per_group && groups == 1, many = many_groups(groups, a.per_group);
+  const bool two = LN && (y == 0 || y > 2);
+  if (y == 0 ? !a.dpw && !a.dpb && !(a.dgate && (one || many)) : y == 1 ? !a.dnw : y == 2 && !a.dnb) return;
   float pw = 1.f, pb = 0.f, gt = 1.f;
   if (tx == 0 && col < a.d) {
     if (a.pw) pw = a.pw[col];
     if (LN && a.pb) pb = a.pb[col];
     if (one && a.gate) gt = a.gate[col];
   }
-  for (int y = blockIdx.y; y < 3 + (a.dgate && groups > 1 ? groups : 0); y += gridDim.y) {
-    const bool two = LN && (y == 0 || y > 2);
-    if (y == 0 ? !a.dpw && !a.dpb && !(a.dgate && one) : y == 1 ? !a.dnw : y == 2 && !a.dnb) continue;
-    const int b0 = y > 2 ? (y - 3) * a.per_group : 0, b1 = y > 2 ? b0 + a.per_group : a.chunks;
-    const int slot = y == 1 ? kDw : y == 2 ? kDb : kS;
-    const bool weigh = y == 0 && a.per_group && groups > 1 && a.gate;   // every chunk's sums times its gate row
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f), z = s;
-    for (int b = b0 + ty; b < b1; b += 32 * U) {
-      float4 v[U], w[LN ? U : 1];
+  auto four = [&](const float* p, float none) {   // of a row of parameters, at column c
+    float4 v = make_float4(none, none, none, none);
+    if (!p) return v;
+    if (gvec) return *reinterpret_cast<const float4*>(p + c);
+    if (c < a.d) v.x = p[c];
+    if (c + 1 < a.d) v.y = p[c + 1];
+    if (c + 2 < a.d) v.z = p[c + 2];
+    if (c + 3 < a.d) v.w = p[c + 3];
+    return v;
+  };
+  auto add = [](float4& s, const float4& v) { s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; };
+  auto scale = [](float4& v, const float4& g) { v.x *= g.x; v.y *= g.y; v.z *= g.z; v.w *= g.w; };
+  // the partial sums of chunks b, b + step .. below b1 (at most U of them) at once
+  auto load = [&](int slot, int b, int step, int b1, float4* v, float4* w) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (LN) w[u] = v[u];
-        if (b + 32 * u < b1) {
-          const float* p = a.part + ((size_t)(b + 32 * u) * a.slots + slot) * a.D + c;
-          v[u] = *reinterpret_cast<const float4*>(p);
-          if (two) w[u] = *reinterpret_cast<const float4*>(p + (kZ - kS) * (size_t)a.D);
+    for (int u = 0; u < U; ++u) {
+      v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (LN) w[u] = v[u];
+      if (b + step * u < b1) {
+        const float* p = a.part + ((size_t)(b + step * u) * a.slots + slot) * a.D + c;
+        v[u] = *reinterpret_cast<const float4*>(p);
+        if (two) w[u] = *reinterpret_cast<const float4*>(p + (kZ - kS) * (size_t)a.D);
+      }
+    }
+  };
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f), z = s, v[U], w[LN ? U : 1];
+  if (y == 0 && many) {
+    const float4 pw4 = four(a.pw, 1.f), pb4 = four(LN ? a.pb : nullptr, 0.f);
+    for (int g = ty; g < groups; g += 32) {
+      float4 gs = make_float4(0.f, 0.f, 0.f, 0.f), gz = gs;
+      const float4 gate = four(a.gate ? a.gate + (size_t)g * a.d : nullptr, 1.f);
+      const int end = (g + 1) * a.per_group;
+      for (int b = g * a.per_group; b < end; b += U) {
+        load(kS, b, 1, end, v, w);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          add(gs, v[u]);
+          if (LN) add(gz, w[u]);
         }
       }
+      if (a.dgate) {
+        float* q = a.dgate + (size_t)g * a.d;
+        float4 r = gs;
+        scale(r, pw4);
+        if (LN) { r.x += pb4.x * gz.x; r.y += pb4.y * gz.y; r.z += pb4.z * gz.z; r.w += pb4.w * gz.w; }
+        scale(r, make_float4(a.beta, a.beta, a.beta, a.beta));
+        if (a.accumulate) add(r, four(q, 0.f));
+        if (gvec) {
+          *reinterpret_cast<float4*>(q + c) = r;
+        } else {
+          if (c < a.d) q[c] = r.x;
+          if (c + 1 < a.d) q[c + 1] = r.y;
+          if (c + 2 < a.d) q[c + 2] = r.z;
+          if (c + 3 < a.d) q[c + 3] = r.w;
+        }
+      }
+      scale(gs, gate);
+      add(s, gs);
+      if (LN) {
+        scale(gz, gate);
+        add(z, gz);
+      }
+    }
+    if (!a.dpw && !a.dpb) return;
+  } else {
+    const int b0 = y > 2 ? (y - 3) * a.per_group : 0, b1 = y > 2 ? b0 + a.per_group : a.chunks;
+    const bool weigh = y == 0 && a.per_group && groups > 1 && a.gate;   // every chunk's sums times its gate row
+    for (int b = b0 + ty; b < b1; b += 32 * U) {
+      load(y == 1 ? kDw : y == 2 ? kDb : kS, b, 32, b1, v, w);
       if (weigh) {
         float4 g[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float* gr = a.gate + (size_t)((b + 32 * u) / a.per_group) * a.d + c;
-          g[u] = make_float4(1.f, 1.f, 1.f, 1.f);
-          if (b + 32 * u >= b1) continue;
-          if (gvec) g[u] = *reinterpret_cast<const float4*>(gr);
-          else {
-            if (c < a.d) g[u].x = gr[0];
-            if (c + 1 < a.d) g[u].y = gr[1];
-            if (c + 2 < a.d) g[u].z = gr[2];
-            if (c + 3 < a.d) g[u].w = gr[3];
-          }
-        }
+        for (int u = 0; u < U; ++u)
+          g[u] = four(b + 32 * u < b1 ? a.gate + (size_t)((b + 32 * u) / a.per_group) * a.d : nullptr, 1.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          v[u].x *= g[u].x; v[u].y *= g[u].y; v[u].z *= g[u].z; v[u].w *= g[u].w;
-          if (LN) { w[u].x *= g[u].x; w[u].y *= g[u].y; w[u].z *= g[u].z; w[u].w *= g[u].w; }
+          scale(v[u], g[u]);
+          if (LN) scale(w[u], g[u]);
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w;
-        if (LN) { z.x += w[u].x; z.y += w[u].y; z.z += w[u].z; z.w += w[u].w; }
+        add(s, v[u]);
+        if (LN) add(z, w[u]);
       }
     }
-    __syncthreads();
-    sh[0][ty][tx] = s;
-    if (LN) sh[LN ? 1 : 0][ty][tx] = z;
-    __syncthreads();
-    // column ty of the block's 32: thread tx of eight takes lanes 4 tx .. 4 tx + 3
-    float sv = 0.f, zv = 0.f;
+  }
+  sh[0][ty][tx] = s;
+  if (LN) sh[LN ? 1 : 0][ty][tx] = z;
+  __syncthreads();
+  // column ty of the block's 32: thread tx of eight takes lanes 4 tx .. 4 tx + 3
+  float sv = 0.f, zv = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sv += reinterpret_cast<const float*>(&sh[0][4 * tx + i][0])[ty];
-      if (LN) zv += reinterpret_cast<const float*>(&sh[LN ? 1 : 0][4 * tx + i][0])[ty];
-    }
+  for (int i = 0; i < 4; ++i) {
+    sv += reinterpret_cast<const float*>(&sh[0][4 * tx + i][0])[ty];
+    if (LN) zv += reinterpret_cast<const float*>(&sh[LN ? 1 : 0][4 * tx + i][0])[ty];
+  }
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) {
-      sv += __shfl_xor_sync(0xffffffffu, sv, o);
-      if (LN) zv += __shfl_xor_sync(0xffffffffu, zv, o);
-    }
-    if (tx != 0 || col >= a.d) continue;
-    auto put = [&](float* o, float v) {
-      if (o) o[col] = a.accumulate ? o[col] + v : v;
-    };
-    if (y == 1) put(a.dnw, sv);
-    else if (y == 2) put(a.dnb, sv);
+  for (int o = 4; o > 0; o >>= 1) {
+    sv += __shfl_xor_sync(0xffffffffu, sv, o);
+    if (LN) zv += __shfl_xor_sync(0xffffffffu, zv, o);
+  }
+  if (tx != 0 || col >= a.d) return;
+  auto put = [&](float* o, float v) {
+    if (o) o[col] = a.accumulate ? o[col] + v : v;
+  };
+  if (y == 1) put(a.dnw, sv);
+  else if (y == 2) put(a.dnb, sv);
+  else {
+    const float dg = a.beta * (pw * sv + pb * zv);
+    if (y > 2) put(a.dgate + (size_t)(y - 3) * a.d, dg);
     else {
-      const float dg = a.beta * (pw * sv + pb * zv);
-      if (y > 2) put(a.dgate + (size_t)(y - 3) * a.d, dg);
-      else {
-        if (one) put(a.dgate, dg);
-        const float f = a.per_group ? a.beta * gt : 1.f;
-        put(a.dpw, f * sv);
-        put(a.dpb, f * zv);
-      }
+      if (one) put(a.dgate, dg);
+      const float f = a.per_group ? a.beta * gt : 1.f;
+      put(a.dpw, f * sv);
+      put(a.dpb, f * zv);
     }
   }
 }
 
-// Chunks of rows for the partial sums, of about `target` rows: whole gate groups together, whose dgate a chunk then writes
-// itself; a group of more than twice the target is cut into chunks, and its dgate joined from theirs. (Cut from the target
-// on, many short groups each had a block of the joining kernel for every 32 columns: 140 x 7576, a gate row for each row,
-// 174 us against 14.)
-void plan_chunks(int N, int gate_rows, int target, int& rows, int& per_group, int& chunks) {
+// Chunks of rows for the partial sums, `slots` of them at most where that is possible (the blocks that run at once): whole gate
+// groups together, whose dgate a chunk then writes itself, or where a group has more than twice the rows of an even share,
+// groups cut into equal chunks, their dgate joined from these (2048 x 4096 bf16: a gate row for each row 51 us, for 3, 32, 64 rows
+// 37, 28, 27; chunks of a fixed length, more than run at once, 47, 78, 54). A row for each chunk only up to 256 rows: beyond, the
+// join's reads cost more than a second row (512 x 768 fp32, LayerNorms 12.1 us against 9.0; 128 x 4096 8.5 against 9.5).
+void plan_chunks(int N, int gate_rows, int slots, int& rows, int& per_group, int& chunks) {
   const int gr = gate_rows && gate_rows < N ? gate_rows : std::max(N, 1);
-  if (gr > 2 * target) {
-    per_group = (gr + target - 1) / target;
+  const int share = std::max(N > 256 ? 2 : 1, (N + slots - 1) / slots);
+  if (gr > 2 * share) {
+    const int groups = (N + gr - 1) / gr;
+    per_group = std::min((gr + share - 1) / share, std::max(1, slots / groups));
     rows = (gr + per_group - 1) / per_group;
-    chunks = (N + gr - 1) / gr * per_group;
+    per_group = (gr + rows - 1) / rows;
+    chunks = groups * per_group;
   } else {
     per_group = 0;
-    rows = std::max(1, target / gr) * gr;
+    rows = (share + gr - 1) / gr * gr;
     chunks = (N + rows - 1) / rows;
   }
 }
 constexpr int kAnyRows = 64;      // rows of a chunk of bwd_cols_k
 // (LayerNorm's sums leave no room for two vectors a thread up to 512 threads)
 int bwd_threads(int nvec, bool ln) { return ln && nvec <= 512 ? (nvec + 31) / 32 * 32 : ring_threads(nvec); }
-// Rows of a chunk of bwd_ring_k: as many chunks as blocks fit on 152 SMs at once (4096 x 768, LayerNorms: five an SM 20.8 us,
-// four 21.5).
-int ring_rows(int N, int d, bool ln) {
-  const int th = bwd_threads(pitch(d) / 8, ln), per_sm = std::max(1, std::min(8, 512 / th));
-  return std::max(1, (N + 152 * per_sm - 1) / (152 * per_sm));
+// Chunks of bwd_ring_k: as many as blocks fit on 152 SMs at once (4096 x 768, LayerNorms: five an SM 20.8 us, four 21.5).
+int ring_slots(int d, bool ln) {
+  return 152 * std::max(1, std::min(8, 512 / bwd_threads(pitch(d) / 8, ln)));
 }
 // What the ring kernel needs behind the ring: w_pre, A, and with gate groups within a chunk the post norm's sums.
 size_t bwd_prm(int D, bool ln, int per_group) { return (size_t)D * 4 * (2 + (per_group ? 0 : ln ? 2 : 1)); }
@@ -1415,10 +1462,10 @@ bool plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks)
   const bool ln = p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER;
   if (p.d <= kRingCols) {
     const int D = pitch(p.d);
-    plan_chunks(p.N, p.gate_rows, ring_rows(p.N, p.d, ln), rows, per_group, chunks);
+    plan_chunks(p.N, p.gate_rows, ring_slots(p.d, ln), rows, per_group, chunks);
     if (4 * (size_t)D * dt_size(p.dtype) + bwd_prm(D, ln, per_group) + 4096 <= (size_t)Occupancy::kMaxSmem) return true;
   }
-  plan_chunks(p.N, p.gate_rows, kAnyRows, rows, per_group, chunks);
+  plan_chunks(p.N, p.gate_rows, std::max(1, (p.N + kAnyRows - 1) / kAnyRows), rows, per_group, chunks);
   return false;
 }
 
@@ -1444,7 +1491,7 @@ bool backward_as(const Bwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
   const bool ln = a.slots > 2;
   const int groups = a.per_group ? a.chunks / a.per_group : 1;
-  const dim3 join((a.D + 31) / 32, 3 + (a.dgate && groups > 1 ? std::min(groups, 60000) : 0));
+  const dim3 join((a.D + 31) / 32, 3 + (a.dgate && groups > 1 && !many_groups(groups, a.per_group) ? groups : 0));
   const bool sums = a.dpw || a.dpb || a.dnw || a.dnb || (a.dgate && a.per_group);   // (dgate of short groups is done by then)
   if (a.ring) {
     note_launch(sums ? 2 : 1);

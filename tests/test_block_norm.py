@@ -299,6 +299,19 @@ def test_gate_groups(B, rows):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("post,pre", [(R.RMS, R.RMS), (R.LAYER, R.RMS), (R.NONE, R.LAYER)])
+@pytest.mark.parametrize("N,d,rows", [(1300, 520, 26), (1300, 1001, 9), (700, 2056, 31), (2500, 33, 300), (5000, 16400, 129)])
+def test_many_gate_groups(B, dtype, post, pre, N, d, rows):
+    """More than a few groups, each cut into chunks of rows, the last one short; the last shape beyond the ring kernels' width."""
+    if d == 16400 and (dtype == "f32" or post != R.RMS):
+        N = 1500
+    check_backward(B, dtype, setting(post, pre, rows=rows), N, d, R.E4M3, accumulate=1)
+    check_backward(B, dtype, setting(post, pre, rows=rows), N, d, R.INT8, subset=("dgate",))
+    check_backward(B, dtype, setting(post, pre, rows=rows), N, d, R.INT8, subset=("dpost_w",))
+
+
+@gpu
 def test_backward_repeats_bit_for_bit(B):
     a = check_backward(B, "bf16", setting(R.LAYER, R.RMS, rows=100), 517, 1032, R.INT8)
     b = check_backward(B, "bf16", setting(R.LAYER, R.RMS, rows=100), 517, 1032, R.INT8)
