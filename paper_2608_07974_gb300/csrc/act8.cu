@@ -14,62 +14,47 @@ using namespace act8;
 constexpr int kThreads = 256;
 
 // Items of a kernel over the 8-column pieces of N rows in whole groups, four neighbouring lanes to a group: every lane of
-// a warp runs the code, `in` says whether its item exists. Rows that do not start on 16 bytes (MODE kSingle) are written
-// through shared memory, a tile of a row to a block (2048 x 22001 from integer codes 111 -> 44 us); they are read value by
-// value, which L1 makes up for (29 us to write such rows as codes; through shared memory 54).
+// a warp runs the code, `in` says whether its item exists. Rows that do not start on 16 bytes (MODE kSingle) are read and
+// written in whole 16-byte words all the same, shifted between neighbouring lanes: 2048 x 22001 bf16 to integer codes 25 us, back
+// 34 (value by value 29 and 111, written through shared memory 43); SwiGLU of 2048 x 11001 46 and 55 us.
 struct Items {
   uint32_t n;      // N * D / 8, below 2^31
   FastDiv row;     // D / 8 pieces to a row
-  uint32_t tiles;  // kSingle: blocks to a row
 };
 struct Item {
   uint32_t r, c8, at;   // row, piece of it, r * (D / 8) + c8
   bool in;
-  int c0, cols;         // kSingle: first column of the block's tile, columns of the row in it
   __device__ __forceinline__ int c() const { return (int)c8 * 8; }
 };
 // Items of a thread: their loads are under way together (2048 x 22016 bf16 to e4m3 24.7 / 21.2 / 22.5 us with one, two, four,
 // back 24.6 / 21.1 / 21.7; SwiGLU forward of 2048 x 11008 32.2 / 29.5 with one, two; the backward, with more streams an item
-// and more registers, gains nothing).
-constexpr int kStoreItems = 2, kLoadItems = 2, kActItems = 2, kActBwdItems = 1;
-template <int MODE, int U>
-constexpr int per_thread = MODE == kSingle ? 1 : U;
+// and more registers, gains nothing). Of rows off 16 bytes (kSingle) the activations take one forward, whose inputs then fill
+// the registers (2048 x 4097 fp32 27.6 us with two, 23.6 with one), and two backward (32.3 with one, 29.3 with two).
+constexpr int kStoreItems = 2, kLoadItems = 2;
+constexpr int act_items(int mode) { return mode == kSingle ? 1 : 2; }
+constexpr int act_bwd_items(int mode) { return mode == kSingle ? 2 : 1; }
 // Item u of U.
-template <int MODE, int U>
-__device__ __forceinline__ Item item(const Items& it, int d, int u) {
+template <int U>
+__device__ __forceinline__ Item item(const Items& it, int u) {
   Item x;
-  if (MODE != kSingle) {
-    x.at = (blockIdx.x * U + u) * kThreads + threadIdx.x;
-    x.in = x.at < it.n;
-    x.r = x.in ? it.row.quot(x.at) : 0;
-    x.c8 = x.at - x.r * it.row.d;
-    x.c0 = x.cols = 0;
-    return x;
-  }
-  x.r = blockIdx.x / it.tiles;
-  const uint32_t tile = blockIdx.x - x.r * it.tiles;
-  x.c8 = tile * blockDim.x + threadIdx.x;
-  x.in = x.c8 < it.row.d;
-  x.at = x.r * it.row.d + x.c8;
-  x.c0 = (int)(tile * blockDim.x * 8);
-  x.cols = max(0, min(d - x.c0, (int)blockDim.x * 8));
+  x.at = (blockIdx.x * U + u) * kThreads + threadIdx.x;
+  x.in = x.at < it.n;
+  x.r = x.in ? it.row.quot(x.at) : 0;
+  x.c8 = x.in ? x.at - x.r * it.row.d : 0;
   return x;
 }
-// One tile of a row in shared memory (nothing where rows start on 16 bytes).
-template <typename T, int MODE>
-struct Tile {
-  static constexpr int N = MODE == kSingle ? kThreads * 8 : 8;
-};
 template <int MODE, typename T>
-__device__ __forceinline__ void tile_out(T* sm, T* p, const Item& x, int d, const float* f) {
-  if (MODE != kSingle) {
-    if (x.in) store8<MODE>(p, x.c(), d, f);
-    return;
+__device__ __forceinline__ void item_out(T* p, const Item& x, int d, const float* f) {
+  if (MODE == kSingle) {
+    uint64_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+    Raw8<T> r;
+    pack8(v, r);
+    store_any(p, x.c(), x.in ? d : 0, r);
+  } else if (x.in) {
+    store8<MODE>(p, x.c(), d, f);
   }
-  store8<kTail>(sm, x.c() - x.c0, x.cols, f);
-  __syncthreads();
-  row_out(p + x.c0, sm, x.cols, (int)threadIdx.x, (int)blockDim.x);
-  __syncthreads();
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -80,20 +65,20 @@ __device__ __forceinline__ void tile_out(T* sm, T* p, const Item& x, int d, cons
 template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, size_t ldx, int d, Items it, uint2* __restrict__ q,
                                                     uint8_t* __restrict__ e) {
-  constexpr int U = per_thread<MODE, kStoreItems>;
+  constexpr int U = kStoreItems;
   pdl_wait();
   pdl_trigger();
   Item i[U];
-  Raw8<T> r[U];
+  Piece<MODE, T> r[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    i[u] = item<MODE, U>(it, d, u);
-    r[u] = load_raw<MODE>(x + i[u].r * ldx, i[u].c(), i[u].in ? d : 0);
+    i[u] = item<U>(it, u);
+    r[u].load(x + i[u].r * ldx, i[u].c(), i[u].in ? d : 0);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float f[8];
-    floats(r[u], f);
+    r[u].floats(f);
     uint2 w;
     const uint32_t b = encode_quarter<FMT>(f, w);
     if (i[u].in) {
@@ -106,8 +91,7 @@ __global__ void __launch_bounds__(kThreads) store_k(const T* __restrict__ x, siz
 template <typename T, int FMT, int MODE>
 __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e, Items it,
                                                    T* __restrict__ x, size_t ldx, int d) {
-  constexpr int U = per_thread<MODE, kLoadItems>;
-  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
+  constexpr int U = kLoadItems;
   pdl_wait();
   pdl_trigger();
   Item i[U];
@@ -115,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, 
   uint32_t b[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    i[u] = item<MODE, U>(it, d, u);
+    i[u] = item<U>(it, u);
     const uint32_t at = i[u].in ? i[u].at : 0;
     w[u] = q[at];
     b[u] = e[at >> 2];
@@ -124,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, 
   for (int u = 0; u < U; ++u) {
     float f[8];
     decode8<FMT>(w[u], b[u], f);
-    tile_out<MODE>(sm, x + i[u].r * ldx, i[u], d, f);
+    item_out<MODE>(x + i[u].r * ldx, i[u], d, f);
   }
 }
 
@@ -147,24 +131,23 @@ constexpr float kGeluK = 0.7978845608028654f, kGeluC = 0.044715f;
 template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f, Items it, T* __restrict__ y,
                                                   uint2* __restrict__ q, uint8_t* __restrict__ e) {
-  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = per_thread<MODE, kActItems>;
-  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
+  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = act_items(MODE);
   pdl_wait();
   pdl_trigger();
   Item i[U];
-  Raw8<T> rg[U], ru[U];
+  Piece<MODE, T> rg[U], ru[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    i[u] = item<MODE, U>(it, f, u);
+    i[u] = item<U>(it, u);
     const T* xr = x + (size_t)i[u].r * W * f;
-    rg[u] = load_raw<MODE>(xr, i[u].c(), i[u].in ? f : 0);
-    if (W == 2) ru[u] = load_raw<MODE>(xr + f, i[u].c(), i[u].in ? f : 0);
+    rg[u].load(xr, i[u].c(), i[u].in ? f : 0);
+    if (W == 2) ru[u].load(xr + f, i[u].c(), i[u].in ? f : 0);
   }
 #pragma unroll
   for (int n = 0; n < U; ++n) {
     float g[8], u[8];
-    floats(rg[n], g);
-    if (W == 2) floats(ru[n], u);
+    rg[n].floats(g);
+    if (W == 2) ru[n].floats(u);
     uint2 w;
     uint32_t b = encode_quarter<FMT>(g, w);
     size_t at = (size_t)i[n].r * W * it.row.d + i[n].c8;
@@ -185,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
       if (W == 2) g[k] = g[k] * sigm<T>(g[k]) * u[k];
       else g[k] = g[k] * sigm<T>(2.f * kGeluK * (g[k] + kGeluC * g[k] * g[k] * g[k]));
     }
-    tile_out<MODE>(sm, y + (size_t)i[n].r * f, i[n], f, g);
+    item_out<MODE>(y + (size_t)i[n].r * f, i[n], f, g);
   }
 }
 
@@ -193,19 +176,18 @@ template <typename T, int FMT, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
                                                       const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
-  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = per_thread<MODE, kActBwdItems>;
-  __shared__ __align__(16) T sm[Tile<T, MODE>::N];
+  constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = act_bwd_items(MODE);
   pdl_wait();
   pdl_trigger();
   Item i[U];
-  Raw8<T> rt[U];
+  Piece<MODE, T> rt[U];
   uint2 qg[U], qu[U];
   uint32_t eg[U], eu[U];
 #pragma unroll
   for (int n = 0; n < U; ++n) {
-    i[n] = item<MODE, U>(it, f, n);
+    i[n] = item<U>(it, n);
     const size_t at = i[n].in ? (size_t)i[n].r * W * it.row.d + i[n].c8 : 0, at2 = i[n].in && W == 2 ? at + it.row.d : at;
-    rt[n] = load_raw<MODE>(dy + (size_t)i[n].r * f, i[n].c(), i[n].in ? f : 0);
+    rt[n].load(dy + (size_t)i[n].r * f, i[n].c(), i[n].in ? f : 0);
     qg[n] = q[at];
     eg[n] = e[at >> 2];
     if (W == 2) {
@@ -216,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
 #pragma unroll
   for (int n = 0; n < U; ++n) {
     float g[8], u[8], t[8], a[8];
-    floats(rt[n], t);
+    rt[n].floats(t);
     decode8<FMT>(qg[n], eg[n], g);
     if (W == 2) decode8<FMT>(qu[n], eu[n], u);
 #pragma unroll
@@ -234,9 +216,9 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
       }
     }
     T* dr = dx + (size_t)i[n].r * W * f;
-    tile_out<MODE>(sm, dr, i[n], f, g);
-    if (W == 2) tile_out<MODE>(sm, dr + f, i[n], f, u);
-    if (y) tile_out<MODE>(sm, y + (size_t)i[n].r * f, i[n], f, a);
+    item_out<MODE>(dr, i[n], f, g);
+    if (W == 2) item_out<MODE>(dr + f, i[n], f, u);
+    if (y) item_out<MODE>(y + (size_t)i[n].r * f, i[n], f, a);
   }
 }
 
@@ -355,18 +337,15 @@ const char* const kShapeMsg =
 bool codes_ok(const void* q, const void* e) { return q && e && ((uintptr_t)q & 15u) == 0; }
 const char* const kPtrMsg = "NULL pointer, or codes (or A) that are not 16-byte aligned";
 
-// Items of N rows and the blocks and threads that take them.
+// Items of N rows and the blocks that take them.
 struct Shape {
   Items it;
-  unsigned blocks, threads;
-  Shape(int N, int d, int mode, unsigned items) {
-    const uint32_t pieces = (uint32_t)(pitch(d) / 8);
+  unsigned blocks;
+  Shape(int N, int d, unsigned items) {
+    const uint32_t pieces = (uint32_t)(pitch(d) / 8), per = kThreads * items;
     it.n = (uint32_t)((size_t)N * pieces);
     it.row = FastDiv(pieces);
-    threads = mode == kSingle ? std::min<unsigned>(kThreads, (pieces + 31) / 32 * 32) : kThreads;
-    it.tiles = (pieces + threads - 1) / threads;
-    const unsigned per = kThreads * items;   // of a block
-    blocks = mode == kSingle ? (unsigned)N * it.tiles : (it.n + per - 1) / per;
+    blocks = (it.n + per - 1) / per;
   }
 };
 
@@ -376,23 +355,23 @@ struct Shape {
 
 template <typename T, int FMT>
 void store_t(const void* x, size_t ldx, int N, int d, int mode, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Shape h(N, d, mode, kStoreItems);
-  launch_pdl(ZL_BY_MODE(store_k, T, FMT), h.blocks, h.threads, 0, s, (const T*)x, ldx, d, h.it, (uint2*)q, e);
+  const Shape h(N, d, kStoreItems);
+  launch_pdl(ZL_BY_MODE(store_k, T, FMT), h.blocks, kThreads, 0, s, (const T*)x, ldx, d, h.it, (uint2*)q, e);
 }
 template <typename T, int FMT>
 void load_t(const uint8_t* q, const uint8_t* e, int N, int d, void* x, size_t ldx, int mode, cudaStream_t s) {
-  const Shape h(N, d, mode, kLoadItems);
-  launch_pdl(ZL_BY_MODE(load_k, T, FMT), h.blocks, h.threads, 0, s, (const uint2*)q, e, h.it, (T*)x, ldx, d);
+  const Shape h(N, d, kLoadItems);
+  launch_pdl(ZL_BY_MODE(load_k, T, FMT), h.blocks, kThreads, 0, s, (const uint2*)q, e, h.it, (T*)x, ldx, d);
 }
 template <typename T, int FMT, int ACT>
 void act_t(const void* x, int N, int f, int mode, void* y, uint8_t* q, uint8_t* e, cudaStream_t s) {
-  const Shape h(N, f, mode, kActItems);
-  launch_pdl(ZL_BY_MODE(act_k, T, FMT, ACT), h.blocks, h.threads, 0, s, (const T*)x, f, h.it, (T*)y, (uint2*)q, e);
+  const Shape h(N, f, act_items(mode));
+  launch_pdl(ZL_BY_MODE(act_k, T, FMT, ACT), h.blocks, kThreads, 0, s, (const T*)x, f, h.it, (T*)y, (uint2*)q, e);
 }
 template <typename T, int FMT, int ACT>
 void act_bwd_t(const uint8_t* q, const uint8_t* e, const void* dy, int N, int f, int mode, void* dx, void* y, cudaStream_t s) {
-  const Shape h(N, f, mode, kActBwdItems);
-  launch_pdl(ZL_BY_MODE(act_bwd_k, T, FMT, ACT), h.blocks, h.threads, 0, s, (const uint2*)q, e, (const T*)dy, f, h.it, (T*)dx,
+  const Shape h(N, f, act_bwd_items(mode));
+  launch_pdl(ZL_BY_MODE(act_bwd_k, T, FMT, ACT), h.blocks, kThreads, 0, s, (const uint2*)q, e, (const T*)dy, f, h.it, (T*)dx,
              (T*)y);
 }
 

@@ -97,10 +97,26 @@ __device__ __forceinline__ void codes4(uint32_t w, float* x) {
   }
 }
 
+// The 16 bytes from byte b (0 .. 15) of two neighbouring 16-byte words on; b a multiple of 2 (HALF) or of 4.
+template <bool HALF>
+__device__ __forceinline__ uint4 shift16(const uint4& lo, const uint4& hi, uint32_t b) {
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  const bool two = b & 8u, one = b & 4u;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = two ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = one ? w[i + 1] : w[i];
+  if (HALF) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (b & 2u) << 3);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // 8 values of a row at column c of d. MODE kWhole: rows start on 16 bytes and d is a multiple of 8; kTail: rows start on 16
-// bytes, and all but a row's last few values are read 16 bytes at a time; kSingle: one value at a time. Columns from d on read
-// 0 and are not written. What is loaded stays packed until it is used, so that the loads of a thread are all under way before
-// the first of them is waited for.
+// bytes, and all but a row's last few values are read 16 bytes at a time; kSingle: rows start anywhere, their values are read
+// in the 16-byte words around them, those near its ends one at a time. Columns from d on read 0 and are not written. What is
+// loaded stays packed until it is used, so that the loads of a thread are all under way before the first of them is waited for.
 enum { kSingle = 0, kTail = 1, kWhole = 2 };
 template <typename T>
 struct Raw8;
@@ -109,6 +125,13 @@ struct Raw8<bf16> {
   uint4 u;
   __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void get(const void* p) { u = *reinterpret_cast<const uint4*>(p); }
+  // from any address of a bf16 (the 16-byte words around it are read)
+  __device__ __forceinline__ void get_around(const void* p) {
+    const uint32_t b = (uint32_t)(uintptr_t)p & 15u;
+    from_words(reinterpret_cast<const uint4*>((const char*)p - b), b);
+  }
+  __device__ __forceinline__ void from_words(const uint4* w, uint32_t b) { u = shift16<true>(w[0], w[1], b); }
+  __device__ __forceinline__ void words(uint4* w) const { w[0] = u; }
   __device__ __forceinline__ void set(void* p) const { *reinterpret_cast<uint4*>(p) = u; }
   __device__ __forceinline__ void pairs(uint64_t* f) const {
     f[0] = bf2_to_f2(u.x); f[1] = bf2_to_f2(u.y); f[2] = bf2_to_f2(u.z); f[3] = bf2_to_f2(u.w);
@@ -126,6 +149,19 @@ struct Raw8<float> {
   __device__ __forceinline__ void get(const void* p) {
     u = reinterpret_cast<const float4*>(p)[0];
     v = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void get_around(const void* p) {
+    const uint32_t b = (uint32_t)(uintptr_t)p & 15u;
+    from_words(reinterpret_cast<const uint4*>((const char*)p - b), b);
+  }
+  __device__ __forceinline__ void words(uint4* w) const {
+    w[0] = make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w));
+    w[1] = make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w));
+  }
+  __device__ __forceinline__ void from_words(const uint4* w, uint32_t b) {
+    const uint4 lo = shift16<false>(w[0], w[1], b), hi = shift16<false>(w[1], w[2], b);
+    u = make_float4(__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w));
+    v = make_float4(__uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w));
   }
   __device__ __forceinline__ void set(void* p) const {
     reinterpret_cast<float4*>(p)[0] = u;
@@ -155,6 +191,13 @@ __device__ __forceinline__ Raw8<T> load_raw(const T* p, int c, int d) {
   } else if (MODE == kTail && c + 8 <= d) {
     r.get(p + c);
   } else {
+    if (MODE == kSingle) {
+      const int s = (int)(((uintptr_t)(p + c) & 15u) / sizeof(T));   // values of the row before these in their first word
+      if (s <= c && c - s + 8 + 16 / (int)sizeof(T) <= d) {
+        r.get_around(p + c);
+        return r;
+      }
+    }
     r.zero();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -186,6 +229,43 @@ template <int MODE, typename T>
 __device__ __forceinline__ void load8(const T* p, int c, int d, float* f) {
   floats(load_raw<MODE>(p, c, d), f);
 }
+// What load_raw reads, packed until floats() asks for it: the 16-byte words around the values where they start anywhere, so
+// that the shift does not wait for them where they are loaded.
+template <int MODE, typename T>
+struct Piece {
+  Raw8<T> r;
+  __device__ __forceinline__ void load(const T* p, int c, int d) { r = load_raw<MODE>(p, c, d); }
+  __device__ __forceinline__ void floats(float* f) const { act8::floats(r, f); }
+};
+template <typename T>
+struct Piece<kSingle, T> {
+  static constexpr int W = sizeof(T) == 2 ? 2 : 3;
+  uint4 w[W];
+  uint32_t b;
+  __device__ __forceinline__ void load(const T* p, int c, int d) {
+    b = (uint32_t)(uintptr_t)(p + c) & 15u;
+    const int s = (int)b / (int)sizeof(T);
+    if (s <= c && c - s + 8 + 16 / (int)sizeof(T) <= d) {
+      const uint4* q = reinterpret_cast<const uint4*>((const char*)(p + c) - b);
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = q[i];
+    } else {
+      Raw8<T> r;
+      r.zero();
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < d) r.put(i, p[c + i]);
+      r.words(w);
+      w[W - 1] = make_uint4(0, 0, 0, 0);
+      b = 0;
+    }
+  }
+  __device__ __forceinline__ void floats(float* f) const {
+    Raw8<T> r;
+    r.from_words(w, b);
+    act8::floats(r, f);
+  }
+};
 template <int MODE, typename T>
 __device__ __forceinline__ void store_raw(T* p, int c, int d, const Raw8<T>& r) {
   if (MODE == kWhole ? c < d : MODE == kTail && c + 8 <= d) {
@@ -209,6 +289,40 @@ __device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (c + i < d) p[c + i] = from_f<T>(f[i]);
+}
+
+// 8 values of a row that starts anywhere, at column c of d, by a warp whose lanes hold neighbouring columns (where the next one
+// is of the same row; every lane calls, with d = 0 one that has none): a lane writes the 16-byte words that begin in its
+// columns, which end in those of the next lane. Only values before the row's or the warp's first word or behind its last one
+// go one at a time.
+template <typename T>
+__device__ __forceinline__ void store_any(T* p, int c, int d, const Raw8<T>& r) {
+  const int lane = threadIdx.x & 31;
+  const int h = (int)((0u - (uint32_t)(uintptr_t)(p + c)) & 15u) / (int)sizeof(T);   // values before the first word
+  constexpr int W = sizeof(T) / 2;
+  uint4 w[W + 1];
+  r.words(w);
+  uint4& next = w[W];
+  next = w[0];
+  next.x = __shfl_down_sync(0xffffffffu, next.x, 1);
+  next.y = __shfl_down_sync(0xffffffffu, next.y, 1);
+  next.z = __shfl_down_sync(0xffffffffu, next.z, 1);
+  if (sizeof(T) == 2) next.w = __shfl_down_sync(0xffffffffu, next.w, 1);
+  const bool words = c + h + 8 <= d && (h == 0 || lane < 31);
+  if (words) {
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      reinterpret_cast<uint4*>(p + c + h)[i] = shift16<sizeof(T) == 2>(w[i], w[i + 1], h * (uint32_t)sizeof(T));
+  }
+  // what neither this lane's words nor those of the lane before hold
+  const int from = lane > 0 && c > 0 && c + h <= d ? h : 0, to = words ? h : min(8, d - c);
+  if (from < to) {
+    float f[8];
+    floats(r, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= from && i < to) p[c + i] = from_f<T>(f[i]);
+  }
 }
 
 // Encodes this thread's 8 values as its quarter of a group (the four lanes 4 g .. 4 g + 3 of the warp hold the group,
@@ -272,20 +386,6 @@ __device__ __forceinline__ void row_in(T* sm, const T* g, int n, int t, int nt) 
   }
   const int done = head + nv * E;
   if (t < n - done) sm[done + t] = g[done + t];
-}
-template <typename T>
-__device__ __forceinline__ void row_out(T* g, const T* sm, int n, int t, int nt) {
-  constexpr int E = 16 / (int)sizeof(T);
-  const int head = min(n, (E - (int)(((uintptr_t)g & 15u) / sizeof(T))) % E), nv = (n - head) / E;
-  if (t < head) g[t] = sm[t];
-  for (int v = t; v < nv; v += nt) {
-    union { uint4 u; T x[E]; } w;
-#pragma unroll
-    for (int i = 0; i < E; ++i) w.x[i] = sm[head + v * E + i];
-    *reinterpret_cast<uint4*>(g + head + v * E) = w.u;
-  }
-  const int done = head + nv * E;
-  if (t < n - done) g[done + t] = sm[done + t];
 }
 
 // Runs the body of a C entry point: no exception leaves it.

@@ -408,11 +408,11 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
           h[j][i] = fma2(mul2(f[i], rr), pa.a[j][i], mul2(alpha, h[j][i]));
           if (LN) h[j][i] = add2(h[j][i], pa.b[j][i]);
         }
-        if (!VEC) cut<VEC>(h[j], c, a.d);   // (0 past d is NaN times 0 in a row with a NaN; the stage's next row is read with it)
+        if (!VEC) cut<VEC>(h[j], c, a.d);   // (0 past d is NaN times 0 in a row with a NaN)
         Raw8<T> out;
         pack8(h[j], out);
         if (VEC) store_raw<kWhole>((T*)a.ho + o, c, a.d, out);
-        else if (c < a.D) out.set(ring + st * g.stage + c * sizeof(T));   // in f's place, which everyone has read
+        else store_any((T*)a.ho + o, c, a.d, out);
       }
     }
     stat(a.pre, [&](int j, uint64_t* x) {
@@ -425,10 +425,6 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       q[a.N] = pr;
       q[2 * (size_t)a.N] = m;
       q[3 * (size_t)a.N] = r;
-    }
-    if (!VEC) {
-      if (!a.pre) __syncthreads();
-      row_out((T*)a.ho + o, reinterpret_cast<const T*>(ring + st * g.stage), a.d, t, nt);
     }
     if (!a.pre) continue;
     const uint64_t mm = f2(-m, -m), rr = f2(r, r);
@@ -445,16 +441,12 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       Raw8<T> out;
       pack8(h[j], out);
       if (VEC) store_raw<kWhole>((T*)a.no + o, c, a.d, out);
-      else if (c < a.D) out.set(ring + st * g.stage + g.pitch + c * sizeof(T));
+      else store_any((T*)a.no + o, c, a.d, out);
       if (KEEP >= 0 && a.nq) {   // of n as it is stored
         float n[8];
         floats(out, n);
         put_codes<KEEP < 0 ? 0 : KEEP>(n, a.nq + (size_t)row * a.D, a.ne + (size_t)row * (a.D >> 5), c, a.D);
       }
-    }
-    if (!VEC) {
-      __syncthreads();
-      row_out((T*)a.no + o, reinterpret_cast<const T*>(ring + st * g.stage + g.pitch), a.d, t, nt);
     }
   }
   if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
@@ -987,8 +979,6 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         words_in(p + 2 * g.pitch, (const T*)a.ho + o, words, t, nt);
       }
       if (a.dho) words_in(p + g.pitch, (const T*)a.dho + o, words, t, nt);
-      else
-        for (int c = t; c < a.d; c += nt) reinterpret_cast<T*>(p + g.pitch)[c] = from_f<T>(0.f);
       if (a.fq) words_in(p + 3 * g.pitch, a.fq + (size_t)n * a.D, a.D / 4, t, nt);
       else words_in(p + 3 * g.pitch, (const T*)a.f + o, words, t, nt);
     } else {
@@ -997,8 +987,6 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         row_in(reinterpret_cast<T*>(p + 2 * g.pitch), (const T*)a.ho + o, a.d, t, nt);
       }
       if (a.dho) row_in(reinterpret_cast<T*>(p + g.pitch), (const T*)a.dho + o, a.d, t, nt);
-      else
-        for (int c = t; c < a.d; c += nt) reinterpret_cast<T*>(p + g.pitch)[c] = from_f<T>(0.f);   // (dh was formed there)
       if (!a.fq) row_in(reinterpret_cast<T*>(p + 3 * g.pitch), (const T*)a.f + o, a.d, t, nt);
       if (a.fq)
         for (int c = t; c < a.D / 16; c += nt)
@@ -1209,9 +1197,9 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (t + j * nt) * 8;
-        if (c >= a.d) continue;
-        uint64_t v[4], A[4];
-        get_pairs(prm + a.D, c, a.D, A);
+        if (VEC && c >= a.d) continue;   // (else every lane stores)
+        uint64_t v[4], A[4] = {0, 0, 0, 0};
+        if (VEC || c < a.D) get_pairs(prm + a.D, c, a.D, A);
         if (a.pre) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -1228,10 +1216,9 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         }
         if (a.dh) {
           Raw8<T> out;
-          if (!VEC) cut<VEC>(v, c, a.d);   // (as in the forward)
           pack8(v, out);
           if (VEC) store_raw<kWhole>((T*)a.dh + o, c, a.d, out);
-          else out.set(ring + st * g.stage + g.pitch + c * sizeof(T));
+          else store_any((T*)a.dh + o, c, a.d, out);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1240,15 +1227,9 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
           v[i] = mul2(v[i], prr);
         }
         Raw8<T> out;
-        if (!VEC) cut<VEC>(v, c, a.d);
         pack8(v, out);
         if (VEC) store_raw<kWhole>((T*)a.df + o, c, a.d, out);
-        else out.set(ring + st * g.stage + c * sizeof(T));
-      }
-      if (!VEC) {
-        __syncthreads();
-        if (a.dh) row_out((T*)a.dh + o, reinterpret_cast<const T*>(ring + st * g.stage + g.pitch), a.d, t, nt);
-        row_out((T*)a.df + o, reinterpret_cast<const T*>(ring + st * g.stage), a.d, t, nt);
+        else store_any((T*)a.df + o, c, a.d, out);
       }
     }
     if (--gate_left == 0 && !a.per_group) {
