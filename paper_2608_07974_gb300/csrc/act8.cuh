@@ -136,6 +136,10 @@ struct Raw8<bf16> {
   __device__ __forceinline__ void pairs(uint64_t* f) const {
     f[0] = bf2_to_f2(u.x); f[1] = bf2_to_f2(u.y); f[2] = bf2_to_f2(u.z); f[3] = bf2_to_f2(u.w);
   }
+  __device__ __forceinline__ void trim(int n) {   // zeros but for the first n
+    auto keep = [n](int i) { return n >= i + 2 ? ~0u : n == i + 1 ? 0xFFFFu : 0u; };
+    u.x &= keep(0); u.y &= keep(2); u.z &= keep(4); u.w &= keep(6);
+  }
   __device__ __forceinline__ void put(int i, bf16 v) {
     const uint32_t b = __bfloat16_as_ushort(v);
     uint32_t& w = i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w;
@@ -169,6 +173,10 @@ struct Raw8<float> {
   }
   __device__ __forceinline__ void pairs(uint64_t* f) const {
     f[0] = f2(u.x, u.y); f[1] = f2(u.z, u.w); f[2] = f2(v.x, v.y); f[3] = f2(v.z, v.w);
+  }
+  __device__ __forceinline__ void trim(int n) {
+    auto keep = [n](int i, float& x) { if (i >= n) x = 0.f; };
+    keep(0, u.x); keep(1, u.y); keep(2, u.z); keep(3, u.w); keep(4, v.x); keep(5, v.y); keep(6, v.z); keep(7, v.w);
   }
   __device__ __forceinline__ void put(int i, float x) {
     (i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : i == 3 ? u.w : i == 4 ? v.x : i == 5 ? v.y : i == 6 ? v.z : v.w) = x;
@@ -368,24 +376,6 @@ __device__ __forceinline__ void decode8(uint2 q, uint32_t e, float* x) {
   codes4<FMT>(q.y, x + 4);
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] *= s;
-}
-
-// A row of n values between global memory, wherever it starts, and a 16-byte aligned row in shared memory, by the nt threads
-// of a block (number t): 16-byte accesses to global memory but for the values before the first and after the last 16-byte
-// boundary. Value by value from every thread, a row of bf16 off 16 bytes took 4 (reading) to 8 (writing) times as long.
-template <typename T>
-__device__ __forceinline__ void row_in(T* sm, const T* g, int n, int t, int nt) {
-  constexpr int E = 16 / (int)sizeof(T);
-  const int head = min(n, (E - (int)(((uintptr_t)g & 15u) / sizeof(T))) % E), nv = (n - head) / E;
-  if (t < head) sm[t] = g[t];
-  for (int v = t; v < nv; v += nt) {
-    union { uint4 u; T x[E]; } w;
-    w.u = *reinterpret_cast<const uint4*>(g + head + v * E);
-#pragma unroll
-    for (int i = 0; i < E; ++i) sm[head + v * E + i] = w.x[i];
-  }
-  const int done = head + nv * E;
-  if (t < n - done) sm[done + t] = g[done + t];
 }
 
 // Runs the body of a C entry point: no exception leaves it.

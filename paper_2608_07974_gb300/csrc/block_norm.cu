@@ -49,9 +49,9 @@ __device__ __forceinline__ void put_codes(const float* x, uint8_t* q, uint8_t* e
 // threads as a row has 8-column vectors or half as many, works through neighbouring rows one after another while the next
 // rows' tensors are copied in (bulk copies of whole rows on an mbarrier). What a row costs is then its block-wide sums, two
 // in turn forward and one backward, and the issue slots of its arithmetic, not the wait for memory.
-// Rows that do not start on 16 bytes, or not of whole vectors, are copied in and out by the block's threads: where they are of
-// whole 4-byte words the next row is under way meanwhile (cp.async), else a row is read as it is needed. RMSNorm, 2048 rows,
-// bf16, forward and backward: 4096 columns 16 and 28 us, 4094 29 and 46 us (36 and 67 without running ahead), 4095 39 and 72.
+// Rows that do not start on 16 bytes, or not of whole vectors, are copied in by the block's threads, a row ahead, and shifted
+// between neighbouring lanes to be written in whole 16-byte words. RMSNorm, 2048 rows,
+// bf16, forward and backward: 4096 columns 16 and 27 us, 4094 25 and 43 (36 and 67 without running ahead), 4095 31 and 54.
 // ------------------------------------------------------------------------------------------------
 constexpr int kStages = 4;
 
@@ -61,13 +61,49 @@ __device__ __forceinline__ void bulk_row(void* dst, const void* src, uint32_t by
                : "memory");
 }
 
-// A row whose start and length are multiples of 4 bytes, copied in 4 bytes at a time without waiting (cp.async).
-__device__ __forceinline__ void words_in(void* sm, const void* g, int words, int t, int nt) {
-  for (int i = t; i < words; i += nt)
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::su32((uint32_t*)sm + i)), "l"((const uint32_t*)g + i)
-                 : "memory");
+// A row whose start and length are multiples of 4 bytes (every fp32 row's are), copied in 4 bytes at a time without waiting.
+__device__ __forceinline__ void words_in(uint8_t* sm, const void* g, int n, int t, int nt) {
+  for (int i = t; i < n / 4; i += nt)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::su32(sm + 4 * i)), "l"((const uint32_t*)g + i) : "memory");
 }
-__device__ __forceinline__ void words_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// A bf16 row of n bytes that starts anywhere, to where it starts as far behind a 16-byte boundary: its whole 16-byte words, and
+// the ends 4 bytes, or a bf16 alone, to each of four threads from `first` on. (Rows of 4-byte words too would be copied in
+// fewer steps, but every vector of them read in two and shifted: 2048 x 4094 forward 28 us against 23, backward 48 against 43.)
+__device__ __forceinline__ uint32_t phase_of(const void* g) { return (uint32_t)(uintptr_t)g & 15u; }
+__device__ __forceinline__ void halves_in(uint8_t* sm, const void* g, int n, int t, int nt, int first) {
+  const int ph = (int)phase_of(g), end = ph + n, b0 = ph ? 16 : 0, b1 = end & ~15;
+  const uint8_t* const base = (const uint8_t*)g - ph;
+#pragma unroll 4
+  for (int b = b0 + t * 16; b < b1; b += nt * 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::su32(sm + b)), "l"(base + b) : "memory");
+  const int u = t >= first ? t - first : t - first + nt;
+  if (u < 4 ? ph == 0 : u >= 8 || b1 < b0) return;
+  const int w = u < 4 ? 4 * u : b1 + 4 * (u - 4);
+  if (w >= ph && w + 4 <= end) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::su32(sm + w)), "l"(base + w) : "memory");
+  } else {
+    const int v = w + 2;
+    if (w >= ph && w + 2 <= end) *reinterpret_cast<uint16_t*>(sm + w) = *reinterpret_cast<const uint16_t*>(base + w);
+    if (v >= ph && v + 2 <= end) *reinterpret_cast<uint16_t*>(sm + v) = *reinterpret_cast<const uint16_t*>(base + v);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void row_in(bool words, uint8_t* sm, const void* g, int n, int t, int nt, int first) {
+  if (sizeof(T) == 4 || words) words_in(sm, g, n, t, nt);
+  else halves_in(sm, g, n, t, nt, first);
+}
+__device__ __forceinline__ void row_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+constexpr uint32_t kPhase = 16;   // bytes more that a row's place takes then
+// Columns c .. c + 7 of row g in shared memory (0 from d on).
+template <bool VEC, typename T>
+__device__ __forceinline__ void row_get(Raw8<T>& r, bool words, const uint8_t* sm, const T* g, int c, int d) {
+  if (VEC || sizeof(T) == 4 || words) {
+    r.get(sm + c * sizeof(T));
+  } else {
+    r.get_around(sm + phase_of(g) + c * sizeof(T));
+    if (c + 8 > d) r.trim(d - c);
+  }
+}
 
 // Sums over the block of one or two values; every thread gets them. The scratch (zeroed before, for the warps that do not
 // exist) alternates between two buffers, so one barrier per sum is enough: who writes a buffer again has passed the barrier
@@ -269,7 +305,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const bool async_in = !VEC && g.stages > 1;
+  const bool ahead = !VEC && g.stages > 1;   // the next row is copied in meanwhile
   auto fill = [&](int k, int st) {   // row number k of this block into a stage
     uint8_t* p = ring + st * g.stage;
     const size_t o = (size_t)(r0 + k) * a.d;
@@ -278,17 +314,14 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       tc::mbar_expect_tx(bar, 2 * bytes);
       bulk_row(p, (const T*)a.f + o, bytes, bar);
       bulk_row(p + g.pitch, (const T*)a.h + o, bytes, bar);
-    } else if (async_in) {
-      words_in(p, (const T*)a.f + o, a.d * (int)sizeof(T) / 4, t, nt);
-      words_in(p + g.pitch, (const T*)a.h + o, a.d * (int)sizeof(T) / 4, t, nt);
     } else {
-      row_in(reinterpret_cast<T*>(p), (const T*)a.f + o, a.d, t, nt);
-      row_in(reinterpret_cast<T*>(p + g.pitch), (const T*)a.h + o, a.d, t, nt);
+      row_in<T>(a.words, p, (const T*)a.f + o, (int)bytes, t, nt, 0);
+      row_in<T>(a.words, p + g.pitch, (const T*)a.h + o, (int)bytes, t, nt, 32 % nt);
     }
   };
   if (VEC && t == 0)
     for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
-  if (async_in) fill(0, 0);
+  if (ahead) fill(0, 0);
   Params<VPT, VEC, LN> pa;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) pa.pre(j, (t + j * nt) * 8, a.d, a.nw, a.nb);
@@ -311,12 +344,11 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
     if (VEC) {
       wait_row(full, at, abort_flag);
     } else {
-      if (async_in) {
-        words_wait();
-      } else {
+      if (!ahead) {
         __syncthreads();
         fill(k, 0);
       }
+      row_wait();
       __syncthreads();
     }
     Raw8<T> rf[VPT], rh[VPT];
@@ -326,8 +358,8 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       rf[j].zero();
       rh[j].zero();
       if (c < a.D) {
-        rf[j].get(ring + st * g.stage + c * sizeof(T));
-        rh[j].get(ring + st * g.stage + g.pitch + c * sizeof(T));
+        row_get<VEC>(rf[j], a.words, ring + st * g.stage, (const T*)a.f + o, c, a.d);
+        row_get<VEC>(rh[j], a.words, ring + st * g.stage + g.pitch, (const T*)a.h + o, c, a.d);
       }
     }
     // 1 / deviation of the values val(j, x) of every vector, and with a LayerNorm their mean; after the first barrier of a row
@@ -337,7 +369,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       rstd = 1.f;
       auto next = [&]() {
         if (VEC && first && t == 0 && k + g.stages < rows && !*abort_flag) fill(k + g.stages, st);
-        if (async_in && first && k + 1 < rows) fill(k + 1, st ^ 1);
+        if (ahead && first && k + 1 < rows) fill(k + 1, st ^ 1);
         first = false;
       };
       if (kind == ZL_NORM_NONE) {
@@ -584,11 +616,11 @@ bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
   static const Occupancy occ(fwd_ring_k<T, VPT, VEC, LN, KEEP>);
   if (!occ.ok) return false;
   Ring g;
-  g.pitch = (uint32_t)a.D * sizeof(T);
+  g.pitch = (uint32_t)a.D * sizeof(T) + (VEC ? 0 : kPhase);
   g.stage = 2 * g.pitch;
   const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), 16}));   // blocks that the registers allow
   const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, (size_t)occ.fixed) - occ.fixed;
-  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : a.words ? 2 : 1;
+  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : 2;
   if ((size_t)g.stages * g.stage + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
   const size_t smem = (size_t)g.stages * g.stage;
   if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
@@ -892,9 +924,10 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
 // joining kernel take 6, launch and the first rows 4; LayerNorms 33.8. Three kernels that each read the rows took 91 us, two
 // barriers a row in one kernel 38.6.
 // ------------------------------------------------------------------------------------------------
-// The normalised f, (f - pm) pr, at column c of a row in shared memory (a row of T, or of codes whose group byte is e).
-template <typename T, bool LN>
-__device__ __forceinline__ void norm_f(const Bwd& a, const uint8_t* row, uint32_t e, int c, float pm, float pr, uint64_t* f) {
+// The normalised f, (f - pm) pr, at column c of row g in shared memory (a row of T, or of codes whose group byte is e).
+template <typename T, bool VEC, bool LN>
+__device__ __forceinline__ void norm_f(const Bwd& a, const uint8_t* row, const T* g, uint32_t e, int c, float pm, float pr,
+                                       uint64_t* f) {
   float sc = 1.f;
   if (a.fq) {
     const uint2 w = *reinterpret_cast<const uint2*>(row + c);
@@ -911,7 +944,7 @@ __device__ __forceinline__ void norm_f(const Bwd& a, const uint8_t* row, uint32_
     sc = group_scale(e);
   } else {
     Raw8<T> r;
-    r.get(row + c * sizeof(T));
+    row_get<VEC>(r, a.words, row, g, c, a.d);
     r.pairs(f);
   }
   if (LN) {   // the product with a power of two is exact
@@ -957,7 +990,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const bool async_in = !VEC && g.stages > 1;
+  const bool next_in = !VEC && g.stages > 1;   // the next row is copied in meanwhile
   auto fill = [&](int k, int st) {   // row number k of this block into a stage
     uint8_t* p = ring + st * g.stage;
     const int n = r0 + k;
@@ -972,30 +1005,19 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       if (a.dho) bulk_row(p + g.pitch, (const T*)a.dho + o, bytes, bar);
       if (a.fq) bulk_row(p + 3 * g.pitch, a.fq + (size_t)n * a.D, (uint32_t)a.D, bar);
       else bulk_row(p + 3 * g.pitch, (const T*)a.f + o, bytes, bar);
-    } else if (async_in) {
-      const int words = a.d * (int)sizeof(T) / 4;
-      if (a.pre) {
-        words_in(p, (const T*)a.dn + o, words, t, nt);
-        words_in(p + 2 * g.pitch, (const T*)a.ho + o, words, t, nt);
-      }
-      if (a.dho) words_in(p + g.pitch, (const T*)a.dho + o, words, t, nt);
-      if (a.fq) words_in(p + 3 * g.pitch, a.fq + (size_t)n * a.D, a.D / 4, t, nt);
-      else words_in(p + 3 * g.pitch, (const T*)a.f + o, words, t, nt);
     } else {
       if (a.pre) {
-        row_in(reinterpret_cast<T*>(p), (const T*)a.dn + o, a.d, t, nt);
-        row_in(reinterpret_cast<T*>(p + 2 * g.pitch), (const T*)a.ho + o, a.d, t, nt);
+        row_in<T>(a.words, p, (const T*)a.dn + o, (int)bytes, t, nt, 0);
+        row_in<T>(a.words, p + 2 * g.pitch, (const T*)a.ho + o, (int)bytes, t, nt, 64 % nt);
       }
-      if (a.dho) row_in(reinterpret_cast<T*>(p + g.pitch), (const T*)a.dho + o, a.d, t, nt);
-      if (!a.fq) row_in(reinterpret_cast<T*>(p + 3 * g.pitch), (const T*)a.f + o, a.d, t, nt);
-      if (a.fq)
-        for (int c = t; c < a.D / 16; c += nt)
-          reinterpret_cast<uint4*>(p + 3 * g.pitch)[c] = reinterpret_cast<const uint4*>(a.fq + (size_t)n * a.D)[c];
+      if (a.dho) row_in<T>(a.words, p + g.pitch, (const T*)a.dho + o, (int)bytes, t, nt, 32 % nt);
+      if (a.fq) row_in<T>(a.words, p + 3 * g.pitch, a.fq + (size_t)n * a.D, a.D, t, nt, 0);
+      else row_in<T>(a.words, p + 3 * g.pitch, (const T*)a.f + o, (int)bytes, t, nt, 96 % nt);
     }
   };
   if (VEC && t == 0)
     for (int k = 0; k < min(rows, g.stages); ++k) fill(k, k);
-  if (async_in && rows > 0) fill(0, 0);
+  if (next_in && rows > 0) fill(0, 0);
   // w_pre and A = beta gate w_post of the block's columns, behind the ring, and where gate groups end within the chunk the
   // post norm's sums over them (every thread reads what it wrote)
   float* const prm = reinterpret_cast<float*>(ring + g.stages * g.stage);
@@ -1111,12 +1133,11 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
     if (VEC) {
       wait_row(full, at, abort_flag);
     } else {
-      if (async_in) {
-        words_wait();
-      } else {
+      if (!next_in) {
         __syncthreads();
         fill(k, 0);
       }
+      row_wait();
       __syncthreads();
     }
     // g, xh and fh of the row, and its sums
@@ -1131,14 +1152,14 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         for (int i = 0; i < 4; ++i) G[j][i] = xh[j][i] = fh[j][i] = 0;
         if (c >= a.D) continue;
         Raw8<T> rd, rn, rx;
-        rd.get(p + g.pitch + c * sizeof(T));
+        row_get<VEC>(rd, a.words || !a.dho, p + g.pitch, (const T*)a.dho + o, c, a.d);
         uint64_t u[4], w[4], A[4];
         get_pairs(prm + a.D, c, a.D, A);
-        norm_f<T, LN>(a, p + 3 * g.pitch, e[j], c, pm, pr, fh[j]);
+        norm_f<T, VEC, LN>(a, p + 3 * g.pitch, (const T*)a.f + o, e[j], c, pm, pr, fh[j]);
         rd.pairs(G[j]);
         if (a.pre) {
-          rn.get(p + c * sizeof(T));
-          rx.get(p + 2 * g.pitch + c * sizeof(T));
+          row_get<VEC>(rn, a.words, p, (const T*)a.dn + o, c, a.d);
+          row_get<VEC>(rx, a.words, p + 2 * g.pitch, (const T*)a.ho + o, c, a.d);
           get_pairs(prm, c, a.D, w);
           rn.pairs(u);
           rx.pairs(xh[j]);
@@ -1183,7 +1204,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       if (VEC && *abort_flag) break;
       // everyone has the row in registers
       if (VEC && t == 0 && k + g.stages < rows) fill(k + g.stages, st);
-      if (async_in && k + 1 < rows) fill(k + 1, st ^ 1);
+      if (next_in && k + 1 < rows) fill(k + 1, st ^ 1);
       float sx[4], sy[4];
       Reducer::warps4(b, sx);
       if (LN) Reducer::warps4(b + 64, sy);
@@ -1456,11 +1477,11 @@ bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
   if (!occ.ok) return false;
   Ring g = {};
   const size_t prm = bwd_prm(a.D, LN, a.per_group);
-  g.pitch = (uint32_t)a.D * sizeof(T);
+  g.pitch = (uint32_t)a.D * sizeof(T) + (VEC ? 0 : kPhase);
   g.stage = 3 * g.pitch + (a.fq ? (uint32_t)a.D : g.pitch);
   const int want = std::max(1, std::min({2048 / th, 65536 / (occ.regs * th), (a.chunks + sm_count() - 1) / sm_count()}));
   const size_t room = std::max((size_t)(Occupancy::kMaxSmem + 1024) / want, occ.fixed + prm) - occ.fixed - prm;
-  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : a.words ? 2 : 1;
+  g.stages = VEC ? (int)std::min<size_t>(kStages, std::max<size_t>(2, room / g.stage)) : 2;
   if ((size_t)g.stages * g.stage + prm + occ.fixed > (size_t)Occupancy::kMaxSmem) g.stages = 1;
   const size_t smem = (size_t)g.stages * g.stage + prm;
   if (smem + occ.fixed > (size_t)Occupancy::kMaxSmem) return false;
