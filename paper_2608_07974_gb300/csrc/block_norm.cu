@@ -1243,9 +1243,12 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          v[i] = fma2(fh[j][i], d2, mul2(A[i], G[j][i]));
-          if (LN) v[i] = add2(v[i], d1);
-          v[i] = mul2(v[i], prr);
+          v[i] = mul2(A[i], G[j][i]);
+          if (a.post) {   // (without a post norm df holds no f: 0 times a NaN or an infinity of it would be NaN)
+            v[i] = fma2(fh[j][i], d2, v[i]);
+            if (LN) v[i] = add2(v[i], d1);
+            v[i] = mul2(v[i], prr);
+          }
         }
         Raw8<T> out;
         pack8(v, out);

@@ -395,6 +395,32 @@ def test_nan_rows_among_many(B, dtype, post, pre, d):
     assert not bool(torch.isfinite(spoilt[1][bad]).all(1).any()) and not bool(torch.isfinite(spoilt[3][3::14]).all(1).any())
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kept", [None, R.E4M3, R.INT8])
+@pytest.mark.parametrize("d", [35, 64, 1000, 4096, 8200])
+def test_branch_gradient_without_norms_holds_no_branch(B, dtype, kept, d):
+    """Neither norm: dh = alpha dh', df = beta gate dh', whatever stands in f (a NaN or an infinity reaches dgate alone, in its
+    own column). One product more than beta gate: three roundings in 24 bits, then the one to the type."""
+    c, N, T = setting(R.NONE, R.NONE), 9, R.DT[dtype]
+    g = torch.Generator().manual_seed(d)
+    f, dho = acts(N, d, dtype, g), torch.randn(N, d, generator=g).to(T)
+    f[1, d // 2], f[4, 3], f[5, d - 1] = float("nan"), float("inf"), float("-inf")
+    gate = 0.5 + torch.rand(1, d, generator=g)
+    dh, df = (torch.full((N, d), 7.0, dtype=T, device="cuda") for _ in range(2))
+    dgate, st = torch.empty(1, d, device="cuda"), torch.tensor([0.0, 1.0, 0.0, 1.0], device="cuda").repeat_interleave(N).view(4, N)
+    p = dims(B, dtype, c, N, d, kept or 0)
+    ws = torch.empty(B.zl_op_block_norm_bwd_bytes(p), dtype=torch.uint8, device="cuda")
+    src = (f.cuda(), None, None) if kept is None else (None, *(t.cuda() for t in R.store(f, kept)))
+    B.zl_op_block_norm_bwd(p, None, *src, None, None, gate.cuda(), None, st, None, dho.cuda(), dh, df, None, None, dgate, None, None, ws)
+    G = dho.double()
+    for got, ref in ((dh, c["alpha"] * G), (df, c["beta"] * gate.double() * G)):
+        R.assert_close(got, ref, (R.HALF[T] + 3 * ULP) * (1 + R.HALF[T]) * ref.abs(), d)
+    bad = torch.zeros(d, dtype=torch.bool)
+    bad[[d // 2, 3, d - 1]] = True
+    assert torch.equal(torch.isfinite(dgate[0]).cpu(), ~bad)
+
+
 # ---- together --------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
