@@ -33,6 +33,12 @@ struct Item {
 constexpr int kStoreItems = 2, kLoadItems = 2;
 constexpr int act_items(int mode) { return mode == kSingle ? 1 : 2; }
 constexpr int act_bwd_items(int mode) { return mode == kSingle ? 2 : 1; }
+// Blocks of the SwiGLU backward on an SM (0: as many as its registers leave): one register above 40 costs the sixth (2048 x
+// 11008 bf16 from integer codes 38.2 us with six, 39.4 with five; 4096 x 8192 fp32 90.3, with 12 bytes spilled, and 99.9). fp32
+// rows with a ragged end stay at five.
+constexpr int act_bwd_blocks(int act, int mode, size_t bytes) {
+  return act != ZL_ACT_SWIGLU || mode == kSingle ? 0 : mode == kTail && bytes == 4 ? 5 : 6;
+}
 // Item u of U.
 template <int U>
 __device__ __forceinline__ Item item(const Items& it, int u) {
@@ -118,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) load_k(const uint2* __restrict__ q, 
 // dx = dy (s + 2 x s (1 - s) k (1 + 3 c x^2)). bf16: e^x and the reciprocal by the fast instructions (a few fp32 ulp,
 // far below the rounding to bf16); fp32: expf and a true division. HBM-bound: a SwiGLU in bf16 moves 8.06 bytes for each of
 // its f values forward, 10.06 backward (y again among them). 2048 x 11008 bf16 from e4m3: forward 29.5 us (6.2 TB/s, 91% of
-// the measured copy rate), backward 35.2 us (6.4 TB/s); from integer codes 29.0 and 37.9; GELU 22.7 and 28.4.
+// the measured copy rate), backward 34.7 us (6.5 TB/s); from integer codes 29.1 and 38.2; GELU 22.6 and 28.4.
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ float sigm(float x) {
@@ -173,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) act_k(const T* __restrict__ x, int f
 }
 
 template <typename T, int FMT, int ACT, int MODE>
-__global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
+__global__ void __launch_bounds__(kThreads, act_bwd_blocks(ACT, MODE, sizeof(T))) act_bwd_k(const uint2* __restrict__ q, const uint8_t* __restrict__ e,
                                                       const T* __restrict__ dy, int f, Items it,
                                                       T* __restrict__ dx, T* __restrict__ y) {
   constexpr int W = ACT == ZL_ACT_SWIGLU ? 2 : 1, U = act_bwd_items(MODE);
@@ -207,7 +213,8 @@ __global__ void __launch_bounds__(kThreads) act_bwd_k(const uint2* __restrict__ 
         const float s = sigm<T>(g[k]), gs = g[k] * s, uu = u[k];
         a[k] = gs * uu;
         u[k] = t[k] * gs;                                    // du
-        g[k] = t[k] * uu * s * (1.f + g[k] * (1.f - s));     // dg
+        // dg: half of silu' (which stays below 1.1) times up first, so that no factor is infinite (dy up may be, and s then 0)
+        g[k] = 2.f * (t[k] * (s * fmaf(g[k], fmaf(-0.5f, s, 0.5f), 0.5f) * uu));
       } else {
         const float x = g[k], s = sigm<T>(2.f * kGeluK * (x + kGeluC * x * x * x));
         a[k] = x * s;

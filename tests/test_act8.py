@@ -362,6 +362,32 @@ def test_activation_of_large_values(B, dtype, fmt, kind):
         assert same(dx[:, f:], 0.25 * torch.where(x > 0, x, torch.zeros_like(x)))
 
 
+@gpu
+@pytest.mark.parametrize("dtype,fmt", [("f32", R.E4M3), ("f32", R.INT8), ("bf16", R.E4M3), ("bf16", R.INT8)])
+def test_swiglu_gradient_of_large_factors(B, dtype, fmt):
+    """Large dy and up beside gates of every size: no gradient is NaN, and where the result fits into the type (below half its
+    largest value) it keeps the bounds of ordinary values. Powers of two, a group of 32 columns for each, so that the
+    checkpoint holds them exactly."""
+    T = R.DT[dtype]
+    gates = torch.tensor([-(2.0 ** 100), -256.0, -128.0, -64.0, -16.0, -2.0, 0.0, 2.0, 2.5, 16.0, 128.0])
+    ups, dys = torch.tensor([2.0 ** -100, 1.0, -(2.0 ** 64), 2.0 ** 127]), torch.tensor([2.0 ** -64, 4.0, -(2.0 ** 90), 1.9375 * 2.0 ** 127])
+    gate, up, dy = (v.flatten().repeat_interleave(32).view(1, -1).to(T) for v in torch.meshgrid(gates, ups, dys, indexing="ij"))
+    x, f = torch.cat([gate, up], 1), gate.shape[1]
+    q, e = R.store(x.view(2, f), fmt)
+    assert torch.equal(R.load(q, e, fmt, f).view(1, -1), x.double())
+    dx = torch.full((1, 2 * f), 7.0, dtype=T, device="cuda")
+    B.zl_op_act8_act_bwd(code(B, dtype), R.SWIGLU, fmt, q.cuda(), e.cuda(), dy.cuda(), 1, f, dx)
+    assert not bool(torch.isnan(dx).any())
+    _, _, ref, bound = act_bounds(x.double(), R.SWIGLU, dtype, dy.double())
+    # a factor s below 2^-120 is flushed or loses digits on the way, its share of the product with it; silu' up / 2 below 2^-126
+    # is off by half of 2^-149, twice dy times which is an error of dg
+    lost = 2.0 ** -120 * (dy.double().abs() * torch.cat([up, gate], 0).double().abs().clamp(min=1)).reshape(1, -1)
+    lost[:, :f] += 2.0 ** -149 * dy.double().abs()
+    fits = ref.abs() <= torch.finfo(T).max / 2
+    R.assert_close(dx.cpu()[fits], ref[fits], (bound + lost)[fits], "dx")
+    assert bool((torch.sign(dx.cpu().double()) == torch.sign(ref))[~fits].all())
+
+
 # ---- weight gradient ----------------------------------------------------------------------------
 DWS = [(1, 1, 1), (16, 16, 16), (24, 40, 1), (8, 32, 5), (130, 72, 50), (256, 128, 203), (33, 65, 77), (384, 1000, 129), (257, 96, 1021), (768, 768, 4096),
        (130, 770, 300)]
