@@ -785,16 +785,15 @@ __global__ void __launch_bounds__(256) dw_reduce_k(const float* __restrict__ ws,
 // ------------------------------------------------------------------------------------------------
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 int g_sms = 0;
-int g_avail = -1;
 
-bool init() {
-  if (g_avail >= 0) return g_avail == 1;
-  g_avail = 0;
+bool find_device() {
   int dev = 0, major = 0, minor = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-  cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-  cudaDeviceGetAttribute(&g_sms, cudaDevAttrMultiProcessorCount, dev);
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&g_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
   if (major != 10 || minor != 3) return false;
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult q;
@@ -802,8 +801,12 @@ bool init() {
       q != cudaDriverEntryPointSuccess || !fn)
     return false;
   g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-  g_avail = 1;
   return true;
+}
+// Whether the kernels run on this machine. Threads that ask while the first one finds out wait for its answer.
+bool init() {
+  static const bool available = find_device();
+  return available;
 }
 
 // 2-D bf16 tensor [outer, inner] (inner contiguous, rows `pitch` apart: 0, inner), box [box_outer, box_inner], 128-byte swizzle.
@@ -970,7 +973,7 @@ Plan choose(int mode, int M, int N, int K, bool rotates = false) {
   };
   static const Kind kinds[] = {{256, 1, 0.295, 2.6}, {128, 1, 0.200, 2.1}, {256, 0, 0.350, 1.6}, {128, 0, 0.240, 1.4},
                                {64, 0, 0.330, 0.6}};
-  const int sms = g_sms > 0 ? g_sms : 152;   // (a workspace may be sized before the device is known)
+  const int sms = g_sms > 0 ? g_sms : 152;   // (without a device a workspace may still be sized)
   const double hbm = 6.0e6;                  // bytes / us
   const bool dw = mode == 2 || mode == 4;    // both operands MN-major
   const double off_a = (dw ? M : K) % 64 != 0, off_b = (mode == 0 ? K : N) % 64 != 0;   // rows off 128-byte lines
@@ -1115,40 +1118,50 @@ bool gemm_tc(int mode, int M, int N, int K, const void* A, const void* B, void* 
 }
 
 namespace {
-int dw_depth(int K, int parts) { return parts > 1 ? parts * ((K + tc::BK - 1) / tc::BK * tc::BK) : K; }
+// The plan of a weight gradient from checkpoints, by which its workspace is sized and its product launched.
+struct DwGemm {
+  tc::Plan tile;
+  int depth, kb_per_split, splits;   // rows of A; k blocks of a split, splits
+  size_t ws;                         // bytes of the splits' partial sums
+};
+DwGemm dw_gemm(int M, int N, int K, int parts) {
+  tc::init();   // (its SM count)
+  DwGemm p;
+  const int Np = (N + 7) / 8 * 8, kb = (K + tc::BK - 1) / tc::BK;
+  p.depth = parts > 1 ? parts * kb * tc::BK : K;
+  p.tile = tc::choose(2, M, Np, p.depth);
+  force_plan(p.tile, 2, M, p.depth);
+  const int nk = (p.depth + tc::BK - 1) / tc::BK;
+  p.kb_per_split = (nk + p.tile.splits - 1) / p.tile.splits;
+  p.splits = (nk + p.kb_per_split - 1) / p.kb_per_split;
+  p.ws = p.splits > 1 ? (size_t)p.splits * M * Np * 4 : 0;
+  return p;
+}
 }  // namespace
 
-size_t gemm_tc_dw_bytes(int M, int N, int K, int parts) {
-  const int Np = (N + 7) / 8 * 8, sp = tc::choose(2, M, Np, dw_depth(K, parts)).splits;
-  return sp > 1 ? (size_t)sp * M * Np * 4 : 0;
-}
+size_t gemm_tc_dw_bytes(int M, int N, int K, int parts) { return K > 0 ? dw_gemm(M, N, K, parts).ws : 0; }
 
 bool gemm_tc_dw(int M, int N, int K, const void* A, int lda, const void* B, int ldb, float* C, const GemmDw& dw, cudaStream_t s) {
   auto al16 = [](const void* p) { return ((uintptr_t)p & 15u) == 0; };
   if (!tc::init() || M < 1 || N < 1 || K < 1 || !al16(A) || !al16(B) || lda % 8 != 0 || ldb % 8 != 0) return false;
   const int Np = (N + 7) / 8 * 8;
+  const DwGemm p = dw_gemm(M, N, K, dw.parts);
+  if (p.ws > dw.ws_bytes) return false;
   tc::Args a = {};
-  a.M = M; a.N = N; a.K = dw_depth(K, dw.parts);
+  a.M = M; a.N = N; a.K = p.depth;
   a.alpha = 1.f;
   a.rope_S = 1;
-  tc::Plan plan = tc::choose(2, M, Np, a.K);
-  force_plan(plan, 2, M, a.K);
   const double a_bytes = (double)M * a.K * 2.0, b_bytes = (double)N * K * 2.0;   // (tile order as in run_tc)
   a.tiles_m = (M + tc::BM - 1) / tc::BM;
-  a.tiles_n = (N + plan.bn - 1) / plan.bn;
+  a.tiles_n = (N + p.tile.bn - 1) / p.tile.bn;
   a.group_m = (a_bytes <= 48e6 || a_bytes <= b_bytes) ? a.tiles_m : std::min(8, a.tiles_m);
-  if (plan.pair) a.group_m = (a.group_m + 1) / 2;
+  if (p.tile.pair) a.group_m = (a.group_m + 1) / 2;
   a.kB = K;
   a.kwrap = (K + tc::BK - 1) / tc::BK;
   a.lda = lda;
   a.ldb = ldb;
-  const int nk = (a.K + tc::BK - 1) / tc::BK;
-  auto split = [&](int n) {
-    a.kb_per_split = (nk + n - 1) / n;
-    a.splits = (nk + a.kb_per_split - 1) / a.kb_per_split;
-  };
-  split(plan.splits);
-  if (a.splits > 1 && (size_t)a.splits * M * Np * 4 > dw.ws_bytes) split(1);   // (a forced plan) no room for the partials
+  a.kb_per_split = p.kb_per_split;
+  a.splits = p.splits;
   const int segs = (a.kb_per_split + tc::kSegBlocks - 1) / tc::kSegBlocks;     // of equal length
   a.kb_per_seg = (a.kb_per_split + segs - 1) / segs;
   a.ldc = N;
@@ -1164,7 +1177,7 @@ bool gemm_tc_dw(int M, int N, int K, const void* A, int lda, const void* B, int 
     a.add = !dw.overwrite;
   }
   note_launch(1);
-  if (!tc::launch_dw(plan.bn, plan.pair, a, A, B, s)) return false;
+  if (!tc::launch_dw(p.tile.bn, p.tile.pair, a, A, B, s)) return false;
   if (a.splits > 1) {
     note_launch(1);
     const int blocks = (int)std::min<size_t>(((size_t)M * Np / 4 + 255) / 256, (size_t)tc::g_sms * 8);

@@ -143,8 +143,8 @@ bool gemm_tc_ext(int mode, int M, int N, int K, const void* A, const void* B, vo
                  const GemmExt& e, const GemmRope* rope, unsigned* err, cudaStream_t s, cudaMemPool_t pool);
 // The weight gradient C [M, N] (fp32) = or += A^T B, bf16, on the tensor cores at any size: A [parts][Kp] rows of M values lda
 // apart, Kp = K in whole blocks of 64, its parts (an fp32 matrix cut into bf16 terms) summed against the same B [K] rows of N
-// values ldb apart; parts 1: A [K]. A and B 16-byte aligned, lda and ldb multiples of 8 (else false); C anywhere. Splits of K
-// use the caller's workspace (gemm_tc_dw_bytes; with less of it there is one split).
+// values ldb apart; parts 1: A [K]. A and B 16-byte aligned, lda and ldb multiples of 8, a workspace of gemm_tc_dw_bytes bytes
+// for the partial sums of splits of K (else false, with nothing launched); C anywhere.
 struct GemmDw {
   int parts, overwrite;
   void* ws;

@@ -453,6 +453,61 @@ def test_weight_gradient_over_many_tokens(B, monkeypatch, dtype, plan, K):
     assert torch.equal(*outs)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("M,N,K", [(128, 64, 4096), (520, 333, 1000), (8, 8, 64)])
+def test_workspace_follows_the_plan(B, monkeypatch, dtype, M, N, K):
+    """The workspace is sized by the plan that the call runs: each of its splits has room for its sums."""
+    size, blocks = {}, -(-K // 64) * (3 if dtype == 0 else 1)     # blocks of 64 tokens, three terms of an fp32 gradient
+    for splits in (1, 2, 3):
+        monkeypatch.setenv("ZL_GEMM_TILE", f"64:{splits}")
+        size[splits] = B.zl_op_act8_dw_bytes(dtype, M, N, K)
+    for splits in (2, 3):
+        n = -(-blocks // -(-blocks // min(splits, blocks)))
+        part = n * M * (-(-N // 8) * 8) * 4 if n > 1 else 0
+        assert size[splits] - size[1] == -(-part // 256) * 256
+
+
+FIRST_CALLS = """
+import sys, threading, torch
+sys.path.insert(0, %r)
+from paper_2608_07974_gb300 import binding as B
+n, M, N, K = 8, 256, 256, 128
+A = torch.randn(K, M, device="cuda").to(torch.bfloat16)
+x = torch.randn(K, N, device="cuda").to(torch.bfloat16)
+q, e = torch.empty(K, N, dtype=torch.uint8, device="cuda"), torch.empty(K, N // 32, dtype=torch.uint8, device="cuda")
+B.zl_op_act8_store(1, 0, x, K, N, N, q, e)
+C, ws = torch.zeros(n, M, N, device="cuda"), torch.empty(n, 16 << 20, dtype=torch.uint8, device="cuda")
+streams = [torch.cuda.Stream() for _ in range(n)]
+torch.cuda.synchronize()
+start, errors = threading.Barrier(n), []
+def call(i):
+    torch.cuda.set_device(0)
+    start.wait()
+    try:
+        B.zl_op_act8_dw(1, 0, M, N, K, A, q, e, C[i], 0, ws[i], streams[i].cuda_stream)
+    except Exception as err:
+        errors.append(str(err))
+threads = [threading.Thread(target=call, args=(i,)) for i in range(n)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+torch.cuda.synchronize()
+assert not errors, errors
+assert all(torch.equal(C[i], C[0]) for i in range(n)) and bool(C[0].any())
+print("all")
+"""
+
+
+@gpu
+def test_first_calls_of_several_threads(B):
+    """A process whose first weight gradients come from eight threads at once."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % root], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "all" in r.stdout, r.stderr[-2000:]
+
+
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_weight_gradient_of_no_tokens(B, dtype):
