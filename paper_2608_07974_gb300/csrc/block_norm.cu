@@ -5,6 +5,7 @@
 
 #include "act8.cuh"
 #include "ops.h"
+#include "per_device.h"
 #include "tcgen05.cuh"
 
 namespace zl {
@@ -589,23 +590,31 @@ __global__ void __launch_bounds__(512) fwd_any_k(const Fwd a) {
   }
 }
 
-// Blocks of a kernel (th threads, `smem` dynamic bytes) that an SM holds, from the registers that it was compiled with.
+// Blocks of a kernel (th threads, `smem` dynamic bytes) that an SM holds, from the registers that it was compiled with. Finding
+// out also lets the kernel take that much shared memory, which holds for one device.
 struct Occupancy {
   int regs = 0, fixed = 0;
-  bool ok = false;
   template <typename K>
-  explicit Occupancy(K kern) {
+  bool find(K kern) {
     cudaFuncAttributes fa;
-    ok = cudaFuncGetAttributes(&fa, kern) == cudaSuccess &&
-         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - (int)fa.sharedSizeBytes) == cudaSuccess;
+    if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess ||
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - (int)fa.sharedSizeBytes) != cudaSuccess)
+      return false;
     regs = (fa.numRegs + 7) / 8 * 8;
     fixed = (int)fa.sharedSizeBytes + 1024;
+    return true;
   }
   int blocks(int th, size_t smem) const {
     return std::max(1, std::min({2048 / th, 65536 / (regs * th), (int)((kMaxSmem + 1024) / (smem + fixed)), 32}));
   }
   static constexpr int kMaxSmem = 232448;
 };
+// That of the current device (NULL: the kernel cannot run there; the CUDA error says why).
+template <typename K>
+const Occupancy* occupancy(PerDevice<Occupancy>& devices, K kern) {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess ? devices.get(dev, [&](Occupancy& o) { return o.find(kern); }) : nullptr;
+}
 
 constexpr int kRingCols = 8192;   // the widest row of the ring kernels
 // Threads of a block for a row of nvec vectors, one vector a thread or two.
@@ -613,8 +622,10 @@ int ring_threads(int nvec) { return nvec <= 224 ? (nvec + 31) / 32 * 32 : (nvec 
 
 template <typename T, int VPT, bool VEC, bool LN, int KEEP>
 bool fwd_ring(const Fwd& a, int th, cudaStream_t s) {
-  static const Occupancy occ(fwd_ring_k<T, VPT, VEC, LN, KEEP>);
-  if (!occ.ok) return false;
+  static PerDevice<Occupancy> devices;
+  const Occupancy* const found = occupancy(devices, fwd_ring_k<T, VPT, VEC, LN, KEEP>);
+  if (!found) return false;
+  const Occupancy& occ = *found;
   Ring g;
   g.pitch = (uint32_t)a.D * sizeof(T) + (VEC ? 0 : kPhase);
   g.stage = 2 * g.pitch;
@@ -1476,8 +1487,10 @@ bool plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks)
 
 template <typename T, int VPT, bool VEC, bool LN>
 bool bwd_ring(const Bwd& a, int th, cudaStream_t s) {
-  static const Occupancy occ(bwd_ring_k<T, VPT, VEC, LN>);
-  if (!occ.ok) return false;
+  static PerDevice<Occupancy> devices;
+  const Occupancy* const found = occupancy(devices, bwd_ring_k<T, VPT, VEC, LN>);
+  if (!found) return false;
+  const Occupancy& occ = *found;
   Ring g = {};
   const size_t prm = bwd_prm(a.D, LN, a.per_group);
   g.pitch = (uint32_t)a.D * sizeof(T) + (VEC ? 0 : kPhase);

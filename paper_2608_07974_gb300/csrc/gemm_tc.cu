@@ -14,6 +14,7 @@
 
 #include "common.cuh"
 #include "ops.h"
+#include "per_device.h"
 #include "tcgen05.cuh"
 
 namespace zl {
@@ -840,10 +841,14 @@ bool make_map_c(CUtensorMap* m, const Args& a) {
 template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false, bool DW = false>
 bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int ctas_per_sm, const GemmExt* ext = nullptr) {
   using C_ = Cfg<BN, UPD, PAIR>;
-  static bool attr = false;
-  static int max_pairs = 0;   // clusters of two that can be resident at once
+  struct Ready {
+    int max_pairs = 0;   // clusters of two that can be resident at once
+  };
+  static PerDevice<Ready> devices;
   auto kern = gemm_tc_k<BN, A_MN, B_MN, UPD, PAIR, DW>;
-  if (!attr) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const Ready* const ready = devices.get(dev, [&](Ready& r) {
     if (UPD) {   // the register split of the fused-update kernels must fit the pool the CTA is launched with
       cudaFuncAttributes fa;
       if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess ||
@@ -865,13 +870,14 @@ bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int cta
       ca[0].val.clusterDim.z = 1;
       oc.attrs = ca;
       oc.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&max_pairs, kern, &oc) != cudaSuccess || max_pairs < 1) {
+      if (cudaOccupancyMaxActiveClusters(&r.max_pairs, kern, &oc) != cudaSuccess || r.max_pairs < 1) {
         cudaGetLastError();
         return false;
       }
     }
-    attr = true;
-  }
+    return true;
+  });
+  if (!ready) return false;
   CUtensorMap ta, tb;
   const bool okA = A_MN ? make_map(&ta, A, (uint64_t)a.M, (uint64_t)a.K, 64, 64, DW ? a.lda : 0)
                         : make_map(&ta, A, (uint64_t)a.K, (uint64_t)a.M, 64, BM);
@@ -890,7 +896,7 @@ bool launch(const Args& a, const void* A, const void* B, cudaStream_t s, int cta
   int grid;
   if (PAIR) {   // one cluster of two per pair of tile rows, as many as can be resident
     const int units = (a.tiles_m + 1) / 2 * a.tiles_n * a.splits;
-    grid = 2 * std::min(units, max_pairs);
+    grid = 2 * std::min(units, ready->max_pairs);
   } else {
     const int units = a.tiles_m * a.tiles_n * a.splits;
     const int slots = g_sms * ctas_per_sm;
