@@ -652,22 +652,20 @@ bool fwd_ring_by(const Fwd& a, int th, cudaStream_t s) {
 // 512 threads on an SM: 2048 x 4096 bf16 with RMS norms 15.7 us, with
 // LayerNorms 21.1 us (one vector in 64 registers 22.7).
 template <typename T, bool VEC>
-void forward_as(const Fwd& a, cudaStream_t s) {
+bool forward_as(const Fwd& a, cudaStream_t s) {
   const int nvec = a.D / 8;
   const bool ln = a.post == ZL_NORM_LAYER || a.pre == ZL_NORM_LAYER;
   note_launch(1);
   if (a.d <= kRingCols) {
     const int th = !ln && nvec <= 512 ? (nvec + 31) / 32 * 32 : ring_threads(nvec);
-    if (th >= nvec ? ln ? fwd_ring_by<T, 1, VEC, true>(a, th, s) : fwd_ring_by<T, 1, VEC, false>(a, th, s)
-                   : ln ? fwd_ring_by<T, 2, VEC, true>(a, th, s) : fwd_ring_by<T, 2, VEC, false>(a, th, s))
-      return;
+    if (th >= nvec) return ln ? fwd_ring_by<T, 1, VEC, true>(a, th, s) : fwd_ring_by<T, 1, VEC, false>(a, th, s);
+    return ln ? fwd_ring_by<T, 2, VEC, true>(a, th, s) : fwd_ring_by<T, 2, VEC, false>(a, th, s);
   }
-  launch_pdl(fwd_any_k<T, VEC>, a.N, 512, 0, s, a);
+  return launch_pdl(fwd_any_k<T, VEC>, a.N, 512, 0, s, a) == cudaSuccess;
 }
 template <typename T>
-void forward(const Fwd& a, cudaStream_t s) {
-  if (a.vec && a.wvec) forward_as<T, true>(a, s);
-  else forward_as<T, false>(a, s);
+bool forward(const Fwd& a, cudaStream_t s) {
+  return a.vec && a.wvec ? forward_as<T, true>(a, s) : forward_as<T, false>(a, s);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1554,6 +1552,10 @@ const char* const kDimsMsg =
     "bad dtype, norm, code format or size (0 <= N <= 2^24, 1 <= d <= 2^20, N x d in whole groups below 2^34, gate_rows >= 0, "
     "eps > 0, accumulate 0 or 1)";
 bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+zl_status ended(bool done, const char* what) {
+  const zl_status st = act8::launched(what);
+  return done || st != ZL_OK ? st : act8::fail(ZL_ERR_CUDA, (std::string(what) + ": the kernel cannot be launched on this device").c_str());
+}
 
 }  // namespace
 }  // namespace zl
@@ -1588,9 +1590,8 @@ zl_status zl_op_block_norm(const zl_block_norm* p, const void* h, const void* f,
     a.words = p->d * dt_size(p->dtype) % 4 == 0 && !(((uintptr_t)h | (uintptr_t)f) & 3u);
     for (const void* t : {h, f, (const void*)h_out, (const void*)n_out}) a.vec &= !t || row_mode(t, p->d, p->d, p->dtype) == kWhole;
     a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(pre_b) && al16(gate);
-    if (p->dtype == ZL_DTYPE_BF16) forward<bf16>(a, (cudaStream_t)stream);
-    else forward<float>(a, (cudaStream_t)stream);
-    return launched("zl_op_block_norm");
+    const bool done = p->dtype == ZL_DTYPE_BF16 ? forward<bf16>(a, (cudaStream_t)stream) : forward<float>(a, (cudaStream_t)stream);
+    return ended(done, "zl_op_block_norm");
   });
 }
 
@@ -1648,8 +1649,7 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
       a.vec &= !t || row_mode(t, d, d, p->dtype) == kWhole;
     a.wvec = al16(post_w) && al16(post_b) && al16(pre_w) && al16(dgate) && al16(gate);
     const bool done = p->dtype == ZL_DTYPE_BF16 ? backward<bf16>(a, s) : backward<float>(a, s);
-    const zl_status st = launched("zl_op_block_norm_bwd");
-    return done || st != ZL_OK ? st : act8::fail(ZL_ERR_CUDA, "zl_op_block_norm_bwd: the kernel cannot be launched on this device");
+    return ended(done, "zl_op_block_norm_bwd");
   });
 }
 
