@@ -322,7 +322,8 @@ zl_status zl_op_qkv_rope(int dtype, int M, int N, int K, const void* A, const vo
  * compute dtype need the alignment of their elements only; rows that start on 16 bytes are read and
  * written faster. These calls allocate nothing. Outputs must not overlap inputs except where said.
  * Errors: ZL_ERR_ARG (a size, format or alignment, a NULL pointer, a workspace that is too small),
- * ZL_ERR_CUDA (a launch failed); kernels report nothing.
+ * ZL_ERR_CUDA (a launch failed); kernels report nothing. Where a wait inside a kernel gives up (see
+ * zl_wait_selftest), what is not formed then becomes NaN: rows, codes, gradients that sum over them.
  * ------------------------------------------------------------------------------------- */
 enum { ZL_ACT8_E4M3 = 0, ZL_ACT8_INT8 = 1 };
 enum { ZL_ACT_SWIGLU = 0, ZL_ACT_GELU = 1 };   /* silu(gate) * up;  GELU (tanh form)        */

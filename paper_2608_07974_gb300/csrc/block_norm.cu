@@ -186,7 +186,7 @@ struct Turn {
   }
 };
 // Waits for the row at hand. A wait that gives up (its limit is about 2 s) raises the block's flag, which every thread sees
-// after its next barrier.
+// after its next barrier: it writes NaN to its columns of the outputs that are not formed then.
 __device__ __forceinline__ void wait_row(uint64_t* full, const Turn& at, volatile int* abort_flag) {
   tc::mbar_wait(&full[at.st], at.phase, abort_flag, nullptr);
 }
@@ -198,6 +198,16 @@ __device__ __forceinline__ void drain(uint64_t* full, Turn at, int stages, int n
     }
     at.next(stages);
   }
+}
+
+// NaN in the 8 columns from c on of a row (VEC kernels, after a wait that gave up).
+template <typename T>
+__device__ __forceinline__ void put_nan(T* p, int c, int d) {
+  const uint64_t nan2 = f2(__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u));
+  const uint64_t v[4] = {nan2, nan2, nan2, nan2};
+  Raw8<T> r;
+  pack8(v, r);
+  store_raw<kWhole>(p, c, d, r);
 }
 
 // What a launch of a ring kernel is given besides its operands.
@@ -279,6 +289,23 @@ struct Params {
   }
 };
 
+// NaN in this thread's columns of what rows n .. end - 1 have not got (a call apart: written inside the kernel it changed how
+// the row loop is compiled, 2048 x 4096 with LayerNorms 22.4 us against 21.0).
+template <typename T, int KEEP>
+__device__ __noinline__ void fwd_give_up(const Fwd& a, int n, int end) {
+  for (; n < end; ++n) {
+    const size_t row = n;
+    for (int c = threadIdx.x * 8; c < a.d; c += blockDim.x * 8) {
+      put_nan((T*)a.ho + row * a.d, c, a.d);
+      if (a.pre) put_nan((T*)a.no + row * a.d, c, a.d);
+      const uint32_t w = KEEP == ZL_ACT8_E4M3 ? 0x7F7F7F7Fu : 0x80808080u;
+      if (a.fq) *reinterpret_cast<uint2*>(a.fq + row * a.D + c) = make_uint2(w, w);
+      if (a.nq) *reinterpret_cast<uint2*>(a.nq + row * a.D + c) = make_uint2(w, w);
+    }
+    if (threadIdx.x < 4) a.stats[threadIdx.x * (size_t)a.N + row] = __uint_as_float(0x7FC00000u);
+  }
+}
+
 // Forward. VEC: rows come by bulk copies. KEEP: the format that f or n are written in, -1: neither is. LN: one of the norms
 // is a LayerNorm. HBM-bound on large batches, 8 bytes a value in bf16 (10.06 with both checkpoints): 4096 x 8192 with RMS
 // norms 45 us (6.0 TB/s, 88% of the measured copy rate; with checkpoints 66 us); on 2048 x 4096, where a block has six or seven
@@ -286,7 +313,7 @@ struct Params {
 // sums a row, 21.1. A block for each row, which waits for it and reads the parameters anew, took 35 and 43 us.
 template <typename T, int VPT, bool VEC, bool LN, int KEEP>
 __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80)
-    fwd_ring_k(const Fwd a, const Ring g) {
+    fwd_ring_k(const __grid_constant__ Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][2][16];
@@ -482,7 +509,9 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       }
     }
   }
-  if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
+  if (!VEC || k == rows) return;
+  if (t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
+  fwd_give_up<T, KEEP>(a, r0 + k, r0 + rows);
 }
 
 __device__ __forceinline__ void put_any(int fmt, const float* x, uint8_t* q, uint8_t* e, size_t row, int c, int D) {
@@ -968,9 +997,24 @@ __device__ __forceinline__ void norm_f(const Bwd& a, const uint8_t* row, const T
   }
 }
 
+// NaN in this thread's columns of what the block's rows from number k on have not got, and of its partial sums.
+template <typename T>
+__device__ __noinline__ void bwd_give_up(const Bwd& a, int k) {
+  int r0, r1;
+  chunk_rows(blockIdx.x, a.N, a.gate_rows ? a.gate_rows : a.N, a.rows, a.per_group, r0, r1);
+  for (int c = threadIdx.x * 8; c < a.d; c += blockDim.x * 8) {
+    for (int n = r0 + k; n < r1; ++n) {
+      if (a.dh) put_nan((T*)a.dh + (size_t)n * a.d, c, a.d);
+      put_nan((T*)a.df + (size_t)n * a.d, c, a.d);
+      if (a.dgate && !a.per_group) put_nan(a.dgate + gate_row(n, a.gate_rows) * a.d, c, a.d);
+    }
+    for (int slot = 0; a.part && slot < a.slots; ++slot) put_nan(a.part + ((size_t)blockIdx.x * a.slots + slot) * a.D, c, a.d);
+  }
+}
+
 // LN: one of the norms is a LayerNorm (its sums of u, v and A, and the biases' gradients).
 template <typename T, int VPT, bool VEC, bool LN>
-__global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
+__global__ void __launch_bounds__(512) bwd_ring_k(const __grid_constant__ Bwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
   __shared__ __align__(16) float sh[2][LN ? 2 : 1][64];
@@ -1271,7 +1315,12 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       gate_left = min(gate_rows, rows - 1 - k);
     }
   }
-  if (k == rows && part) {
+  if (VEC && k < rows) {
+    if (t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
+    bwd_give_up<T>(a, k);
+    return;
+  }
+  if (part) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (t + j * nt) * 8;
@@ -1291,7 +1340,6 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const Bwd a, const Ring g) {
       }
     }
   }
-  if (VEC && k < rows && t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
 }
 
 // The gradients from the chunks' partial sums: a block takes 32 columns (8 lanes of four), 32 lanes of chunks each adding every

@@ -466,8 +466,8 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
     uint8_t* stage_out = outbuf + q * (2 * 32 * 128);
     const bool f32out = g.mode >= 2;
     const int ccols = f32out ? 32 : 64;   // columns per chunk
-    int it = 0, nchunk = 0, drain = 0;
-    for (int unit = unit0; unit < num_units; unit += ustride, ++it) {
+    int it = 0, nchunk = 0, drain = 0, unit = unit0;
+    for (; unit < num_units; unit += ustride, ++it) {
       int tm, tn;
       unit_tile(g, unit, num_tiles, PAIR, crank, tm, tn);
       const int split = unit / num_tiles;
@@ -651,6 +651,19 @@ __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
       if (!ok) break;
     }
     if (lane == 0) bulk_wait_all();   // every store of this warp has landed in global memory
+    if constexpr (DW) {   // (no error word) a wait gave up: NaN in this warp's rows of the tiles that are not formed
+      __syncwarp();
+#pragma unroll 1
+      for (; unit < num_units; unit += ustride) {
+        int tm, tn;
+        unit_tile(g, unit, num_tiles, PAIR, crank, tm, tn);
+        const int m0 = tm * BM + q * 32, n1 = min(tn * BN + BN, g.N);
+        float* const cs = (float*)g.C + (size_t)(unit / num_tiles) * g.M * g.ldc;
+#pragma unroll 1
+        for (int m = m0; m < min(m0 + 32, g.M); ++m)
+          for (int n = tn * BN + lane; n < n1; n += 32) cs[(size_t)m * g.ldc + n] = __uint_as_float(0x7FC00000u);
+      }
+    }
   }
 
   __syncthreads();
