@@ -342,7 +342,7 @@ const char* const kShapeMsg =
     "bad dtype, code format, activation or size (0 <= rows <= 2^24, 1 <= columns <= 2^20, rows x columns in whole groups "
     "below 2^34, row strides >= columns, accumulate 0 or 1)";
 bool codes_ok(const void* q, const void* e) { return q && e && ((uintptr_t)q & 15u) == 0; }
-const char* const kPtrMsg = "NULL pointer, or codes (or A) that are not 16-byte aligned";
+const char* const kPtrMsg = "NULL pointer, a tensor off the alignment of its elements, or codes (or A) that are not 16-byte aligned";
 
 // Items of N rows and the blocks that take them.
 struct Shape {
@@ -416,6 +416,7 @@ void prep_t(const DwPrep& p, unsigned blocks, cudaStream_t s) {
 
 using namespace zl;
 using zl::act8::entry;
+using zl::act8::on_elements;
 using zl::act8::row_mode;
 
 extern "C" {
@@ -424,7 +425,7 @@ zl_status zl_op_act8_store(int dtype, int fmt, const void* x, int N, int d, int 
   return entry([&]() -> zl_status {
     if (!act_shape(dtype, fmt, N, d) || ldx < d) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
-    if (!x || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
+    if (!x || !on_elements({x}, dt_size(dtype)) || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     note_launch(1);
     ZL_BY_TYPE(store_t, dtype, fmt, x, (size_t)ldx, N, d, row_mode(x, (size_t)d, (size_t)ldx, dtype), q, e, (cudaStream_t)stream);
     return launched("zl_op_act8_store");
@@ -435,7 +436,7 @@ zl_status zl_op_act8_load(int dtype, int fmt, const uint8_t* q, const uint8_t* e
   return entry([&]() -> zl_status {
     if (!act_shape(dtype, fmt, N, d) || ldx < d) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
-    if (!x || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
+    if (!x || !on_elements({x}, dt_size(dtype)) || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     note_launch(1);
     ZL_BY_TYPE(load_t, dtype, fmt, q, e, N, d, x, (size_t)ldx, row_mode(x, (size_t)d, (size_t)ldx, dtype), (cudaStream_t)stream);
     return launched("zl_op_act8_load");
@@ -446,7 +447,7 @@ zl_status zl_op_act8_act(int dtype, int act, int fmt, const void* x, int N, int 
   return entry([&]() -> zl_status {
     if ((act != ZL_ACT_SWIGLU && act != ZL_ACT_GELU) || !act_shape(dtype, fmt, N, f)) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
-    if (!x || !y || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
+    if (!x || !y || !on_elements({x, y}, dt_size(dtype)) || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     const int mode = std::min(row_mode(x, f, f, dtype), row_mode(y, f, f, dtype));
     note_launch(1);
     ZL_BY_TYPE(act_by, dtype, fmt, act, x, N, f, mode, y, q, e, (cudaStream_t)stream);
@@ -459,7 +460,7 @@ zl_status zl_op_act8_act_bwd(int dtype, int act, int fmt, const uint8_t* q, cons
   return entry([&]() -> zl_status {
     if ((act != ZL_ACT_SWIGLU && act != ZL_ACT_GELU) || !act_shape(dtype, fmt, N, f)) return fail(ZL_ERR_ARG, kShapeMsg);
     if (N == 0) return ZL_OK;
-    if (!dy || !dx || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
+    if (!dy || !dx || !on_elements({dy, dx, y}, dt_size(dtype)) || !codes_ok(q, e)) return fail(ZL_ERR_ARG, kPtrMsg);
     const int mode = std::min({row_mode(dy, f, f, dtype), row_mode(dx, f, f, dtype), y ? row_mode(y, f, f, dtype) : kWhole});
     note_launch(1);
     ZL_BY_TYPE(act_bwd_by, dtype, fmt, act, q, e, dy, N, f, mode, dx, y, (cudaStream_t)stream);
@@ -482,11 +483,11 @@ zl_status zl_op_act8_dw(int dtype, int fmt, int M, int N, int K, const void* A, 
     if (!dw_shape(dtype, fmt, M, N, K) || (accumulate != 0 && accumulate != 1)) return fail(ZL_ERR_ARG, kShapeMsg);
     cudaStream_t s = (cudaStream_t)stream;
     if (K == 0) {
-      if (!C) return fail(ZL_ERR_ARG, kPtrMsg);
+      if (!C || !on_elements({C}, 4)) return fail(ZL_ERR_ARG, kPtrMsg);
       if (!accumulate) cudaMemsetAsync(C, 0, (size_t)M * N * 4, s);
       return launched("zl_op_act8_dw");
     }
-    if (!A || !C || !codes_ok(q, e) || ((uintptr_t)A & 15u)) return fail(ZL_ERR_ARG, kPtrMsg);
+    if (!A || !C || !codes_ok(q, e) || ((uintptr_t)A & 15u) || !on_elements({C}, 4)) return fail(ZL_ERR_ARG, kPtrMsg);
     const DwPlan p = dw_plan(dtype, M, N, K);
     if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < p.b + p.a + p.splits)
       return fail(ZL_ERR_ARG, "the workspace must be 256-byte aligned and hold zl_op_act8_dw_bytes() bytes");

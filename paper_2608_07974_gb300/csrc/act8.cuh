@@ -8,6 +8,7 @@
 #pragma once
 #include <cuda_fp8.h>
 
+#include <initializer_list>
 #include <string>
 
 #include "common.cuh"
@@ -396,6 +397,12 @@ inline zl_status launched(const char* what) {
   return e == cudaSuccess ? ZL_OK : fail(ZL_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
 }
 
+// Whether every pointer lies on elements of that many bytes (a kernel faults on others).
+inline bool on_elements(std::initializer_list<const void*> ps, size_t bytes) {
+  for (const void* p : ps)
+    if ((uintptr_t)p % bytes) return false;
+  return true;
+}
 // The mode of rows of d values from p, ld apart.
 inline int row_mode(const void* p, size_t d, size_t ld, int dt) {
   if (((uintptr_t)p & 15u) || ld * (dt == ZL_DTYPE_BF16 ? 2 : 4) % 16) return kSingle;

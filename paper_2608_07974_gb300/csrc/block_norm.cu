@@ -1599,6 +1599,7 @@ bool dims_ok(const zl_block_norm* p) {
 const char* const kDimsMsg =
     "bad dtype, norm, code format or size (0 <= N <= 2^24, 1 <= d <= 2^20, N x d in whole groups below 2^34, gate_rows >= 0, "
     "eps > 0, accumulate 0 or 1)";
+const char* const kElementsMsg = "a tensor off the alignment of its elements";
 bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 zl_status ended(bool done, const char* what) {
   const zl_status st = act8::launched(what);
@@ -1611,6 +1612,7 @@ zl_status ended(bool done, const char* what) {
 using namespace zl;
 using zl::act8::entry;
 using zl::act8::launched;
+using zl::act8::on_elements;
 using zl::act8::kWhole;
 using zl::act8::row_mode;
 
@@ -1629,6 +1631,8 @@ zl_status zl_op_block_norm(const zl_block_norm* p, const void* h, const void* f,
       return act8::fail(ZL_ERR_ARG, "NULL pointer, or n_out without a pre norm");
     if (!f_q != !f_e || !n_q != !n_e || (n_q && !p->pre_norm) || !al16(f_q) || !al16(n_q))
       return act8::fail(ZL_ERR_ARG, "codes come with their group bytes and 16-byte aligned, n's with a pre norm");
+    if (!on_elements({h, f, h_out, n_out}, dt_size(p->dtype)) || !on_elements({post_w, post_b, gate, pre_w, pre_b, stats}, 4))
+      return act8::fail(ZL_ERR_ARG, kElementsMsg);
     Fwd a = {};
     a.h = h; a.f = f; a.pw = post_w; a.pb = post_b; a.gate = gate; a.nw = pre_w; a.nb = pre_b;
     a.ho = h_out; a.no = n_out; a.stats = stats; a.fq = f_q; a.fe = f_e; a.nq = n_q; a.ne = n_e;
@@ -1676,6 +1680,9 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
       return act8::fail(ZL_ERR_ARG, "NULL pointer, or dn without a pre norm, or no gradient at all");
     if (!f == !f_q || !f_q != !f_e || !al16(f_q))
       return act8::fail(ZL_ERR_ARG, "f either in dtype or as 16-byte aligned codes with their group bytes");
+    if (!on_elements({h_out, f, dn, dh_out, dh, df}, dt_size(p->dtype)) ||
+        !on_elements({post_w, post_b, gate, pre_w, stats, dpost_w, dpost_b, dgate, dpre_w, dpre_b}, 4))
+      return act8::fail(ZL_ERR_ARG, kElementsMsg);
     size_t need = 0;
     zl_op_block_norm_bwd_bytes(p, &need);
     if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < need)

@@ -100,6 +100,23 @@ def test_activations_refuse(B, bad):
     assert err.value.status == B.ZL_ERR_ARG
 
 
+@pytest.mark.parametrize("dtype,off", [(0, 1), (0, 2), (0, 3), (1, 1)])
+def test_addresses_inside_an_element_are_refused(B, dtype, off):
+    """Every tensor in turn off the alignment of its elements (4 bytes of fp32, 2 of bf16), which a kernel would fault on."""
+    from paper_2608_07974_gb300.binding import _check, _lib
+    Q = P + off
+    calls = [lambda: B.zl_op_act8_store(dtype, 0, Q, 4, 64, 64, P, P), lambda: B.zl_op_act8_load(dtype, 0, P, P, 4, 64, 64, Q),
+             lambda: B.zl_op_act8_act(dtype, 0, 0, Q, 4, 64, P, P, P), lambda: B.zl_op_act8_act(dtype, 1, 0, P, 4, 64, Q, P, P),
+             lambda: B.zl_op_act8_act_bwd(dtype, 0, 0, P, P, Q, 4, 64, P), lambda: B.zl_op_act8_act_bwd(dtype, 1, 0, P, P, P, 4, 64, Q),
+             lambda: B.zl_op_act8_act_bwd(dtype, 1, 0, P, P, P, 4, 64, P, Q),
+             lambda: _check(_lib.zl_op_act8_dw(dtype, 0, 32, 64, 16, P, P, P, Q, 0, P, 1 << 24, None)),
+             lambda: _check(_lib.zl_op_act8_dw(dtype, 0, 32, 64, 0, None, None, None, Q, 0, None, 0, None))]
+    for k, call in enumerate(calls):
+        with pytest.raises(B.ZLError) as err:
+            call()
+        assert err.value.status == B.ZL_ERR_ARG, k
+
+
 @pytest.mark.parametrize("bad", [dict(dtype=-1), dict(fmt=2), dict(M=0), dict(N=0), dict(K=-1), dict(A=None), dict(q=None), dict(C=None),
                                  dict(acc=2), dict(ws=None), dict(ws="small"), dict(A=P + 8)])
 def test_weight_gradient_refuses(B, bad):

@@ -104,6 +104,20 @@ def test_backward_refuses(B, bad):
     assert err.value.status == B.ZL_ERR_ARG
 
 
+@pytest.mark.parametrize("dtype,off", [(0, 1), (0, 2), (0, 3), (1, 1)])
+def test_addresses_inside_an_element_are_refused(B, dtype, off):
+    """Every tensor in turn off the alignment of its elements (4 bytes of fp32, 2 of bf16), which a kernel would fault on."""
+    Q = P + off
+    for name in ("h", "f", "h_out", "n_out", "post_w", "post_b", "gate", "pre_w", "pre_b", "stats"):
+        with pytest.raises(B.ZLError) as err:
+            call_forward(B, dtype=dtype, post=2, pre=2, **{name: Q})
+        assert err.value.status == B.ZL_ERR_ARG, name
+    for name in ("h_out", "f", "dn", "dh_out", "dh", "df", "post_w", "post_b", "gate", "pre_w", "stats", "dpost_w", "dpost_b", "dgate", "dpre_w", "dpre_b"):
+        with pytest.raises(B.ZLError) as err:
+            call_backward(B, dtype=dtype, post=2, pre=2, **({"f_q": None, "f_e": None} if name == "f" else {}), **{name: Q})
+        assert err.value.status == B.ZL_ERR_ARG, name
+
+
 def test_struct_matches_the_header(B):
     import ctypes
     from tests.test_abi import _header_struct_fields
