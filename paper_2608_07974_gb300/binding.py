@@ -420,6 +420,15 @@ def _rows_ptr(t, want, rows: int, cols: int, ld: int, cur: int, name: str):
     return t.data_ptr()
 
 
+def _workspace(ws, want, cur: int):
+    """(pointer, bytes) of a workspace, whose size the call checks: a tensor, or None where it needs none."""
+    if ws is None:
+        return None, 0
+    if ws.__class__ is int:
+        raise TypeError("ws: an address, expected a uint8 tensor (an address has no size)")
+    return _ptr(ws, want, 0, cur, "ws"), ws.numel()
+
+
 def zl_op_act8_store(dtype: int, fmt: int, x, N: int, d: int, ldx: int, q, e, stream: int = 0) -> None:
     """x: 2-D, rows of d values ldx apart."""
     torch, f32, bf16, u8 = _types or _torch()
@@ -464,7 +473,7 @@ def zl_op_act8_dw(dtype: int, fmt: int, M: int, N: int, K: int, A, q, e, Cm, acc
     cur, g = _here(torch), (N + 31) // 32
     _check(_lib.zl_op_act8_dw(dtype, fmt, M, N, K, _ptr(A, bf16 if dtype == ZL_DTYPE_BF16 else f32, K * M, cur, "A"),
                               _ptr(q, u8, K * g * 32, cur, "q"), _ptr(e, u8, K * g, cur, "e"), _ptr(Cm, f32, M * N, cur, "C"),
-                              accumulate, _ptr(ws, u8, 0, cur, "ws"), 0 if ws is None else ws.numel(), stream))
+                              accumulate, *_workspace(ws, u8, cur), stream))
 
 
 def zl_op_block_norm(p: zl_block_norm, h, f, post_w, post_b, gate, pre_w, pre_b, h_out, n_out, stats, f_q=None, f_e=None,
@@ -499,8 +508,7 @@ def zl_op_block_norm_bwd(p: zl_block_norm, h_out, f, f_q, f_e, post_w, post_b, g
         _ptr(gate, f32, ng, cur, "gate"), _ptr(pre_w, f32, d, cur, "pre_w"), _ptr(stats, f32, 4 * N, cur, "stats"),
         _ptr(dn, at, n, cur, "dn"), _ptr(dh_out, at, n, cur, "dh_out"), _ptr(dh, at, n, cur, "dh"), _ptr(df, at, n, cur, "df"),
         _ptr(dpost_w, f32, d, cur, "dpost_w"), _ptr(dpost_b, f32, d, cur, "dpost_b"), _ptr(dgate, f32, ng, cur, "dgate"),
-        _ptr(dpre_w, f32, d, cur, "dpre_w"), _ptr(dpre_b, f32, d, cur, "dpre_b"), _ptr(ws, u8, 0, cur, "ws"),
-        0 if ws is None else ws.numel(), stream))
+        _ptr(dpre_w, f32, d, cur, "dpre_w"), _ptr(dpre_b, f32, d, cur, "dpre_b"), *_workspace(ws, u8, cur), stream))
 
 
 def zl_profile(ctx, on: bool) -> None:

@@ -148,6 +148,15 @@ def test_binding_checks_tensors(B):
         B.zl_op_act8_store(0, 0, P, 4, 64, 64, q.to(torch.int8), e)
 
 
+def test_binding_takes_no_workspace_by_address(B):
+    """An address says nothing of its size: refused by name (it ended in an AttributeError)."""
+    p = B.zl_block_norm(dtype=0, post_norm=1, pre_norm=1, N=4, d=64, gate_rows=0, eps=1e-5, res_scale=1, branch_scale=1, fmt=0, accumulate=0)
+    for call in (lambda: B.zl_op_act8_dw(1, 0, 32, 64, 16, P, P, P, P, 0, P),
+                 lambda: B.zl_op_block_norm_bwd(p, P, P, None, None, P, None, None, P, P, P, P, P, P, None, None, None, None, None, P)):
+        with pytest.raises(TypeError, match="ws"):
+            call()
+
+
 @gpu
 def test_binding_checks_device_tensors(B):
     x = torch.zeros(4, 128, device="cuda")
