@@ -8,6 +8,7 @@
 #pragma once
 #include <cuda_fp8.h>
 
+#include <exception>
 #include <initializer_list>
 #include <string>
 
@@ -384,9 +385,14 @@ template <typename F>
 zl_status entry(F&& body) {
   try {
     return body();
+  } catch (const std::exception& e) {   // (out of host memory)
+    try {
+      set_last_error(e.what());
+    } catch (...) {
+    }
   } catch (...) {
-    return ZL_ERR_CUDA;
   }
+  return ZL_ERR_CUDA;
 }
 inline zl_status fail(zl_status st, const char* msg) {
   set_last_error(msg);
