@@ -246,7 +246,6 @@ struct DwPlan {
   bool copy_a;               // A through the workspace: cut into terms, or its rows onto 16 bytes
   size_t b, a, splits;       // bytes of the workspace's pieces
 };
-size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 DwPlan dw_plan(int dtype, int M, int N, int K) {
   DwPlan p;
   p.Mp = (M + 7) / 8 * 8;

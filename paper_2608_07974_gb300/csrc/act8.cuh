@@ -276,18 +276,10 @@ struct Piece<kSingle, T> {
     act8::floats(r, f);
   }
 };
-template <int MODE, typename T>
+// Rows of whole vectors (kWhole).
+template <typename T>
 __device__ __forceinline__ void store_raw(T* p, int c, int d, const Raw8<T>& r) {
-  if (MODE == kWhole ? c < d : MODE == kTail && c + 8 <= d) {
-    r.set(p + c);
-    return;
-  }
-  if (MODE == kWhole) return;
-  float f[8];
-  floats(r, f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < d) p[c + i] = from_f<T>(f[i]);
+  if (c < d) r.set(p + c);
 }
 template <int MODE, typename T>
 __device__ __forceinline__ void store8(T* p, int c, int d, const float* f) {
@@ -403,6 +395,8 @@ inline zl_status launched(const char* what) {
   return e == cudaSuccess ? ZL_OK : fail(ZL_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
 }
 
+// Bytes of a workspace's piece, so that the next one starts on 256.
+inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 // Whether every pointer lies on elements of that many bytes (a kernel faults on others).
 inline bool on_elements(std::initializer_list<const void*> ps, size_t bytes) {
   for (const void* p : ps)

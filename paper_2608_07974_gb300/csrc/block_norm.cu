@@ -106,11 +106,11 @@ __device__ __forceinline__ void row_get(Raw8<T>& r, bool words, const uint8_t* s
   }
 }
 
-// Sums over the block of one or two values; every thread gets them. The scratch (zeroed before, for the warps that do not
+// Sums over the block; every thread gets them. The scratch (zeroed before, for the warps that do not
 // exist) alternates between two buffers, so one barrier per sum is enough: who writes a buffer again has passed the barrier
 // of the sum between, after which everyone had read it.
 struct Reducer {
-  float (*sh)[2][16];
+  float (*sh)[16];
   int turn;
   __device__ __forceinline__ static float total(const float* b) {
     uint64_t v[8];
@@ -128,7 +128,7 @@ struct Reducer {
     return f.x + f.y;
   }
   __device__ __forceinline__ void sum(float& x) {
-    float* b = sh[turn][0];
+    float* b = sh[turn];
     turn ^= 1;
     x = warp_sum(x);
     if ((threadIdx.x & 31) == 0) b[threadIdx.x >> 5] = x;
@@ -155,22 +155,6 @@ struct Reducer {
     for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __shfl_sync(0xffffffffu, v, 8 * i);
-  }
-  __device__ __forceinline__ void sum(float& x, float& y) {
-    float(*b)[16] = sh[turn];
-    turn ^= 1;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      x += __shfl_xor_sync(0xffffffffu, x, o);
-      y += __shfl_xor_sync(0xffffffffu, y, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-      b[0][threadIdx.x >> 5] = x;
-      b[1][threadIdx.x >> 5] = y;
-    }
-    __syncthreads();
-    x = total(b[0]);
-    y = total(b[1]);
   }
 };
 
@@ -207,7 +191,7 @@ __device__ __forceinline__ void put_nan(T* p, int c, int d) {
   const uint64_t v[4] = {nan2, nan2, nan2, nan2};
   Raw8<T> r;
   pack8(v, r);
-  store_raw<kWhole>(p, c, d, r);
+  store_raw(p, c, d, r);
 }
 
 // What a launch of a ring kernel is given besides its operands.
@@ -316,7 +300,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
     fwd_ring_k(const __grid_constant__ Fwd a, const Ring g) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ uint64_t full[kStages];
-  __shared__ __align__(16) float sh[2][2][16];
+  __shared__ __align__(16) float sh[2][16];
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
   const int t = threadIdx.x, nt = blockDim.x;
@@ -327,7 +311,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = t; i < 64; i += nt) (&sh[0][0][0])[i] = 0.f;
+  if (t < 32) (&sh[0][0])[t] = 0.f;
   for (int k = 0; k < 2 * g.stages; ++k)   // columns past d read 0
     for (int c = a.d + t; c < a.D; c += nt) reinterpret_cast<T*>(ring + (k >> 1) * g.stage + (k & 1) * g.pitch)[c] = from_f<T>(0.f);
   __syncthreads();
@@ -471,7 +455,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
         if (!VEC) cut<VEC>(h[j], c, a.d);   // (0 past d is NaN times 0 in a row with a NaN)
         Raw8<T> out;
         pack8(h[j], out);
-        if (VEC) store_raw<kWhole>((T*)a.ho + o, c, a.d, out);
+        if (VEC) store_raw((T*)a.ho + o, c, a.d, out);
         else store_any((T*)a.ho + o, c, a.d, out);
       }
     }
@@ -500,7 +484,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
       if (!VEC || KEEP >= 0) cut<VEC>(h[j], c, a.d);
       Raw8<T> out;
       pack8(h[j], out);
-      if (VEC) store_raw<kWhole>((T*)a.no + o, c, a.d, out);
+      if (VEC) store_raw((T*)a.no + o, c, a.d, out);
       else store_any((T*)a.no + o, c, a.d, out);
       if (KEEP >= 0 && a.nq) {   // of n as it is stored
         float n[8];
@@ -1291,7 +1275,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const __grid_constant__ Bwd a,
         if (a.dh) {
           Raw8<T> out;
           pack8(v, out);
-          if (VEC) store_raw<kWhole>((T*)a.dh + o, c, a.d, out);
+          if (VEC) store_raw((T*)a.dh + o, c, a.d, out);
           else store_any((T*)a.dh + o, c, a.d, out);
         }
 #pragma unroll
@@ -1305,7 +1289,7 @@ __global__ void __launch_bounds__(512) bwd_ring_k(const __grid_constant__ Bwd a,
         }
         Raw8<T> out;
         pack8(v, out);
-        if (VEC) store_raw<kWhole>((T*)a.df + o, c, a.d, out);
+        if (VEC) store_raw((T*)a.df + o, c, a.d, out);
         else store_any((T*)a.df + o, c, a.d, out);
       }
     }
@@ -1587,7 +1571,6 @@ bool backward(const Bwd& a, cudaStream_t s) {
 }
 
 int part_slots(const zl_block_norm& p) { return p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER ? 4 : 2; }
-size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 bool dims_ok(const zl_block_norm* p) {
   auto norm = [](int k) { return k >= ZL_NORM_NONE && k <= ZL_NORM_LAYER; };
