@@ -106,9 +106,9 @@ __device__ __forceinline__ void row_get(Raw8<T>& r, bool words, const uint8_t* s
   }
 }
 
-// Sums over the block; every thread gets them. The scratch (zeroed before, for the warps that do not
-// exist) alternates between two buffers, so one barrier per sum is enough: who writes a buffer again has passed the barrier
-// of the sum between, after which everyone had read it.
+// Sums over the block; every thread gets them. The scratch (zeroed before, for the warps that do not exist) alternates between
+// two buffers, so one barrier per sum is enough: who writes a buffer again has passed the barrier of the sum between, after
+// which everyone had read it.
 struct Reducer {
   float (*sh)[16];
   int turn;
