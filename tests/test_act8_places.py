@@ -141,3 +141,81 @@ def test_segments_bound_the_truncation(B, monkeypatch, dtype, plan, N, off):
     err = float((C.double() - ref).norm() / ref.norm())
     print(f"relative error {err:.2e}")
     assert err <= 64.5 * 2.0 ** -23 + 1.5 * 16.5 * 2.0 ** -24, err
+
+
+def big(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+
+@pytest.fixture
+def room():
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+TAIL = 70
+
+
+def test_activation_beyond_32_bits(B, room):
+    """More than 2^32 values of x: the last rows as in a call of their own."""
+    f, dt = 11008, B.ZL_DTYPE_BF16
+    N = (1 << 32) // (2 * f) + 2 * TAIL
+    x, y, again, dx, dy = big(N, 2 * f), big(N, f), big(N, f), big(N, 2 * f), big(N, f)
+    q, e = big(2 * N, f, dtype=torch.uint8), big(2 * N, f // 32, dtype=torch.uint8)
+    x[-TAIL:].normal_()
+    dy[-TAIL:].normal_()
+    B.zl_op_act8_act(dt, R.SWIGLU, R.INT8, x, N, f, y, q, e)
+    B.zl_op_act8_act_bwd(dt, R.SWIGLU, R.INT8, q, e, dy, N, f, dx, again)
+    y2, again2, dx2 = big(TAIL, f), big(TAIL, f), big(TAIL, 2 * f)
+    q2, e2 = big(2 * TAIL, f, dtype=torch.uint8), big(2 * TAIL, f // 32, dtype=torch.uint8)
+    B.zl_op_act8_act(dt, R.SWIGLU, R.INT8, x[-TAIL:], TAIL, f, y2, q2, e2)
+    B.zl_op_act8_act_bwd(dt, R.SWIGLU, R.INT8, q2, e2, dy[-TAIL:], TAIL, f, dx2, again2)
+    for a, b in ((y, y2), (again, again2), (dx, dx2), (q, q2), (e, e2)):
+        assert torch.equal(a[-len(b):], b)
+        assert bool((a[:-len(b)] == (10 if a is e else 0)).all())
+
+
+@pytest.mark.parametrize("d", [4096, 4095, 9000])
+def test_block_norm_beyond_32_bits(B, room, d):
+    """More than 2^32 values a tensor: the last rows as in a call of their own (each kernel's rows do not depend on their number)."""
+    N, D, dt = (1 << 32) // d + 2 * TAIL, R.width(d), B.ZL_DTYPE_BF16
+    h, f, ho, n = big(N, d), big(N, d), big(N, d), big(N, d)
+    st, (fq, fe) = big(4, N, dtype=torch.float32), (big(N, D, dtype=torch.uint8), big(N, D // 32, dtype=torch.uint8))
+    h[-TAIL:].normal_()
+    f[-TAIL:].normal_()
+    w = torch.rand(d, device="cuda") + 0.5
+
+    def call(rows, *t):
+        p = B.zl_block_norm(dtype=dt, post_norm=R.RMS, pre_norm=R.RMS, N=rows, d=d, gate_rows=0, eps=1e-5, res_scale=1, branch_scale=0.5, fmt=0, accumulate=0)
+        h_, f_, ho_, n_, st_, fq_, fe_ = t
+        B.zl_op_block_norm(p, h_, f_, w, None, None, w, None, ho_, n_, st_, fq_, fe_)
+        ws = torch.empty(B.zl_op_block_norm_bwd_bytes(p), dtype=torch.uint8, device="cuda")
+        dn, dh, df = n_, h_, f_          # n as its own gradient; the inputs are not needed any more
+        B.zl_op_block_norm_bwd(p, ho_, None, fq_, fe_, w, None, None, w, st_, dn, None, dh, df, None, None, None, None, None, ws)
+
+    small = [h[-TAIL:].clone(), f[-TAIL:].clone(), big(TAIL, d), big(TAIL, d), big(4, TAIL, dtype=torch.float32), big(TAIL, D, dtype=torch.uint8),
+             big(TAIL, D // 32, dtype=torch.uint8)]
+    call(TAIL, *small)
+    call(N, h, f, ho, n, st, fq, fe)
+    for a, b in zip((h, f, ho, n, st.t(), fq, fe), [t.t() if t.shape[0] == 4 and t.dtype == torch.float32 else t for t in small]):
+        assert torch.equal(a[-TAIL:], b)
+    for t in (h, f, ho, n, fq):
+        assert not bool(t[:-TAIL].any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weight_gradient_beyond_32_bits(B, room, dtype):
+    """More than 2^32 values of X, nothing in the first rows but zeros: the gradient of the last ones."""
+    M, N, K, dt, T = 64, 8200, 525000, test_act8.code(B, dtype), R.DT[dtype]
+    A, x = big(K, M, dtype=T), torch.randn(TAIL, N, device="cuda").to(T)
+    q, e = big(K, R.width(N), dtype=torch.uint8), torch.full((K, R.width(N) // 32), 10, dtype=torch.uint8, device="cuda")
+    A[-TAIL:].normal_()
+    A[:-TAIL] = 1
+    B.zl_op_act8_store(dt, R.E4M3, x, TAIL, N, N, q[-TAIL:], e[-TAIL:])
+    ws = torch.empty(B.zl_op_act8_dw_bytes(dt, M, N, K), dtype=torch.uint8, device="cuda")
+    C = torch.full((M, N), float("nan"), device="cuda")
+    B.zl_op_act8_dw(dt, R.E4M3, M, N, K, A, q, e, C, 0, ws)
+    X = R.load(q[-TAIL:].cpu(), e[-TAIL:].cpu(), R.E4M3, N)
+    a = A[-TAIL:].double().cpu()
+    R.assert_close(C, a.T @ X, (TAIL + 64) * 2.0 ** -23 * (a.abs().T @ X.abs()), "C")
