@@ -352,7 +352,9 @@ zl_status zl_op_act8_act_bwd(int dtype, int act, int fmt, const uint8_t* q, cons
 /* Weight gradient of a linear from the checkpoint of its input: C [M, N] fp32 = A^T X (accumulate 0) or
  * C += A^T X (accumulate 1), A [K, M] (dtype) the gradient at the linear's output, X [K, N] held as q, e
  * (K rows of N columns): mode 2 of zl_op_gemm with its B in 8 bits. The products run on the tensor cores
- * with fp32 sums; an fp32 A is taken in three bf16 terms, which hold all its digits down to 2^-133. A
+ * with fp32 sums, which are truncated within 2048 rows and rounded between such segments (relative to an
+ * fp64 product 6e-7 for values of both signs; for values of one sign 3e-7 over 2048 rows, 4e-6 over 65536);
+ * an fp32 A is taken in three bf16 terms, which hold all its digits down to 2^-133. A
  * must be 16-byte aligned. ws: a device buffer of at least zl_op_act8_dw_bytes bytes, 256-byte aligned, that no
  * other call uses meanwhile (nor another graph that may run at the same time). */
 zl_status zl_op_act8_dw_bytes(int dtype, int M, int N, int K, size_t* bytes);

@@ -292,8 +292,8 @@ __device__ __noinline__ void fwd_give_up(const Fwd& a, int n, int end) {
 
 // Forward. VEC: rows come by bulk copies. KEEP: the format that f or n are written in, -1: neither is. LN: one of the norms
 // is a LayerNorm. HBM-bound on large batches, 8 bytes a value in bf16 (10.06 with both checkpoints): 4096 x 8192 with RMS
-// norms 45 us (6.0 TB/s, 88% of the measured copy rate; with checkpoints 66 us); on 2048 x 4096, where a block has six or seven
-// rows, the launch, the first rows' copies and the sums' latency show: 15.7 us (20.4 with checkpoints), LayerNorms, with four
+// norms 46 us (5.8 TB/s, 86% of the measured copy rate; with checkpoints 69 us); on 2048 x 4096, where a block has six or seven
+// rows, the launch, the first rows' copies and the sums' latency show: 15.7 us (20.9 with checkpoints), LayerNorms, with four
 // sums a row, 21.1. A block for each row, which waits for it and reads the parameters anew, took 35 and 43 us.
 template <typename T, int VPT, bool VEC, bool LN, int KEEP>
 __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) == 4) ? 128 : VPT == 1 ? 64 : 80)
@@ -941,9 +941,9 @@ __global__ void __launch_bounds__(256) bwd_rows_k(const Bwd a) {
 // and of v fh. These are linear in m1 and m2: with g = dh' + r u,
 //   sum v fh = sum A fh g - r m1 sum A fh - r m2 sum A fh xh,   sum v = sum A g - r m1 sum A - r m2 sum A xh
 // so one barrier a row yields every mean: three sums with RMS norms, eight at most.
-// HBM-bound on large batches, 11.03 bytes a value in bf16 with f from its checkpoint: 4096 x 8192 73 us (5.1 TB/s, 75% of the
-// measured copy rate; without gradients of parameters 65 us); 2048 x 4096 27.5 us, of which the partial sums and their
-// joining kernel take 6, launch and the first rows 4; LayerNorms 33.8. Three kernels that each read the rows took 91 us, two
+// HBM-bound on large batches, 11.03 bytes a value in bf16 with f from its checkpoint: 4096 x 8192 71 us (5.2 TB/s, 76% of the
+// measured copy rate; without gradients of parameters 65 us); 2048 x 4096 27.1 us, of which the partial sums and their
+// joining kernel take 6, launch and the first rows 4; LayerNorms 34.2. Three kernels that each read the rows took 91 us, two
 // barriers a row in one kernel 38.6.
 // ------------------------------------------------------------------------------------------------
 // The normalised f, (f - pm) pr, at column c of row g in shared memory (a row of T, or of codes whose group byte is e).
@@ -1502,8 +1502,8 @@ int ring_slots(int d, bool ln) {
 }
 // What the ring kernel needs behind the ring: w_pre, A, and with gate groups within a chunk the post norm's sums.
 size_t bwd_prm(int D, bool ln, int per_group) { return (size_t)D * 4 * (2 + (per_group ? 0 : ln ? 2 : 1)); }
-// The chunks, and whether the ring kernel takes the rows: up to 8192 columns, and what does not fit in shared memory (fp32
-// LayerNorms beyond 7100 columns with several gate groups to a chunk) not.
+// The chunks, and whether the ring kernel takes the rows: up to 8192 columns, and what does not fit in shared memory not (fp32
+// with gate groups that lie whole in a chunk: LayerNorms beyond 7136 columns, RMS norms beyond 8128).
 bool plan_chunks(const zl_block_norm& p, int& rows, int& per_group, int& chunks) {
   const bool ln = p.post_norm == ZL_NORM_LAYER || p.pre_norm == ZL_NORM_LAYER;
   if (p.d <= kRingCols) {

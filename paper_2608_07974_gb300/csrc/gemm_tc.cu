@@ -162,11 +162,13 @@ __device__ __forceinline__ void unit_tile(const Args& g, int unit, int num_tiles
 // first CTA issues read both CTAs' shared memory. What bounds the single-CTA mainloop is shared memory (128
 // bytes a cycle): a 128 x 256 x 64 block reads 48 KB and its copies write 48 KB, 768 cycles against 512 of
 // products. A pair's CTA reads and writes 32 KB each per 512 cycles, and six stages fit instead of four.
-// DW (a kernel of its own too, mode 2 or 3): the accumulation is cut into segments of kb_per_seg k blocks. The tensor cores
+// DW (a kernel of its own too, mode 2, 3 or 5): the accumulation is cut into segments of kb_per_seg k blocks. The tensor cores
 // truncate as they add to an accumulator, an error that grows with the number of additions and always points to zero:
-// relative to an fp64 product 3.5e-6 over K = 8192 in one accumulation, 1.35e-5 over 65536 (an fp32 library product 3.5e-7
-// and 1e-6). Segments of at most 2048 are added to C by the TMA unit, which rounds to nearest: 9e-7 and less at any K. The
-// epilogue of a segment runs under the products of the next one, C's tiles stay in L2 meanwhile.
+// relative to an fp64 product (2-norm) 3.5e-6 over K = 8192 normal values in one accumulation, 1.35e-5 over 65536 (an fp32
+// library product 3.5e-7 and 1e-6), 3.1e-4 over 65536 values of one sign and many sizes. Segments of at most 2048 are added to
+// C by the TMA unit, which rounds to nearest: normal values 6.3e-7 at K = 2048 and 8192 (library 1.5e-7, 3.5e-7), 9e-7 and less
+// beyond; of one sign 3.4e-7, 1.7e-6 and 4.1e-6 over 2048, 8192 and 65536 (library 1e-7, 1.7e-7, 1.2e-7). The epilogue of a
+// segment runs under the products of the next one, C's tiles stay in L2 meanwhile. A wait that gives up leaves NaN in C.
 template <int BN, bool A_MN, bool B_MN, bool UPD = false, bool PAIR = false, bool DW = false>
 __global__ void __launch_bounds__(UPD ? kThreadsUpd : kThreads, 1)
     gemm_tc_k(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
