@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(LN || (VPT == 2 && sizeof(T) 
     }
   }
   if (!VEC || k == rows) return;
-  if (t == 0) drain(full, at, g.stages, min(rows - k, g.stages));
+  if (t == 0) drain(full, at, g.stages, min(rows - k, g.stages + 1));   // (one more: the row at hand's stage may be filling again)
   fwd_give_up<T, KEEP>(a, r0 + k, r0 + rows);
 }
 
