@@ -669,6 +669,7 @@ struct RowTerms {
   // Sums s e^{m / T} as m and 1 / s: of the others, all, all at T = 1 (TWO), the teacher's. Probabilities go by x - m, which is exact
   // or nearly so, and not by x - log sum, whose rounding (2^-24 of 20 or 40) would be in all of a row's.
   float om, oi, pr, am, ai, cm, ci, qm, qi;   // pr: the others' probability
+  float bad;                       // NaN where the row has no softmax (a NaN, +inf or nothing but -inf in it), else 0
 };
 struct LossShared {
   Lse p[kWarps], c[kWarps], r[kWarps], q[kWarps];   // the warps' sums: others, all (TWO), record, teacher
@@ -861,9 +862,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
       t.lseq = vocab::lse_value(Q, 1.f);
       t.lpr = vocab::lse_value(P, inv_T) - t.lse;
       t.lqr = rest - t.lseq;
-      const bool none = P.m <= -vocab::kFar;   // no others, or only masks: e_v 0 (NaN where the whole row is -inf)
+      t.bad = A.m == -INFINITY ? __uint_as_float(0x7FC00000u) : A.s * 0.f;
+      const bool none = P.m <= -vocab::kFar;   // no others, or only masks: e_v 0
       t.om = none ? 0.f : P.m;
-      t.oi = A.m == -INFINITY ? __uint_as_float(0x7FC00000u) : none ? 0.f : 1.f / P.s;
+      t.oi = none ? 0.f : 1.f / P.s;
       t.pr = none ? 0.f : P.s * ex2((P.m - A.m) * s) / A.s;
       t.am = A.m;
       t.ai = 1.f / A.s;
@@ -880,7 +882,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
   auto p_of = [&](float x) { return ex2((x - t.am) * s) * t.ai; };
   auto q_of = [&](float x) { return ex2((x - t.qm) * kL2e) * t.qi; };
   // the divergence
-  auto xlog = [](float p, float d) { return p > 0.f ? p * d : 0.f; };
+  auto xlog = [](float p, float d) { return p == 0.f ? 0.f : p * d; };   // (a p of NaN stays)
   float kl = 0.f;
   if (mass) {
     if (warp < kw) {
@@ -902,12 +904,12 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
   // Pass 2, of a column v outside the record: with e_v = e^{x_v - others} (its share of the others' mass) p_v = p_r e_v, and
   // T dKL/dz_v = e_v (p_r - q_r) (dir 1) or e_v p_r (lp_r - lq_r - KL) (dir 0): no quotient of probabilities near 0.
   // dz_v = wa p1_v + wk other e_v; without a second softmax p1_v = p_r e_v.
-  const float w = 1.f / t.omega, wa = w * a.alpha, wk = mass ? w * (1.f - a.alpha) * a.T : 0.f;
+  const float w = 1.f / t.omega, wa = w * a.alpha, wk = (mass ? w * (1.f - a.alpha) * a.T : 0.f) + t.bad;
   float other = t.pr;
   if (has_rest) other = a.dir == 1 ? t.pr - q_of(rest) : xlog(t.pr, t.lpr - t.lqr - kl);
   const float ck = (wk == 0.f ? 0.f : wk * other) * t.oi, cs = fmaf(wa, t.pr * t.oi, ck), c1 = wa * t.ci;
   if (rank == 0 && tid == 0)
-    a.row_loss[row] = (a.alpha > 0.f ? a.alpha * (t.lse1 - zy) : 0.f) + (kl_on ? (1.f - a.alpha) * a.T * a.T * kl : 0.f);
+    a.row_loss[row] = (a.alpha > 0.f ? a.alpha * (t.lse1 - zy) : 0.f) + (kl_on ? (1.f - a.alpha) * a.T * a.T * kl : 0.f) + t.bad;
   const uint64_t s2 = f2(s, s), cs2 = f2(TWO ? ck : cs, TWO ? ck : cs), c12 = f2(c1, c1), L2 = f2(kL2e, kL2e);
   const uint64_t om2 = f2(-t.om, -t.om), cm2 = f2(-t.cm, -t.cm);
   auto grad = [&](float x) {
