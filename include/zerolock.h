@@ -451,7 +451,8 @@ zl_status zl_op_top_logits(int dtype, const void* z, int N, int V, int ld, int k
  * rest (from zl_op_top_logits at the same T); with rest NULL the teacher is the record alone (its k values at T, renormalised),
  * the student its softmax over all V columns. kl_dir 0: KL(p || teacher) (needs rest), 1: KL(teacher || p). idx, val: [N, k],
  * as above; an entry whose column lies outside [0, V) is left out, as is one whose column came earlier in the row, so a
- * record may hold fewer than k. A record without any mass (every val and rest -inf) adds no divergence.
+ * record may hold fewer than k. A record without any mass (every val and rest -inf) adds no divergence;
+ * a NaN or +inf in a val that counts, or in rest, makes that row's loss and gradient NaN (a teacher's NaN comes that way).
  * A teacher's mass of 0 where p has some makes kl_dir 0 infinite (and 1 the reverse), as its formula says. alpha 1 reads no
  * record and ignores T (idx, val, rest may be NULL). Writes dz = dloss/dz [N, ld] (dtype, may be z; columns V .. ld - 1 become 0). */
 zl_status zl_op_top_loss(int dtype, const void* z, const int32_t* idx, const float* val, const float* rest,

@@ -101,3 +101,47 @@ def test_a_broken_student_row_against_an_empty_record(B, alpha, kl_dir):
         z[r, :V] = -math.inf
         check_row_is_nan(loss_of(B, "f32", z, rec, y, V, alpha, 1.0, kl_dir), want, r, V)
         z[r] = clean
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,ld,off,k", SHAPES)
+@pytest.mark.parametrize("alpha", [0.0, 0.5])
+@pytest.mark.parametrize("kl_dir,with_rest", [(0, 1), (1, 1), (1, 0)])
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_a_broken_teacher_row(B, dtype, N, V, ld, off, k, alpha, kl_dir, with_rest, T):
+    """A NaN or +inf among the record's values or as its rest: no divergence is known. With an entry that is left out it goes too,
+    and with alpha 1 nothing of the record is read."""
+    z, t, y = case(dtype, N, V, ld, off, 13)
+    idx, val, rest = record(B, dtype, t, V, k, T)
+    r = 1
+
+    def go(idx, val, rest, a=alpha):
+        return loss_of(B, dtype, z, (idx, val, rest if with_rest else None), y, V, a, T, kl_dir)
+
+    want = go(idx, val, rest)
+    for bad in (math.nan, math.inf):
+        for at in (0, k // 2, k - 1):
+            v = val.clone()
+            v[r, at] = bad
+            check_row_is_nan(go(idx, v, rest), want, r, V)
+        if with_rest:
+            u = rest.clone()
+            u[r] = bad
+            check_row_is_nan(go(idx, val, u), want, r, V)
+        i, v, v2 = idx.clone(), val.clone(), val.clone()
+        i[r, 2], v[r, 2], v2[r, 2] = -1, bad, 0.0
+        for a, b in zip(go(i, v, rest), go(i, v2, rest)):
+            assert torch.equal(a, b) and not bool(torch.isnan(b).any())
+        v[r] = bad
+        for a, b in zip(go(idx, v, rest, 1.0), go(idx, val, rest, 1.0)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kl_dir", [0, 1])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_teacher_that_diverged(B, kl_dir, bad):
+    """Its logits to the record to the loss: NaN arrives."""
+    z, t, y = case("bf16", 7, 1000, 1008, 0, 14)
+    want = loss_of(B, "bf16", z, record(B, "bf16", t, 1000, 12, 1.0), y, 1000, 0.5, 1.0, kl_dir)
+    t[1, 400] = bad
+    check_row_is_nan(loss_of(B, "bf16", z, record(B, "bf16", t, 1000, 12, 1.0), y, 1000, 0.5, 1.0, kl_dir), want, 1, 1000)
