@@ -420,10 +420,9 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
 
 /* Cross entropy of the logits z = n W^T (n [N, d], W [V, d], dtype, dense, 16-byte aligned; d % 8 == 0, 8 <= d <= 2^16) that
  * never lie in memory: row_loss_i = lse_i - z_iy, lse [N] fp32 = log sum_v exp(z_iv) (of every row, in Omega or not). The
- * products run on the tensor cores with fp32 sums; an fp32 operand is taken in three bf16 terms, six products of them: up to 1024
- * rows each term holds the leading bits that the ones before it left; above, the terms hold a row to within 2^-24 of the next power of
- * two above its largest magnitude. ws: a device buffer of at least zl_op_vocab_loss_bytes bytes (fp32: the terms of n and, above 1024
- * rows, of W are in it), 256-byte aligned. */
+ * products run on the tensor cores with fp32 sums; an fp32 operand is taken in three bf16 terms, each the leading 8 bits that the ones
+ * before it left, and six products of them (what is left out is below 2^-21 of |a| |b|). ws: a device buffer of at least
+ * zl_op_vocab_loss_bytes bytes (fp32: the terms of n and, above 1024 rows, of W are in it), 256-byte aligned. */
 zl_status zl_op_vocab_loss_bytes(int dtype, int N, int d, int V, size_t* bytes);
 zl_status zl_op_vocab_loss(int dtype, const void* n, const void* W, const int32_t* labels, int N, int d, int V, float* row_loss,
                            float* lse, float* loss, void* ws, size_t ws_bytes, void* stream);

@@ -58,8 +58,6 @@ struct Args {
   int splits, kb_per_split, kb_per_seg, kb_small;   // kb_small: k blocks of the smaller pairs of terms
   uint32_t pair_a, pair_b;           // pair tables
   int a_term, b_term, b_first;       // rows between terms, first row of B
-  const float *a_scale, *b_scale;    // digits: of A's rows, of B's rows from b_first on
-  const float* row_scale;            // kOut32: C's rows are divided by it
   // kLse
   const int32_t* labels;
   float2* part;
@@ -89,19 +87,6 @@ __device__ __forceinline__ void unit_tile(const Args& g, int unit, int num_tiles
   tm = first + r % gm;
   tn = r / gm;
   if (pair) tm = 2 * tm + (int)crank;
-}
-
-// x[e] *= s sc[e], one after the other (both are powers of two: no rounding, and their product may be out of range).
-template <int N>
-__device__ __forceinline__ void scale_columns(float* x, float s, const float* __restrict__ sc) {
-#pragma unroll
-  for (int e = 0; e < N; e += 4) {
-    const float4 t = *reinterpret_cast<const float4*>(sc + e);
-    x[e] = x[e] * s * t.x;
-    x[e + 1] = x[e + 1] * s * t.y;
-    x[e + 2] = x[e + 2] * s * t.z;
-    x[e + 3] = x[e + 3] * s * t.w;
-  }
 }
 
 template <bool A_MN, bool B_MN, int KIND, bool PAIR, bool DIRECT>
@@ -427,7 +412,6 @@ __global__ void __launch_bounds__(DIRECT ? kThreadsDirect : kThreads, 1)
         unit_tile(g, unit, num_tiles, PAIR, crank, tm, tn);
         const int m = tm * BM + q * 32 + lane, n0 = tn * g.bn;
         const int y = m < g.M ? g.labels[m] : -1;
-        const float sa = g.a_scale && m < g.M ? g.a_scale[m] : 1.f;
         if (!(ok = gather(0, g.nk))) break;
         Lse A = lse_empty();
 #pragma unroll
@@ -436,7 +420,6 @@ __global__ void __launch_bounds__(DIRECT ? kThreadsDirect : kThreads, 1)
           const int nv = min(g.bn - c, g.N - n0 - c);   // columns of the tile and of the vocabulary
           if (nv <= 0) continue;
           float (&x)[32] = *reinterpret_cast<float (*)[32]>(&v[32 * j]);
-          if (g.a_scale) scale_columns<32>(x, sa, g.b_scale + n0 + c);
           if (nv < 32) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = e < nv ? x[e] : -INFINITY;
@@ -471,14 +454,11 @@ __global__ void __launch_bounds__(DIRECT ? kThreadsDirect : kThreads, 1)
         const int kb0 = split * g.kb_per_split, kbe = min(g.nk, kb0 + g.kb_per_split);
         if (kb0 >= kbe) continue;   // (a shorter last piece of the vocabulary)
         int y = -1;
-        float l = 0.f, sa = 1.f;
+        float l = 0.f;
         if (KIND == kGradZ && m < g.M) {   // under way while the accumulator is waited for
           y = g.labels[m];
           l = g.lse[m];
-          if (g.a_scale) sa = g.a_scale[m];
         }
-        if (KIND == kOut32 && g.row_scale && m < g.M) sa = 1.f / g.row_scale[m];
-        if (KIND != kGradZ) sa *= weight;
         if (!(ok = gather(kb0, kbe))) break;
         const bool on = y >= 0 && y < g.V;
 #pragma unroll
@@ -488,7 +468,6 @@ __global__ void __launch_bounds__(DIRECT ? kThreadsDirect : kThreads, 1)
           float* const x = v + CH * j;
           if constexpr (KIND == kGradZ) {
             const int nv = g.V - g.first - n0 - c, e0 = y - g.first - n0 - c;
-            if (g.a_scale) scale_columns<CH>(x, sa, g.b_scale + n0 + c);
             const uint64_t l2 = f2(-l, -l), k2 = f2(kL2e, kL2e);
 #pragma unroll
             for (int e = 0; e < CH; e += 2) {   // (the difference first: it is exact where p is near 1)
@@ -504,11 +483,10 @@ __global__ void __launch_bounds__(DIRECT ? kThreadsDirect : kThreads, 1)
 #pragma unroll
               for (int e = 0; e < CH; ++e) x[e] = on && e < nv ? x[e] : 0.f;
             }
-            if (g.a_scale) scale_columns<CH>(x, 1.f, g.b_scale + n0 + c);
           }
-          if (KIND != kGradZ && (g.row_scale || g.omega)) {
+          if (KIND != kGradZ && g.omega) {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) x[e] *= sa;
+            for (int e = 0; e < CH; ++e) x[e] *= weight;
           }
           if constexpr (KIND == kGradZ) {
             // straight to memory, 32 bytes (a whole sector) at a time: staged for a bulk copy, the fences between the proxies and the
@@ -710,8 +688,6 @@ bool prepare(Args& a, CUtensorMap& ta, CUtensorMap& tb, int M, int N, int K, con
   a.a_term = o.a_term;
   a.b_term = o.b_term;
   a.b_first = o.b_first;
-  a.a_scale = o.a_scale;
-  a.b_scale = o.b_scale ? o.b_scale + o.b_first : nullptr;
   const bool okA = o.a_mn ? map2d(&ta, o.A, (uint64_t)M, (uint64_t)o.a_rows, (uint64_t)o.lda, 64)
                           : map2d(&ta, o.A, (uint64_t)K, (uint64_t)o.a_rows, (uint64_t)o.lda, (uint32_t)box_a);
   a.Bf = (const float*)o.B;
@@ -809,14 +785,13 @@ bool gemm_grad_z(int M, int n, int K, const Operands& o, const Tiles& t, const i
   return t.pair ? launch<false, false, kGradZ, true>(a, ta, tb, ta, s) : launch<false, false, kGradZ, false>(a, ta, tb, ta, s);
 }
 
-bool gemm_out(int M, int N, int K, const Operands& o, const Tiles& t, int out_f32, void* C, int add, const float* row_scale,
-              const float* omega, const float* dloss, cudaStream_t s) {
+bool gemm_out(int M, int N, int K, const Operands& o, const Tiles& t, int out_f32, void* C, int add, const float* omega,
+              const float* dloss, cudaStream_t s) {
   Args a = {};
   CUtensorMap ta, tb, tcm;
   if (!o.b_mn || !prepare(a, ta, tb, M, N, K, o, t) || !map_out(&tcm, C, out_f32 != 0, N, M, t.splits)) return false;
   a.C = C;
   a.add = add;
-  a.row_scale = row_scale;
   a.omega = omega;
   a.dloss = dloss;
   if (o.direct) return launch<false, true, kOut32, false, true>(a, ta, tb, tcm, s);

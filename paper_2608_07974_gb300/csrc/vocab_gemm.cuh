@@ -7,13 +7,11 @@
 namespace zl {
 namespace vocab {
 
-// An fp32 matrix takes part as three bf16 terms, x = h + m + l. Of the nine products of two such matrices the six largest are
-// formed, smallest first; what is left out is below 2^-24 of |a| |b|. Two ways to cut x:
-//   leading bits   h, m and l each the leading 8 bits of what is left: exact
-//   digits         of a row scaled by a power of two s >= max |x|: h, m, l whole multiples of 2^-7, 2^-15, 2^-23 of s, rounded to
-//                  nearest, within 2^-24 s of x. Products of digits h are whole multiples of 2^-14, and 1024 of them add up without
-//                  an error: the tensor cores cut off what does not fit an fp32 sum, towards zero, each time they add 16 products,
-//                  which for logits of 10 or 20 came to several times the rounding of an fp32 product.
+// An fp32 matrix takes part as three bf16 terms, x = h + m + l, each the leading 8 bits of what is left: exact, and every value by
+// itself. (Fixed-point digits under a scale for each row add up without an error in the tensor cores, and the same products took 10%
+// less time; but a row with a column 300 times the others holds those in 16 bits, and a gradient times a small row's scale falls below
+// the smallest bf16.) Of the nine products of two such matrices the six largest are formed, smallest first. What is left out, m l
+// twice and l l, is below 2^-21 of |a| |b| (|m| < 2^-7 |x|, |l| < 2^-15 |x|), with the product's sign.
 constexpr int kTerms = 3, kPairs = 6;
 
 // C [M, N] = A B^T (b_mn 0: B [N, K]) or A B (b_mn 1: B [K, N]), A [M, K] or with a_mn its transpose [K, M]; fp32 sums in
@@ -25,8 +23,7 @@ struct Operands {
   int lda, ldb;                // multiples of 8
   int a_term, b_term, terms;
   int b_first;                 // first row of B (its columns in the product where b_mn is 0)
-  int direct;                  // B is fp32 as it is, its terms (leading bits, like A's) are formed in the product; bn is 128
-  const float *a_scale, *b_scale;   // digits: the rows' scales (b_scale of the rows from 0 on, readable up to 256 past the last)
+  int direct;                  // B is fp32 as it is, its terms are formed in the product; bn is 128
 };
 
 // How a product is cut: tiles of 128 (pair: 256) x bn, `splits` cuts of K, each of several accumulations in TMEM of at most
@@ -48,14 +45,13 @@ bool gemm_lse(int M, int V, int K, const Operands& o, const Tiles& t, const int3
 inline int lse_parts(int V, const Tiles& t) { return 2 * ((V + t.bn - 1) / t.bn); }
 // dz = e^{z - lse} - [label] in the rows of Omega, 0 else, for the columns first .. first + n of a vocabulary of V (0 past it): bf16
 // terms [o.terms][rows_p][ldz], rows M .. rows_p zeros. Without the rows' common weight, whose rounding would be in every value:
-// where p is small, dz is exactly -1 at the label. With scales the columns are multiplied by b_scale (so that a product with B's
-// digits needs no scale).
+// where p is small, dz is exactly -1 at the label.
 bool gemm_grad_z(int M, int n, int K, const Operands& o, const Tiles& t, const int32_t* labels, const float* lse, int first, int V,
                  void* dz, int rows_p, int ldz, cudaStream_t s);
 // C = A B: bf16 C [M, N] (a_mn), or fp32 slices [splits][M, N], one for each split, overwritten or (add) added to.
-// C times loss_weight(omega, dloss) (omega NULL: 1); its rows divided by row_scale (fp32 C, may be NULL).
-bool gemm_out(int M, int N, int K, const Operands& o, const Tiles& t, int out_f32, void* C, int add, const float* row_scale,
-              const float* omega, const float* dloss, cudaStream_t s);
+// C times loss_weight(omega, dloss) (omega NULL: 1).
+bool gemm_out(int M, int N, int K, const Operands& o, const Tiles& t, int out_f32, void* C, int add, const float* omega,
+              const float* dloss, cudaStream_t s);
 
 }  // namespace vocab
 }  // namespace zl

@@ -28,27 +28,24 @@ constexpr size_t kPieceBytes = 192u << 20;
 constexpr int kMinPiece = 1024;
 // k blocks (of 64) of one accumulation in TMEM: the tensor cores cut off what does not fit an fp32 sum, always towards zero, each
 // time they add 16 products. With bf16 logits summed over 4096 in one accumulation lse was off by 1.7e-6 and the row losses by 2.6e-6,
-// relative (an fp32 library product: 2.7e-7, 6.2e-7; in eight: 2e-7, 3e-7). Digits add up exactly over 1024. What leaves in bf16 is cut
-// off far below its rounding.
-constexpr int kSegLogits = 8, kSegDigits = 16, kSegF32 = 4, kSegDirect = 2, kSegAll = 1 << 20;
+// relative (an fp32 library product: 2.7e-7, 6.2e-7; in eight: 2e-7, 3e-7). fp32 logits: 2048 x 4096 x 32000 in accumulations of 256
+// 1.4e-7 and 2.0e-7 in 1.95 ms, of 128 0.9e-7 and 1.5e-7 in 2.12. What leaves in bf16 is cut off far below its rounding.
+constexpr int kSegLogits = 8, kSegF32 = 4, kSegDirect = 2, kSegAll = 1 << 20;
 // Up to so many rows the products with an fp32 W read it as it is and cut it into its terms themselves, once for every 128 rows:
 // beyond, the terms' way through memory (16 bytes a value of W instead of 4) costs less than cutting again.
 constexpr int kDirectRows = 1024;
-constexpr int kScalePad = 256;   // scales that a tile past the last row may read
 
 inline int up64(int n) { return (n + 63) / 64 * 64; }
 
-// An fp32 matrix [rows, d] as its bf16 terms [3][rows_p, d], rows past `rows` zeros: digits, with the rows' scales (1 for a row of
-// zeros and the kScalePad rows past rows_p), or leading bits.
+// An fp32 matrix [rows, d] as its bf16 terms [3][rows_p, d], rows past `rows` zeros.
 struct Cut {
   const float* src;
   bf16* dst;
-  float* scale;   // NULL: leading bits
   int rows, rows_p;
 };
-// |Omega| by block 0 (where omega is not NULL), up to three matrices into their terms by the others, a warp a row.
-__global__ void __launch_bounds__(kPrepThreads) vocab_prep_k(const Cut a, const Cut b, const Cut c, int d, const int32_t* __restrict__ labels,
-                                                             int N, int V, float* omega) {
+// |Omega| by block 0 (where omega is not NULL), up to two matrices into their terms by the others, a warp a row.
+__global__ void __launch_bounds__(kPrepThreads) vocab_prep_k(const Cut a, const Cut b, int d, const int32_t* __restrict__ labels, int N,
+                                                             int V, float* omega) {
   pdl_wait();
   pdl_trigger();
   int block = blockIdx.x;
@@ -73,64 +70,25 @@ __global__ void __launch_bounds__(kPrepThreads) vocab_prep_k(const Cut a, const 
   if (row >= a.rows_p) {
     row -= a.rows_p;
     m = b;
-    if (row >= b.rows_p) {
-      row -= b.rows_p;
-      m = c;
-    }
   }
   if (row >= m.rows_p) return;
   const float* const x = m.src + (size_t)row * d;
   const bool in = row < m.rows;
-  float scale = 1.f;
-  if (m.scale) {
-    uint32_t top = 0;   // bits of the largest magnitude (of a NaN or an infinity if one is there)
-    if (in)
-      for (int i = lane; i < d / 4; i += 32) {
-        const float4 f = reinterpret_cast<const float4*>(x)[i];
-        top = max(max(top, __float_as_uint(f.x) & 0x7FFFFFFFu), __float_as_uint(f.y) & 0x7FFFFFFFu);
-        top = max(max(top, __float_as_uint(f.z) & 0x7FFFFFFFu), __float_as_uint(f.w) & 0x7FFFFFFFu);
-      }
-    top = __reduce_max_sync(0xffffffffu, top);
-    // the next power of two above it, 2^127 at most (digits then reach twice their range)
-    if (top >= 0x7F800000u) scale = __uint_as_float(0x7FC00000u);
-    else if (top) scale = __uint_as_float(min((top >> 23) + 1u, 254u) << 23);
-    if (lane == 0) m.scale[row] = scale;
-    if (row == m.rows_p - 1)
-      for (int i = lane; i < kScalePad; i += 32) m.scale[m.rows_p + i] = 1.f;
-  }
-  const float inv = 1.f / scale;   // (2^-127 at the least: exact)
   for (int i = lane; i < d / 8; i += 32) {
     float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (in) Vec8<float>::load(x + 8 * i, f);
     bf16* out = m.dst + (size_t)row * d + 8 * i;
-    if (m.scale) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = f[k] * inv * 128.f;   // in units of the first digit
-      float unit = 0x1p-7f;
+    for (int t = 0; t < kTerms; ++t, out += (size_t)m.rows_p * d) {
+      float h[8];
 #pragma unroll
-      for (int t = 0; t < kTerms; ++t, out += (size_t)m.rows_p * d, unit *= 0x1p-8f) {
-        float h[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float r = rintf(f[k]);
-          h[k] = r * unit;
-          f[k] = (f[k] - r) * 256.f;
-        }
-        Vec8<bf16>::store(out, h);
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t u = __float_as_uint(f[k]);
+        const bool fin = (u & 0x7F800000u) != 0x7F800000u;
+        h[k] = fin ? __uint_as_float(u & 0xFFFF0000u) : f[k];   // a NaN or an infinity goes whole into the first term
+        f[k] = fin ? f[k] - h[k] : 0.f;
       }
-    } else {
-#pragma unroll
-      for (int t = 0; t < kTerms; ++t, out += (size_t)m.rows_p * d) {
-        float h[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t u = __float_as_uint(f[k]);
-          const bool fin = (u & 0x7F800000u) != 0x7F800000u;
-          h[k] = fin ? __uint_as_float(u & 0xFFFF0000u) : f[k];   // a NaN or an infinity goes whole into the first term
-          f[k] = fin ? f[k] - h[k] : 0.f;
-        }
-        Vec8<bf16>::store(out, h);
-      }
+      Vec8<bf16>::store(out, h);
     }
   }
 }
@@ -219,13 +177,13 @@ bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 struct FwdPlan {
   Tiles t;
   int terms, parts, direct;
-  size_t part, zl, counter, nt, wt, ns, vs, end;
+  size_t part, zl, counter, nt, wt, end;
 };
 FwdPlan fwd_plan(int dtype, int N, int d, int V) {
   FwdPlan p;
   p.terms = dtype == ZL_DTYPE_F32 ? kTerms : 1;
   p.direct = p.terms > 1 && N <= kDirectRows;
-  p.t = p.direct ? plan_direct(N, V, d, kSegDirect, 1) : plan(kLse, N, V, d, p.terms, 16, p.terms > 1 ? kSegDigits : kSegLogits, 1);
+  p.t = p.direct ? plan_direct(N, V, d, kSegDirect, 1) : plan(kLse, N, V, d, p.terms, 16, p.terms > 1 ? kSegF32 : kSegLogits, 1);
   p.parts = lse_parts(V, p.t);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up256(bytes); return o; };
@@ -233,10 +191,7 @@ FwdPlan fwd_plan(int dtype, int N, int d, int V) {
   p.zl = take((size_t)N * 4);
   p.part = take((size_t)p.parts * N * 8);
   p.nt = take(p.terms > 1 ? (size_t)kTerms * N * d * 2 : 0);
-  const bool digits = p.terms > 1 && !p.direct;
-  p.wt = take(digits ? (size_t)kTerms * V * d * 2 : 0);
-  p.ns = take(digits ? ((size_t)N + kScalePad) * 4 : 0);
-  p.vs = take(digits ? ((size_t)V + kScalePad) * 4 : 0);
+  p.wt = take(p.terms > 1 && !p.direct ? (size_t)kTerms * V * d * 2 : 0);
   p.end = at;
   return p;
 }
@@ -245,7 +200,7 @@ FwdPlan fwd_plan(int dtype, int N, int d, int V) {
 struct BwdPlan {
   Tiles z, dn, dw;
   int terms, piece, rows_p, v_p, direct;
-  size_t omega, dz, acc, nt, n3, wt, ns, vs, end;
+  size_t omega, dz, acc, nt, wt, end;
 };
 BwdPlan bwd_plan(int dtype, int N, int d, int V) {
   BwdPlan b;
@@ -261,7 +216,7 @@ BwdPlan bwd_plan(int dtype, int N, int d, int V) {
   for (int k = least; k < least + 4; ++k) {   // as few pieces as may be, or a few more where their waves are fuller
     const int piece = up64((V + k - 1) / k), n = (V + piece - 1) / piece;
     if (k > least && piece < kMinPiece) break;
-    const Tiles z = b.direct ? plan_direct(N, piece, d, kSegDirect, 1) : plan(kGradZ, N, piece, d, b.terms, 64, b.terms > 1 ? kSegDigits : kSegAll, 1),
+    const Tiles z = b.direct ? plan_direct(N, piece, d, kSegDirect, 1) : plan(kGradZ, N, piece, d, b.terms, 64, seg, 1),
                 dn = b.direct ? plan_direct(N, d, piece, kSegDirect, 32, n) : plan(kOut32, N, d, piece, b.terms, 32, seg, 32, n),
                 dw = plan(b.terms > 1 ? kOut32 : kOut16, piece, d, N, b.terms, b.terms > 1 ? 32 : 64, seg, 1);
     const double us = n * (z.us + dn.us + dw.us);
@@ -279,20 +234,16 @@ BwdPlan bwd_plan(int dtype, int N, int d, int V) {
   b.dz = take(row * b.piece);
   b.acc = take(b.terms > 1 && b.dn.splits == 1 ? 0 : (size_t)b.dn.splits * N * d * 4);
   b.nt = take(b.terms > 1 ? (size_t)kTerms * b.rows_p * d * 2 : 0);
-  const bool digits = b.terms > 1 && !b.direct;
-  b.n3 = take(digits ? (size_t)kTerms * b.rows_p * d * 2 : 0);
-  b.ns = take(digits ? ((size_t)b.rows_p + kScalePad) * 4 : 0);
-  b.vs = take(digits ? ((size_t)b.v_p + kScalePad) * 4 : 0);
-  b.wt = take(digits ? (size_t)kTerms * b.v_p * d * 2 : 0);
+  b.wt = take(b.terms > 1 && !b.direct ? (size_t)kTerms * b.v_p * d * 2 : 0);
   b.end = at;
   return b;
 }
 
-void launch_prep(const Cut& a, const Cut& b, const Cut& c, int d, const int32_t* labels, int N, int V, float* omega, cudaStream_t s) {
+void launch_prep(const Cut& a, const Cut& b, int d, const int32_t* labels, int N, int V, float* omega, cudaStream_t s) {
   note_launch(1);
   constexpr int rows = kPrepThreads / 32;
-  const size_t blocks = ((size_t)a.rows_p + b.rows_p + c.rows_p + rows - 1) / rows + (omega ? 1 : 0);
-  launch_pdl(vocab_prep_k, (unsigned)blocks, kPrepThreads, 0, s, a, b, c, d, labels, N, V, omega);
+  const size_t blocks = ((size_t)a.rows_p + b.rows_p + rows - 1) / rows + (omega ? 1 : 0);
+  launch_pdl(vocab_prep_k, (unsigned)blocks, kPrepThreads, 0, s, a, b, d, labels, N, V, omega);
 }
 
 }  // namespace
@@ -332,18 +283,15 @@ zl_status zl_op_vocab_loss(int dtype, const void* n, const void* W, const int32_
     if (!ws || ((uintptr_t)ws & 255u) || ws_bytes < p.end) return fail(ZL_ERR_ARG, kWsMsg);
     uint8_t* const w = (uint8_t*)ws;
     const void *A = n, *B = W;
-    const float *ns = nullptr, *vs = nullptr;
     if (p.terms > 1) {
-      const Cut cn{(const float*)n, (bf16*)(w + p.nt), p.direct ? nullptr : (float*)(w + p.ns), N, N};
+      const Cut cn{(const float*)n, (bf16*)(w + p.nt), N, N};
       Cut cw{};
-      if (!p.direct) cw = Cut{(const float*)W, (bf16*)(w + p.wt), (float*)(w + p.vs), V, V};
-      launch_prep(cn, cw, Cut{}, d, labels, N, V, nullptr, s);
+      if (!p.direct) cw = Cut{(const float*)W, (bf16*)(w + p.wt), V, V};
+      launch_prep(cn, cw, d, labels, N, V, nullptr, s);
       A = w + p.nt;
       if (!p.direct) B = w + p.wt;
-      ns = cn.scale;
-      vs = cw.scale;
     }
-    const Operands o{A, B, 0, 0, p.terms * N, (p.direct ? 1 : p.terms) * V, d, d, N, V, p.terms, 0, p.direct, ns, vs};
+    const Operands o{A, B, 0, 0, p.terms * N, (p.direct ? 1 : p.terms) * V, d, d, N, V, p.terms, 0, p.direct};
     bool ok = gemm_lse(N, V, d, o, p.t, labels, (float2*)(w + p.part), (float*)(w + p.zl), (unsigned*)(w + p.counter), s);
     if (ok) {
       note_launch(1);
@@ -383,27 +331,22 @@ zl_status zl_op_vocab_loss_bwd(int dtype, const void* n, const void* W, const in
     uint8_t* const w = (uint8_t*)ws;
     const bool f32 = p.terms > 1;
     float* const omega = (float*)(w + p.omega);
-    const void *A = n, *A3 = n, *B = W;   // A3: n in its product with dz
+    const void *A = n, *B = W;
     int n_rows = N, w_rows = V, n_term = 0, w_term = 0;   // of the operands in memory
-    const float *ns = nullptr, *vs = nullptr;
-    Cut cn{}, cw{}, c3{};
+    Cut cn{}, cw{};
     if (f32) {
-      cn = Cut{(const float*)n, (bf16*)(w + p.nt), p.direct ? nullptr : (float*)(w + p.ns), N, p.rows_p};
-      A = A3 = w + p.nt;
+      cn = Cut{(const float*)n, (bf16*)(w + p.nt), N, p.rows_p};
+      A = w + p.nt;
       n_rows = kTerms * p.rows_p;
       n_term = p.rows_p;
       if (!p.direct) {
-        cw = Cut{(const float*)W, (bf16*)(w + p.wt), (float*)(w + p.vs), V, p.v_p};
-        if (dW) c3 = Cut{(const float*)n, (bf16*)(w + p.n3), nullptr, N, p.rows_p};
-        A3 = w + p.n3;
+        cw = Cut{(const float*)W, (bf16*)(w + p.wt), V, p.v_p};
         B = w + p.wt;
-        ns = cn.scale;
-        vs = cw.scale;
         w_rows = kTerms * p.v_p;
         w_term = p.v_p;
       }
     }
-    launch_prep(cn, cw, c3, d, labels, N, V, omega, s);
+    launch_prep(cn, cw, d, labels, N, V, omega, s);
     void* const dz = w + p.dz;
     const int z_rows = p.terms * p.rows_p;
     const bool direct = f32 && p.dn.splits == 1;   // dn is where its sums are formed
@@ -411,14 +354,13 @@ zl_status zl_op_vocab_loss_bwd(int dtype, const void* n, const void* W, const in
     bool ok = true;
     for (int first = 0; ok && first < V; first += p.piece) {
       const int m = std::min(p.piece, V - first), m64 = up64(m);
-      ok = gemm_grad_z(N, m64, d, Operands{A, B, 0, 0, n_rows, w_rows, d, d, n_term, w_term, p.terms, first, p.direct, ns, vs}, p.z, labels, lse, first,
-                       V, dz, p.rows_p, p.piece, s);
+      ok = gemm_grad_z(N, m64, d, Operands{A, B, 0, 0, n_rows, w_rows, d, d, n_term, w_term, p.terms, first, p.direct}, p.z, labels, lse, first, V, dz, p.rows_p, p.piece, s);
       if (ok && dn)
-        ok = gemm_out(N, d, m64, Operands{dz, B, 0, 1, z_rows, w_rows, p.piece, d, p.rows_p, w_term, p.terms, first, p.direct, nullptr, nullptr}, p.dn, 1,
-                      acc, first > 0, nullptr, direct ? omega : nullptr, dloss, s);
+        ok = gemm_out(N, d, m64, Operands{dz, B, 0, 1, z_rows, w_rows, p.piece, d, p.rows_p, w_term, p.terms, first, p.direct}, p.dn, 1,
+                      acc, first > 0, direct ? omega : nullptr, dloss, s);
       if (ok && dW)
-        ok = gemm_out(m, d, N, Operands{dz, A3, 1, 1, z_rows, n_rows, p.piece, d, p.rows_p, n_term, p.terms, 0, 0, nullptr, nullptr}, p.dw,
-                      f32, (uint8_t*)dW + (size_t)first * d * es, 0, vs ? vs + first : nullptr, omega, dloss, s);
+        ok = gemm_out(m, d, N, Operands{dz, A, 1, 1, z_rows, n_rows, p.piece, d, p.rows_p, n_term, p.terms, 0, 0}, p.dw, f32,
+                      (uint8_t*)dW + (size_t)first * d * es, 0, omega, dloss, s);
     }
     if (ok && dn && !direct) {
       note_launch(1);
