@@ -29,7 +29,10 @@ constexpr int kMinPiece = 1024;
 // k blocks (of 64) of one accumulation in TMEM: the tensor cores cut off what does not fit an fp32 sum, always towards zero, each
 // time they add 16 products. With bf16 logits summed over 4096 in one accumulation lse was off by 1.7e-6 and the row losses by 2.6e-6,
 // relative (an fp32 library product: 2.7e-7, 6.2e-7; in eight: 2e-7, 3e-7). fp32 logits: 2048 x 4096 x 32000 in accumulations of 256
-// 1.4e-7 and 2.0e-7 in 1.95 ms, of 128 0.9e-7 and 1.5e-7 in 2.12. What leaves in bf16 is cut off far below its rounding.
+// 1.4e-7 and 2.0e-7 in 1.95 ms, of 128 0.9e-7 and 1.5e-7 in 2.12. The backward's
+// logits too: where the label's p is near 1, dz is the difference p - 1, and of a logit of 100 (products of one sign) one
+// accumulation lost 1.2e-3, six times 1 - p = 2e-4; the pieces' products take 4% longer for it.
+// Sums that leave in bf16 are cut off far below its rounding.
 constexpr int kSegLogits = 8, kSegF32 = 4, kSegDirect = 2, kSegAll = 1 << 20;
 // Up to so many rows the products with an fp32 W read it as it is and cut it into its terms themselves, once for every 128 rows:
 // beyond, the terms' way through memory (16 bytes a value of W instead of 4) costs less than cutting again.
@@ -216,7 +219,7 @@ BwdPlan bwd_plan(int dtype, int N, int d, int V) {
   for (int k = least; k < least + 4; ++k) {   // as few pieces as may be, or a few more where their waves are fuller
     const int piece = up64((V + k - 1) / k), n = (V + piece - 1) / piece;
     if (k > least && piece < kMinPiece) break;
-    const Tiles z = b.direct ? plan_direct(N, piece, d, kSegDirect, 1) : plan(kGradZ, N, piece, d, b.terms, 64, seg, 1),
+    const Tiles z = b.direct ? plan_direct(N, piece, d, kSegDirect, 1) : plan(kGradZ, N, piece, d, b.terms, 64, b.terms > 1 ? seg : kSegLogits, 1),
                 dn = b.direct ? plan_direct(N, d, piece, kSegDirect, 32, n) : plan(kOut32, N, d, piece, b.terms, 32, seg, 32, n),
                 dw = plan(b.terms > 1 ? kOut32 : kOut16, piece, d, N, b.terms, b.terms > 1 ? 32 : 64, seg, 1);
     const double us = n * (z.us + dn.us + dw.us);
