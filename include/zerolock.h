@@ -439,7 +439,8 @@ zl_status zl_op_vocab_loss_bwd(int dtype, const void* n, const void* W, const in
 
 /* The record of a teacher: of every row of z [N, ld] (dtype, columns >= V ignored) the k largest logits, in falling order, equal
  * ones (0 and -0 are) by rising column, NaN above +inf: idx [N, k] int32 and val [N, k] fp32 (z's values), and rest [N] fp32 =
- * log sum_{other columns} exp(z / T) (-inf if there are none, NaN if a NaN or +inf is among them). 1 <= k <= min(V, ZL_TOP_MAX); T > 0. Rows may start anywhere
+ * log sum_{other columns} exp(z / T) (-inf if there are none, NaN if a NaN or +inf is among them). 1 <= k <= min(V, ZL_TOP_MAX); T > 0 and
+ * log2(e) / T finite (4.3e-39 and up; z / T of a low T should be too). Rows may start anywhere
  * (ld >= V, z on its elements); rows on 16 bytes are read faster. */
 zl_status zl_op_top_logits(int dtype, const void* z, int N, int V, int ld, int k, float T, int32_t* idx, float* val,
                            float* rest, void* stream);
@@ -453,7 +454,7 @@ zl_status zl_op_top_logits(int dtype, const void* z, int N, int V, int ld, int k
  * record may hold fewer than k. A record without any mass (every val and rest -inf) adds no divergence;
  * a NaN or +inf in a val that counts, or in rest, makes that row's loss and gradient NaN (a teacher's NaN comes that way).
  * A teacher's mass of 0 where p has some makes kl_dir 0 infinite (and 1 the reverse), as its formula says. alpha 1 reads no
- * record and ignores T (idx, val, rest may be NULL). Writes dz = dloss/dz [N, ld] (dtype, may be z; columns V .. ld - 1 become 0). */
+ * record and does not use T, which is checked like k (idx, val, rest may be NULL). Writes dz = dloss/dz [N, ld] (dtype, may be z; columns V .. ld - 1 become 0). */
 zl_status zl_op_top_loss(int dtype, const void* z, const int32_t* idx, const float* val, const float* rest,
                          const int32_t* labels, int N, int V, int ld, int k, float alpha, float T, int kl_dir, void* dz,
                          float* row_loss, float* loss, void* stream);

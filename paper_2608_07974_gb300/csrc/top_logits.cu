@@ -481,9 +481,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_logits_k(const T* __res
   const float bound = floor_of_half<T>(sh.lo);
   const uint32_t pair = __float_as_uint(bound) >> 16 | (__float_as_uint(bound) & 0xFFFF0000u);
   // note the words with values not below the bound (a NaN is not), sum all that is: relative to the bound, which none exceeds
-  const float base = bound * a.scale;
-  const bool fixed = fabsf(base) < vocab::kFar;
-  const uint64_t s2 = f2(a.scale, a.scale), nb = fixed ? f2(-base, -base) : 0ull;
+  const bool fixed = fabsf(bound) < INFINITY;
+  const float ref = fixed ? bound : 0.f;
+  const uint64_t s2 = f2(a.scale, a.scale), nr = f2(-ref, -ref);
   uint64_t sum2 = 0ull;
   sl.pass([&](const uint4& u, int i, int) {
     float x[W];
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_logits_k(const T* __res
     uint64_t t = 0ull;
 #pragma unroll
     for (int e = 0; e < W; e += 2) {
-      const float2 v = uf2(fma2(f2(x[e], x[e + 1]), s2, nb));
+      const float2 v = uf2(mul2(add2(f2(x[e], x[e + 1]), nr), s2));
       const uint64_t p = f2(ex2(v.x), ex2(v.y));
       t = e == 0 ? p : add2(t, p);
     }
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_logits_k(const T* __res
   const float2 lanes = uf2(sum2);
   float sum = lanes.x + lanes.y;
   const bool single_in = tid < ns && !(single < bound);
-  if (tid < ns && single < bound) sum += ex2(fmaf(single, a.scale, fixed ? -base : 0.f));
+  if (tid < ns && single < bound) sum += ex2((single - ref) * a.scale);
   // (a bound that is not finite is no reference; and where every thread's sum is tiny, its terms lie so far below the bound that
   // they lost digits)
   const bool good = __syncthreads_or(fixed && sum >= 0x1p-60f);
@@ -664,11 +664,12 @@ struct LossArgs {
 
 // What a row's log-sum-exps and the teacher's come to, formed by one warp.
 struct RowTerms {
-  float lse, lse1, lseq;           // of z / T, z and the teacher
   float lpr, lqr, omega;           // the rest's log probabilities; |Omega|
-  // Sums s e^{m / T} as m and 1 / s: of the others, all, all at T = 1 (TWO), the teacher's. Probabilities go by x - m, which is exact
-  // or nearly so, and not by x - log sum, whose rounding (2^-24 of 20 or 40) would be in all of a row's.
-  float om, oi, pr, am, ai, cm, ci, qm, qi;   // pr: the others' probability
+  // Sums s e^{m / T} as m, 1 / s and log s: of the others, all, all at T = 1 (those at T but for TWO), the teacher's. Probabilities and
+  // their logarithms go by x - m, which is exact or nearly so, and not by x - log sum, whose rounding (2^-24 of 20 or 40, and of as many
+  // over T) would be in all of a row's.
+  float om, oi, pr, am, ai, al, cm, ci, cl, qm, qi, ql;   // pr: the others' probability
+  int held;                        // the record holds something
   float bad;                       // NaN where the row or its record has no softmax (a NaN, +inf; a row of nothing but -inf), else 0
 };
 struct LossShared {
@@ -683,6 +684,7 @@ struct LossShared {
 
 // Bytes of a slice's bitmap.
 int mark_bytes(int V, int W, int split) { return (((V / W + split) / split * W + 31) / 32 + 1) * 4; }
+constexpr float kMasked = 1e38f;   // logits below -kMasked are masks
 constexpr int kEntries = (ZL_TOP_MAX + kThreads - 1) / kThreads;   // of a record, a thread
 
 // TWO: the task term's softmax is another one than the divergence's (T != 1, both terms).
@@ -774,15 +776,6 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
     if (TWO) vocab::run_add(Cr, x, mx, kL2e);
   });
   Lse P = vocab::run_sum(Pr), C = vocab::run_sum(Cr);
-  if (__syncthreads_and(P.m == -INFINITY)) {   // nothing, or masks of the lowest value: as such they count
-    const T* const p = reinterpret_cast<const T*>(sl.src);
-#pragma unroll 1
-    for (int i = tid; i < sl.n * W; i += kThreads) {
-      if (bits[i >> 5] >> (i & 31) & 1u) continue;
-      vocab::lse_add1(P, to_f(p[i]), s);
-      if (TWO) vocab::lse_add1(C, to_f(p[i]), kL2e);
-    }
-  }
   if (tid < ns && !marked(sp.single_at(tid))) {
     vocab::lse_add1(P, single, s);
     if (TWO) vocab::lse_add1(C, single, kL2e);
@@ -857,30 +850,33 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
       RowTerms t;
       t.omega = a.count_here ? (float)n : a.loss[1];
       const Lse A = vocab::lse_merge(P, R, s);
-      t.lse = vocab::lse_value(A, inv_T);
-      t.lse1 = TWO ? vocab::lse_value(C, 1.f) : t.lse;
-      t.lseq = vocab::lse_value(Q, 1.f);
-      t.lpr = vocab::lse_value(P, inv_T) - t.lse;
-      t.lqr = rest - t.lseq;
+      t.al = log2f(A.s) * kLn2;
+      t.ql = log2f(Q.s) * kLn2;
+      t.lpr = (P.m - A.m) * inv_T + (log2f(P.s) * kLn2 - t.al);
+      t.lqr = (rest - Q.m) - t.ql;
+      t.held = !(Q.m == -INFINITY && Q.s == 0.f);
       t.bad = A.m == -INFINITY ? __uint_as_float(0x7FC00000u) : (A.s + Q.s) * 0.f;
-      const bool none = P.m <= -vocab::kFar;   // no others, or only masks: e_v 0
+      const bool none = P.m <= -kMasked;   // no others, or only masks: e_v 0
       t.om = none ? 0.f : P.m;
       t.oi = none ? 0.f : 1.f / P.s;
       t.pr = none ? 0.f : P.s * ex2((P.m - A.m) * s) / A.s;
       t.am = A.m;
       t.ai = 1.f / A.s;
-      t.cm = TWO ? C.m : 0.f;
-      t.ci = TWO ? 1.f / C.s : 0.f;
+      t.cm = TWO ? C.m : A.m;
+      t.ci = TWO ? 1.f / C.s : t.ai;
+      t.cl = TWO ? log2f(C.s) * kLn2 : t.al;
       t.qm = Q.m;
       t.qi = 1.f / Q.s;
       sh.t = t;
     }
   }
   __syncthreads();
-  const RowTerms t = sh.t;
-  const bool mass = kl_on && t.lseq != -INFINITY;   // the record holds something
+  const RowTerms& t = sh.t;
+  const bool mass = kl_on && t.held;
   auto p_of = [&](float x) { return ex2((x - t.am) * s) * t.ai; };
   auto q_of = [&](float x) { return ex2((x - t.qm) * kL2e) * t.qi; };
+  auto logp = [&](float x) { return (x - t.am) * inv_T - t.al; };
+  auto logq = [&](float x) { return (x - t.qm) - t.ql; };
   // the divergence
   auto xlog = [](float p, float d) { return p == 0.f ? 0.f : p * d; };   // (a p of NaN stays)
   float kl = 0.f;
@@ -889,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
 #pragma unroll
       for (int e = 0; e < kEntries; ++e) {
         if (col[e] < 0) continue;
-        const float lp = zt[e] * inv_T - t.lse, q = lq[e] - t.lseq;
+        const float lp = logp(zt[e]), q = logq(lq[e]);
         kl += a.dir == 1 ? xlog(q_of(lq[e]), q - lp) : xlog(p_of(zt[e]), lp - q);
       }
       if (has_rest && tid == 0) kl += a.dir == 1 ? xlog(q_of(rest), t.lqr - t.lpr) : xlog(t.pr, t.lpr - t.lqr);
@@ -909,7 +905,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
   if (has_rest) other = a.dir == 1 ? t.pr - q_of(rest) : xlog(t.pr, t.lpr - t.lqr - kl);
   const float ck = (wk == 0.f ? 0.f : wk * other) * t.oi, cs = fmaf(wa, t.pr * t.oi, ck), c1 = wa * t.ci;
   if (rank == 0 && tid == 0)
-    a.row_loss[row] = (a.alpha > 0.f ? a.alpha * (t.lse1 - zy) : 0.f) + (kl_on ? (1.f - a.alpha) * a.T * a.T * kl : 0.f) + t.bad;
+    a.row_loss[row] = (a.alpha > 0.f ? a.alpha * ((t.cm - zy) + t.cl) : 0.f) + (kl_on ? (1.f - a.alpha) * a.T * (a.T * kl) : 0.f) + t.bad;
   const uint64_t s2 = f2(s, s), cs2 = f2(TWO ? ck : cs, TWO ? ck : cs), c12 = f2(c1, c1), L2 = f2(kL2e, kL2e);
   const uint64_t om2 = f2(-t.om, -t.om), cm2 = f2(-t.cm, -t.cm);
   auto grad = [&](float x) {
@@ -949,7 +945,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) {
       if (col[e] < 0 || !here(col[e])) continue;
-      const float lp = zt[e] * inv_T - t.lse, q = lq[e] - t.lseq, p = p_of(zt[e]);
+      const float lp = logp(zt[e]), q = logq(lq[e]), p = p_of(zt[e]);
       float g = 0.f;
       if (mass) g = a.dir == 1 ? p - q_of(lq[e]) : xlog(p, lp - q - kl);
       const float v = (wa != 0.f ? wa * ((TWO ? ex2((zt[e] - t.cm) * kL2e) * t.ci : p) - (col[e] == y ? 1.f : 0.f)) : 0.f) + wk * g;
@@ -1015,11 +1011,11 @@ bool allow(K* kern, PerDevice<bool>& devices) {
 
 bool shape_ok(int dtype, int N, int V, int ld, int k, float T) {
   return (dtype == ZL_DTYPE_F32 || dtype == ZL_DTYPE_BF16) && N >= 0 && N <= ZL_VOCAB_MAX_ROWS && V >= 2 && V <= ZL_VOCAB_MAX &&
-         ld >= V && k >= 1 && k <= V && k <= ZL_TOP_MAX && T > 0.f && std::isfinite(T) && std::isfinite(1.f / T);
+         ld >= V && k >= 1 && k <= V && k <= ZL_TOP_MAX && T > 0.f && std::isfinite(T) && std::isfinite(kL2e / T);
 }
 const char* const kShapeMsg =
     "bad dtype or size (0 <= N <= 2^24, 2 <= V <= 2^20, ld >= V, 1 <= k <= min(V, 1024)), or a temperature that is not positive "
-    "and finite";
+    "and finite, or so low that log2(e) / T is not";
 const char* const kPtrMsg = "NULL pointer, or a tensor off the alignment of its elements";
 
 template <typename T>

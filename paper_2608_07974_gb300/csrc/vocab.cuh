@@ -14,8 +14,9 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// sum e^{x / T} = s e^{m / T}, with m the largest x so far (-inf, 0: the empty sum); scale = log2 e / T is folded into the
-// exponent's FMA. m stays in the units of x: a mask of the type's lowest value times the scale would overflow.
+// sum e^{x / T} = s e^{m / T}, with m the largest x so far (-inf, 0: the empty sum); scale = log2 e / T. Exponents are (x - m) scale, the
+// difference first: it is exact or nearly so, while x scale - m scale carries the rounding of numbers of the size of x / T, which at a
+// low temperature is larger than the exponent (T = 1e-6, logits of 20: a probability of 4 instead of 1). m stays in the units of x.
 struct Lse {
   float m, s;
 };
@@ -26,60 +27,64 @@ __device__ __forceinline__ void lse_raise(Lse& A, float m, float scale) {
     A.m = m;
   }
 }
-constexpr float kFar = 1e38f;   // exponents beyond it: nothing finite yet, or only masks
-__device__ __forceinline__ float lse_far(const Lse& A, float x, float scale) {
-  return A.m == -INFINITY && !(x != x) ? 0.f : ex2((x - A.m) * scale);
-}
+// What is taken off an exponent's x: m, or 0 where nothing but -inf has come.
+__device__ __forceinline__ float lse_ref(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ void lse_add1(Lse& A, float x, float scale) {
   lse_raise(A, x, scale);
-  const float b = A.m * scale;
-  A.s += fabsf(b) < kFar ? ex2(fmaf(x, scale, -b)) : lse_far(A, x, scale);
+  A.s += ex2((x - lse_ref(A.m)) * scale);
 }
-// N values whose largest is mx (NaN if one is).
+// N values whose largest is mx (NaN if one is). With m scale below kNear one FMA instead: its rounding is that of the log-sum-exp itself
+// (under the products' epilogue 3% of their time).
+constexpr float kNear = 4096.f;
 template <int N>
 __device__ __forceinline__ void lse_add(Lse& A, const float (&x)[N], float mx, float scale) {
   lse_raise(A, mx, scale);
-  const float b = A.m * scale;
-  if (!(fabsf(b) < kFar)) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) A.s += lse_far(A, x[i], scale);
-    return;
-  }
-  const uint64_t s2 = f2(scale, scale), nb = f2(-b, -b);
+  const float m = lse_ref(A.m), b = m * scale;
+  const uint64_t s2 = f2(scale, scale);
   uint64_t t = 0ull;
+  if (fabsf(b) < kNear) {
+    const uint64_t nb = f2(-b, -b);
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    const float2 v = uf2(fma2(f2(x[2 * i], x[2 * i + 1]), s2, nb));
-    const uint64_t e = f2(ex2(v.x), ex2(v.y));
-    t = i == 0 ? e : add2(t, e);
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 v = uf2(fma2(f2(x[2 * i], x[2 * i + 1]), s2, nb));
+      const uint64_t e = f2(ex2(v.x), ex2(v.y));
+      t = i == 0 ? e : add2(t, e);
+    }
+  } else {
+    const uint64_t nm = f2(-m, -m);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 v = uf2(mul2(add2(f2(x[2 * i], x[2 * i + 1]), nm), s2));
+      const uint64_t e = f2(ex2(v.x), ex2(v.y));
+      t = i == 0 ? e : add2(t, e);
+    }
   }
   const float2 v = uf2(t);
   A.s += v.x + v.y;
 }
 // The same for many values a thread, in as few instructions as may be (a loop whose rare paths are long waits for its
-// instructions): the sum's reference m is raised only when a value would lie more than 2^kSlack above it. Masks, whose exponents
-// overflow, are left out: a sum that stays empty may hold nothing else, and is formed again with lse_add1 where that matters.
+// instructions): the sum's reference m is raised only when a value would lie more than 2^kSlack above it.
 struct LseRun {
-  float m, limit, nb;   // reference, the value up to which it holds, -m scale (0 while m is -inf)
+  float m, limit, nm;   // reference, the value up to which it holds, -m (0 while m is -inf)
   uint64_t s;           // two lanes
   float slack;
 };
 constexpr float kSlack = 24.f;
-__device__ __forceinline__ LseRun run_empty(float scale) { return LseRun{-INFINITY, -kFar / scale, 0.f, 0ull, kSlack / scale}; }
+__device__ __forceinline__ LseRun run_empty(float scale) { return LseRun{-INFINITY, -INFINITY, 0.f, 0ull, kSlack / scale}; }
 template <int N>
 __device__ __forceinline__ void run_add(LseRun& A, const float (&x)[N], float mx, float scale) {
   if (!(mx <= A.limit)) {   // (a NaN stays in the sum)
     const float c = A.m == -INFINITY ? 0.f : ex2((A.m - mx) * scale);
     A.s = mul2(A.s, f2(c, c));
     A.m = mx;
-    A.nb = -mx * scale;
+    A.nm = -mx;
     A.limit = mx + A.slack;
   }
-  const uint64_t s2 = f2(scale, scale), nb = f2(A.nb, A.nb);
+  const uint64_t s2 = f2(scale, scale), nm = f2(A.nm, A.nm);
   uint64_t t = 0ull;
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {
-    const float2 v = uf2(fma2(f2(x[2 * i], x[2 * i + 1]), s2, nb));
+    const float2 v = uf2(mul2(add2(f2(x[2 * i], x[2 * i + 1]), nm), s2));
     const uint64_t e = f2(ex2(v.x), ex2(v.y));
     t = i == 0 ? e : add2(t, e);
   }

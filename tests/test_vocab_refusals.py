@@ -91,3 +91,11 @@ def test_binding_refuses_types_and_addresses_of_workspaces(B):
         B.zl_op_vocab_loss(B.ZL_DTYPE_BF16, P, P, torch.zeros(4, dtype=torch.int64), 4, 64, 100, P, P, P, None)
     with pytest.raises(TypeError):
         B.zl_op_vocab_loss_bwd(B.ZL_DTYPE_BF16, P, P, P, 4, 64, 100, P, None, P, P, P)
+
+
+@host_only
+@pytest.mark.parametrize("T", [3e-39, 4.1e-39])
+def test_temperatures_whose_scale_overflows_are_refused(B, T):
+    """1 / T is finite there, log2(e) / T, by which exponents are scaled, is not."""
+    assert B._lib.zl_op_top_logits(*{**TOP, "T": T}.values()) == B.ZL_ERR_ARG
+    assert B._lib.zl_op_top_loss(*{**LOSS, "T": T}.values()) == B.ZL_ERR_ARG
