@@ -410,7 +410,7 @@ zl_status zl_op_block_norm_bwd(const zl_block_norm* p, const void* h_out, const 
  * Nothing is allocated and every call may be captured into a graph; a workspace belongs to one call at a time (and to one
  * graph that may run at that time). Outputs must not overlap inputs except where said. Errors: ZL_ERR_ARG (a size, a
  * temperature, NULL, an alignment, a workspace that is too small), ZL_ERR_CUDA (a launch failed).
- * A logit of -inf, or of the type's lowest value beside others, is a column with probability 0. A NaN or +inf, or nothing but
+ * A logit of -inf, or of the type's lowest value beside others, is a column with probability 0 (nothing but the lowest: equal logits). A NaN or +inf, or nothing but
  * -inf in a row of Omega, makes that row's loss and gradient NaN.
  * ------------------------------------------------------------------------------------- */
 #define ZL_VOCAB_MAX_ROWS (1 << 24)

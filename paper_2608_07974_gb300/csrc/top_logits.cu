@@ -856,7 +856,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_loss_k(const T* z0, T* 
       t.lqr = (rest - Q.m) - t.ql;
       t.held = !(Q.m == -INFINITY && Q.s == 0.f);
       t.bad = A.m == -INFINITY ? __uint_as_float(0x7FC00000u) : (A.s + Q.s) * 0.f;
-      const bool none = P.m <= -kMasked;   // no others, or only masks: e_v 0
+      // no others, or only masks beside the record's logits: e_v 0 (a row of nothing but masks has their softmax)
+      const bool none = P.m == -INFINITY || (P.m <= -kMasked && A.m > -kMasked);
       t.om = none ? 0.f : P.m;
       t.oi = none ? 0.f : 1.f / P.s;
       t.pr = none ? 0.f : P.s * ex2((P.m - A.m) * s) / A.s;

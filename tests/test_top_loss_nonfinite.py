@@ -145,3 +145,24 @@ def test_a_teacher_that_diverged(B, kl_dir, bad):
     want = loss_of(B, "bf16", z, record(B, "bf16", t, 1000, 12, 1.0), y, 1000, 0.5, 1.0, kl_dir)
     t[1, 400] = bad
     check_row_is_nan(loss_of(B, "bf16", z, record(B, "bf16", t, 1000, 12, 1.0), y, 1000, 0.5, 1.0, kl_dir), want, 1, 1000)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,ld,off,k", SHAPES)
+@pytest.mark.parametrize("alpha", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("kl_dir,with_rest", [(0, 1), (1, 1), (1, 0)])
+@pytest.mark.parametrize("T", [1.0, 2.0, 0.5])
+def test_a_row_of_nothing_but_the_lowest_value(B, dtype, N, V, ld, off, k, alpha, kl_dir, with_rest, T):
+    """A softmax does not change when a number is added to all logits: such a row has that of a row of zeros, to the rounding of its
+    loss, log V and a divergence (2^-20 of up to 40), and of its gradient."""
+    z, t, y = case(dtype, N, V, ld, off, 15)
+    idx, val, rest = record(B, dtype, t, V, k, T)
+    rec = (idx, val, rest if with_rest else None)
+    z[1, :V] = 0.0
+    dz0, rl0, loss0 = loss_of(B, dtype, z, rec, y, V, alpha, T, kl_dir)
+    z[1, :V] = torch.finfo(TYPES[dtype]).min
+    dz, rl, loss = loss_of(B, dtype, z, rec, y, V, alpha, T, kl_dir)
+    tol = 2.0 ** -20 * 40 * max(1.0, T * T)
+    assert float((rl - rl0).abs().max()) <= tol and float((loss - loss0).abs().max()) <= tol
+    tol = (2.0 ** -18 + torch.finfo(TYPES[dtype]).eps) * dz0.float().abs() + (1 - alpha) * T * 2.0 ** -20 * 40 / V
+    assert bool(((dz.float() - dz0.float()).abs() <= tol).all())
