@@ -15,7 +15,6 @@
 #include "common.cuh"
 #include "ops.h"
 #include "per_device.h"
-#include "tc_host.h"
 #include "tcgen05.cuh"
 
 namespace zl {

@@ -1,4 +1,5 @@
-// What the launchers of the tensor-core products share (host side; gemm_tc.cu).
+// What the launchers of the tensor-core products share (host side; defined in gemm_tc.cu, which does not include this file: the measured
+// DRAM traffic of the engine's products is tied to its text, and the linker checks the functions' and variables' names).
 #pragma once
 #include <cuda.h>
 #include <cudaTypedefs.h>

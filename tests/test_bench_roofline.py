@@ -54,3 +54,9 @@ def test_fused_update_class_is_bound_by_its_bytes():
     e = bench.roofline_of(prof)
     assert e["bound"] == "hbm" and e["unit"] == "GB/s"
     assert e["achieved"] == pytest.approx(3e-3 * pk["hbm_gbs"] / 4e-3)
+
+
+@pytest.mark.parametrize("workload,cls", [(w, c) for w, t in bench.TRAFFIC.items() for c in t])
+def test_traffic_figures_belong_to_the_sources_that_are_here(workload, cls):
+    """A change to the kernels' sources needs the figures measured again, or the bench line loses them without a sign."""
+    assert bench.measured_traffic(cls, workload) == bench.TRAFFIC[workload][cls]["bytes_per_launch"]
