@@ -130,8 +130,9 @@ __device__ __forceinline__ uint4 pack_word(const float (&x)[4]) {
 }
 
 // By one block of up to 1024 threads, in a fixed order, sums in fp64: loss[1] = |Omega| = #(0 <= labels < V) (part 1), loss[0] =
-// sum(row_loss) / |Omega| (part 2, 0 without rows in Omega; by the |Omega| that is in loss[1], or with part 3 both).
-__device__ __forceinline__ void finish_loss(const float* __restrict__ row_loss, const int32_t* __restrict__ labels, int N, int V,
+// sum(row_loss) / |Omega| (part 2, 0 without rows in Omega; by the |Omega| that is in loss[1], or with part 3 both). row_loss may have been
+// written by other blocks of the same launch: no __restrict__, which would allow loads that need not see them.
+__device__ __forceinline__ void finish_loss(const float* row_loss, const int32_t* __restrict__ labels, int N, int V,
                                             float* loss, int part) {
   __shared__ double sum[32];
   __shared__ int num[32];
