@@ -335,3 +335,14 @@ def test_outputs_stay_in_bounds(B):
     torch.cuda.synchronize()
     for n, x in f.items():
         assert bool((x[:guard] == 55).all()) and bool((x[-guard:] == 55).all()), n
+
+
+@pytest.mark.parametrize("N", [256, 257, 511, 512, 513])
+def test_loss_set_counted_by_the_rows_or_by_a_launch(B, N):
+    """Up to 512 rows every row counts |Omega| itself, one label a thread up to 256 and two above; more are counted by a launch. Holes
+    lie on both sides of 256."""
+    V, k = 40, 4
+    z, (idx, val, r) = teacher_record(B, "f32", N, V, k, 1.0, 2)
+    y = labels_of(N, V)
+    y[N - 1], y[N - 2], y[255] = -1, 3, V
+    check_loss(B, "f32", rows(z, torch.float32), idx, val, r, y, V, 0.5, 1.0, 1)
