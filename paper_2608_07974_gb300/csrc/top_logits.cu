@@ -178,8 +178,8 @@ __device__ __forceinline__ bool word_below(const uint4& u, float bound, uint32_t
 // byte.
 // A row is shared by a cluster where it is long or rows are few: its CTAs exchange their bins, all find the same bound, and the
 // first one takes their candidates and sums.
-// 4096 x 50257 bf16, k 64: 106 us, 3.9 TB/s of the one reading (57% of the copy rate); the first pass alone takes 56, the search and what
-// follows the second pass are latency. 509 x 32000 fp32, k 256: 34 us.
+// 4096 x 50257 bf16, k 64: 106 us, 3.9 TB/s of the one reading (57% of the copy rate): the search and what follows the second pass are
+// latency (warps wait for loads and at barriers, 0.6 instructions a cycle). 509 x 32000 fp32, k 256: 28 us, as a call among others 34.
 // ------------------------------------------------------------------------------------------------
 struct TopArgs {
   int N, V, ld, k, split, bins, cap;   // CTAs a row, bins of one, room for candidates
@@ -596,8 +596,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_logits_k(const T* __res
       left[p - k] = x;   // (collected in any order, summed in this one)
     }
   };
-  // A candidate's place is the number of candidates before it: g lanes count for one. Many are sorted instead (355 of 64 bits: 6 us
-  // by counting, 3 sorted).
+  // A candidate's place is the number of candidates before it: g lanes count for one. Many are sorted instead, since counting grows with
+  // their square. 1216 x 32000 bf16, counted / sorted: 64 in the record (90 candidates) 28 / 32 us, 110 (150) 33.5 / 37.5, 160 (220) 40.5 / 42,
+  // 256 (355) 53 / 54: level beyond some 200.
   if (n <= 160) {
     int g = 1;
     while (g < 8 && n * g * 2 <= kThreads) g *= 2;
@@ -646,7 +647,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) top_logits_k(const T* __res
 // gradient of the others, after which the record's columns and the label's are written over. The CTAs that share a row exchange
 // their sums over the others, and each forms what goes by the record alone.
 // 0 log 0 = 0 throughout; a record without any mass adds nothing, one with a NaN or +inf makes the row NaN.
-// Bound by HBM (the row in, its gradient out): 4096 x 50257 bf16 157 us, 5.3 TB/s (78% of the copy rate).
+// Bound by HBM (the row in, its gradient out): 4096 x 50257 bf16 165 us, 5.0 TB/s (74% of the copy rate). Where dz and z lie differently against
+// 16 bytes the gradient leaves in single values, a word's neighbours in one thread: 520 us (fp32 327 against 287).
 // ------------------------------------------------------------------------------------------------
 // Up to so many rows every row counts |Omega| itself (2 KB of labels in L2 against a launch).
 constexpr int kCountHere = 2 * kThreads;

@@ -6,8 +6,10 @@
 // (the vocabulary rarely is a multiple of anything); an fp32 operand takes part as three bf16 terms, the products of the
 // terms being further k blocks (or, DIRECT, further products of a k block whose B is cut in the kernel); and epilogues gather a row's
 // share in registers first. Every wait is bounded; where one gives up, what is not formed is NaN.
-// Bound by the tensor cores, few rows by the reading of B. Measured: 2048 x 4096 x 32000 bf16 284 us (the burst peak's 284), 4096 x 768
-// x 50257 196 us reduced to log-sum-exps (85%), 58 us a piece of 12608 columns as dz (73%: the stores), 8 x 768 x 50257 18 us (4.3 TB/s).
+// Bound by the tensor cores, few rows by the reading of B. Measured: 2048 x 4096 x 32000 bf16 287 to 296 us (the burst peak's 284), 4096 x
+// 768 x 50257 198 us reduced to log-sum-exps (84%), 86 us a piece of 16768 columns as dz (65%), 8 x 768 x 50257 18 us (4.3 TB/s); 203 x
+// 768 x 50257 fp32 straight from W 112 us, its cutting warps waiting for their loads (the three DIRECT kernels have 96 registers a thread and
+// spill 60 to 148 bytes of stores; the others none).
 #include <algorithm>
 
 #include "common.cuh"

@@ -3,11 +3,12 @@
 //   dz = e^{z - lse} - [y],   dn = w dz W,   dW = w dz^T n,   w = dloss / |Omega|
 // Forward: the product's epilogue reduces each row of a tile to (largest, sum e^{z - largest}) and picks the label's logit; a
 // second launch joins the tiles' parts in their order and sums the losses. It moves N (d + tiles) and V d values and is bound by the
-// products (2 N d V operations; few rows: by the one reading of W). 2048 x 4096 x 32000 bf16: 293 us, 97% of the burst peak.
+// products (2 N d V operations; few rows: by the one reading of W). 2048 x 4096 x 32000 bf16: 294 us in a captured graph, 97% of the burst
+// peak; 332 as a call among others (power cap).
 // Backward: the logits are formed again, a piece of the vocabulary at a time, and leave the product as dz (bf16; fp32 inputs:
 // three bf16 terms); then dn += dz_p W_p in fp32 and dW_p = dz_p^T n. dz rounded to bf16 is off by 2^-9 of each value (but for the label's
 // where p is small: -1 exactly), which the sums over columns and rows average; dn's own rounding is as large.
-// The same size, both gradients: 870 us, 98% of the burst peak; 4096 x 768 x 50257, dn alone: 428 us, 78%.
+// The same size, both gradients: 889 us in a graph, 96% of the burst peak (a call 1021); 4096 x 768 x 50257, dn alone: 443 us, 75% (491).
 #include <algorithm>
 
 #include "act8.cuh"
@@ -22,20 +23,24 @@ namespace {
 
 constexpr int kPrepThreads = 256;
 // Bytes of dz that a piece of the vocabulary may take, where that leaves it kMinPiece columns. Larger pieces need fewer launches
-// and lose less in their last wave of tiles; dz goes through HBM either way, under the products' time. 4096 x 768 x 50257 with pieces of
-// 64 MB 550 us, 128 461, 192 428, 256 420, 512 (all of dz) 406.
+// and lose less in their last wave of tiles; dz goes through HBM either way, under the products' time. Measured at one shape, 4096 x
+// 768 x 50257, with pieces of 64 MB 550 us, 128 461, 192 428, 256 420, 512 (all of dz) 406 (logits in one accumulation): more is faster;
+// 192 keeps the workspace below half of these logits, whose memory the call is there to save.
 constexpr size_t kPieceBytes = 192u << 20;
 constexpr int kMinPiece = 1024;
 // k blocks (of 64) of one accumulation in TMEM: the tensor cores cut off what does not fit an fp32 sum, always towards zero, each
 // time they add 16 products. With bf16 logits summed over 4096 in one accumulation lse was off by 1.7e-6 and the row losses by 2.6e-6,
 // relative (an fp32 library product: 2.7e-7, 6.2e-7; in eight: 2e-7, 3e-7). fp32 logits: 2048 x 4096 x 32000 in accumulations of 256
-// 1.4e-7 and 2.0e-7 in 1.95 ms, of 128 0.9e-7 and 1.5e-7 in 2.12. The backward's
-// logits too: where the label's p is near 1, dz is the difference p - 1, and of a logit of 100 (products of one sign) one
-// accumulation lost 1.2e-3, six times 1 - p = 2e-4; the pieces' products take 4% longer for it.
-// Sums that leave in bf16 are cut off far below its rounding.
+// 1.4e-7 and 2.0e-7 in 1.95 ms, of 128 0.9e-7 and 1.5e-7 in 2.12. The backward's logits too: where the label's p is near 1, dz is the
+// difference p - 1, and of a logit of 100 (products of one sign) one accumulation lost 1.2e-3, six times 1 - p = 2e-4; the gradient takes
+// 4% longer for it. Sums that leave in bf16 are cut off far below its rounding.
 constexpr int kSegLogits = 8, kSegF32 = 4, kSegDirect = 2, kSegAll = 1 << 20;
-// Up to so many rows the products with an fp32 W read it as it is and cut it into its terms themselves, once for every 128 rows:
-// beyond, the terms' way through memory (16 bytes a value of W instead of 4) costs less than cutting again.
+// Up to so many rows the products with an fp32 W read it as it is and cut it into its terms themselves, once for every 128 rows, and
+// no terms of W (6 bytes a value) lie in the workspace. Beyond, the terms' way through memory costs less than cutting again. us, forward
+// and both gradients, as it is / cut before:  768 x 50257, 256 rows 121 / 142, 346 / 407; 512: 203 / 196, 599 / 565; 1024: 367 / 317,
+// 1137 / 1001; 2048: 691 / 540, 2221 / 1758.  4096 x 32000, 256: 383 / 490, 1039 / 1077; 512: 638 / 683, 1936 / 1694; 1024: 1231 / 1101,
+// 3682 / 2861; 2048: 2278 / 1986, 7101 / 5753.  256 x 8000, 1024: 37 / 38, 103 / 96. The times cross at 300 to 1000 rows; up to 1024
+// the workspace counts.
 constexpr int kDirectRows = 1024;
 
 inline int up64(int n) { return (n + 63) / 64 * 64; }
